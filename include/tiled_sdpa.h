@@ -44,8 +44,10 @@ enum {
     TSDPA_ERR_WORKSPACE = 9,     /* tiled_sdpa_fwd_kv with more than one split, tiled_sdpa_bwd: workspace NULL,
                                     not 16-byte aligned, or smaller than the matching *_workspace_bytes reports */
     TSDPA_ERR_BAD_SPLITS = 10,   /* splits < 0 or > TSDPA_MAX_SPLITS                         */
-    TSDPA_ERR_STATIC_SCRATCH = 11 /* tiled_sdpa_fwd_kvcache_static: the split states need more than
+    TSDPA_ERR_STATIC_SCRATCH = 11, /* tiled_sdpa_fwd_kvcache_static: the split states need more than
                                     TSDPA_STATIC_SCRATCH_BYTES, or the buffer's address cannot be obtained */
+    TSDPA_ERR_BAD_EPS = 12,      /* eps is negative, infinite or NaN                         */
+    TSDPA_ERR_BAD_STRIDE = 13    /* a stride of rows is negative or not a multiple of 8 elements, or rows to be written overlap */
 };
 
 enum { TSDPA_MAX_SPLITS = 128 };
@@ -265,6 +267,28 @@ int tiled_sdpa_fwd_paged(const void *q, const void *k_pages, const void *v_pages
                          float scale, int dtype, void *stream, int tile_m, int tile_n, unsigned flags,
                          int splits, void *workspace, unsigned long long workspace_bytes);
 
+/*
+ * tiled_sdpa_fwd_kvcache and tiled_sdpa_fwd_paged for a tree of drafted tokens (speculative decoding): the T queries of an entry are
+ * tokens of a tree whose keys are the last T rows of the entry's kv_lens[b], and each sees the rows before those (the cached
+ * sequence) and the tokens that its mask names.
+ *
+ *   mask       : device int64, ceil(T / 64) words per token, 8-byte aligned: bit j % 64 of word j / 64 of token i is set iff token i sees
+ *                token j (key row kv_lens[b] - T + j); tiled_sdpa_tree_mask makes it, any other pattern is as good.  Bits from T on are
+ *                not looked at, nor are those of rows before the entry's first (an entry shorter than T).
+ *   mask_batch : words from one entry's mask to the next (at least T * ceil(T / 64)), 0 = one mask for all entries.
+ *
+ * A token that sees no key gets O = 0 and LSE = -infinity.  Values of keys that a token does not see do not reach it, whatever they
+ * are: rows of k or v of other tokens may hold infinities and NaN.  T <= 65536; everything else as for the two calls named
+ * (the tile is the library's choice; split counts and workspace as for grouped heads there).
+ */
+int tiled_sdpa_fwd_tree(const void *q, const void *k, const void *v, void *o, float *lse, const int *kv_lens,
+                        const long long *mask, long long mask_batch, int B, int H, int Hkv, int T, int Skv, int D,
+                        float scale, int dtype, void *stream, int splits, void *workspace, unsigned long long workspace_bytes);
+int tiled_sdpa_fwd_tree_paged(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,
+                              const int *kv_lens, const int *block_table, const long long *mask, long long mask_batch,
+                              int B, int H, int Hkv, int T, int max_blocks, int block_rows, int D,
+                              float scale, int dtype, void *stream, int splits, void *workspace, unsigned long long workspace_bytes);
+
 /* Splits the heuristic picks (1 when the query tiles alone fill the GPU); returns a status code. */
 int tiled_sdpa_kv_default_splits(int B, int H, int Sq, int Skv, int D, int dtype, unsigned flags, int *splits);
 /* The same for a call with an explicit tile (both 0: the value above).  The two differ where the heuristic would
@@ -337,6 +361,129 @@ unsigned long long tiled_sdpa_bwd_workspace_bytes(int B, int H, int S);
  * FP32 sums of dQ, about 4*B*H*S*D bytes and at most 2.3 GB; otherwise what tiled_sdpa_bwd_workspace_bytes says.  flags as for the
  * call.  Never fails: for arguments that the call refuses, the latter too. */
 unsigned long long tiled_sdpa_bwd_full_workspace_bytes(int B, int H, int Hkv, int S, int D, unsigned flags);
+
+/*
+ * ---- Around attention: trees of drafted tokens, a cache's pages, and queries and keys on their way to attention.
+ *
+ * Trees of drafted tokens (speculative decoding): parents [B, T] -> which tokens each token follows.
+ *
+ *   parents : device int32 [B, T]: the token that token i of a tree follows, an earlier one (0 <= parent < i); any other value
+ *             means that i follows the cached sequence itself.
+ *   mask    : device int64 [B, T, ceil(T/64)]: bit j % 64 of word j / 64 of row i is set iff j is i or one of its ancestors: what
+ *             tiled_sdpa_fwd_tree reads.  One mask serves all layers of a step.
+ *   depths  : NULL, or device int32 [B, T]: the number of ancestors: the token's distance from the first position behind the
+ *             cached sequence (see tiled_sdpa_cache_step).
+ *   T       : 0 ... 1024.
+ */
+int tiled_sdpa_tree_mask(const int *parents, long long *mask, int *depths, int B, int T, void *stream);
+
+/*
+ * The cache's side of a serving step: every entry of a batch appends tokens or drops some, and gets the pages it needs for
+ * that, the slot of each new token, and its position.  Nothing is read back by the host: a captured step serves any lengths.
+ *
+ *   kv_lens      : device int32 [B]: rows of each entry now.  An entry holds exactly ceil(rows / block_rows) pages, the first of
+ *                  its row of block_table.
+ *   counts       : device int32 [B]: rows to append (0 ... S), or to drop (negative: rejected drafts; -kv_lens[b] for a request
+ *                  that is done).
+ *   depths       : NULL, or device int32 [B, S] (tiled_sdpa_tree_mask): token i of an entry has position
+ *                  new_lens[b] - S + depths[b][i] instead of the one of its row.
+ *   block_table  : device int32 [B, max_blocks], in and out: as for tiled_sdpa_fwd_paged.  NULL = a dense cache [B, Hkv, block_rows, D]
+ *                  (entry b's rows are slots b * block_rows ...); free_pages and pool are then not looked at.
+ *   free_pages   : device int32 [pool_size], in and out: pages that no entry holds, the first pool[0] of them; room for all pages
+ *                  (page numbers are below pool_size).
+ *   pool         : device int32 [2]; pool[0] = pages in free_pages.
+ *   new_lens     : device int32 [B]: kv_lens + counts.
+ *   slots        : device int32 [B, S]: row new_lens[b] - S + i of entry b for token i, as page * block_rows + row in the page, if the
+ *                  step appended it; else -1 (entries with fewer than S new tokens have them at the end, as the queries of
+ *                  TSDPA_FLAG_CAUSAL are the last positions).
+ *   positions    : device int32 [B, S]: the row's position (0 where there is no slot).
+ *   new_pool     : device int32 [2]: pages free after the step, and 0; or, of a step that is REFUSED, the pages as they were and
+ *                  what is missing: pages (dense: rows) that the pool or the ends of entries lack, -1 if a length, count or pool
+ *                  cannot be one (negative, beyond the capacity, more than S).  A refused step changes nothing: new_lens =
+ *                  kv_lens, every slot -1.
+ *
+ * Pages go in this order: those given up (entry by entry) to those needed (entry by entry), then from the end of the pool; what is
+ * left of those given up goes on its end, the first last, so that dropping what was appended restores the pool.  Only
+ * block_table's columns from the pages held on and free_pages' elements from pool[0] on are written.  The outputs must not
+ * overlap the inputs (new_lens and new_pool are others than kv_lens and pool, to be exchanged from step to step).
+ * B <= 8192; page numbers times block_rows, B * S and B * max_blocks fit an int.
+ */
+int tiled_sdpa_cache_step(const int *kv_lens, const int *counts, const int *depths, int *block_table, int *free_pages, const int *pool,
+                          int *new_lens, int *slots, int *positions, int *new_pool,
+                          int B, int S, int max_blocks, int block_rows, int pool_size, void *stream);
+
+/* Rows of D values of [B, S, heads, D], strides in elements: a projection's output, or a view into a packed one.  data is 16-byte
+ * aligned, the values of a row are adjacent, the strides are multiples of 8. */
+typedef struct {
+    void *data;
+    long long batch, row, head;
+} tsdpa_rows;
+
+enum { TSDPA_FLAG_INTERLEAVED = 16u };   /* pairs are neighbouring columns (2 i, 2 i + 1) instead of (i, i + rot / 2) */
+enum { TSDPA_F32 = 2 };                  /* a type of weights */
+
+/* Norm and rotation of queries and keys: what the three calls below have in common. */
+typedef struct {
+    int B, S, H, Hkv, D;         /* D: 64, 96, 128 or 160 */
+    int dtype;                   /* of the rows: TSDPA_F16 or TSDPA_BF16 */
+    int rot;                     /* columns 0 ... rot - 1 are rotated; a multiple of 16, 0 ... D */
+    unsigned flags;              /* TSDPA_FLAG_INTERLEAVED or 0 */
+    float eps;                   /* >= 0 */
+    int weight_dtype;            /* TSDPA_F32 or the rows' */
+    const void *q_weight, *k_weight;   /* device [D], 16-byte aligned; NULL: that tensor is rotated without a norm */
+    const int *positions;        /* device int32; token (b, s) is at positions[axis * pos_axis + b * pos_batch + s] on an axis */
+    long long pos_batch, pos_axis;
+    const float *inv_freq;       /* device FP32 [rot / 2]: angle of a pair = position * inv_freq, radians */
+    const int *axes;             /* NULL (one axis), or device int32 [rot / 2]: the axis of each pair, 0 ... n_axes - 1 (clamped to that) */
+    int n_axes;
+} tsdpa_rope;
+
+/*
+ * Queries and keys from the projection to attention, in one pass: the RMS norm of each head's row, the weight of each column, the
+ * rotation of each pair (a, b) by its angle,
+ *     y = x / sqrt(mean(x^2) + eps) * w,     (y_a cos - y_b sin, y_b cos + y_a sin),
+ * and the layout.  FP32 throughout (angles in 64 bits up to whole turns: any position is as exact as the first), one rounding.  The mean
+ * of squares is taken in FP32: BF16 values whose squares overflow it (beyond 1e18) have no norm.
+ *
+ *   q, k         : tsdpa_rows of [B, S, H, D] and [B, S, Hkv, D].
+ *   q_out, k_out : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned: what tiled_sdpa_fwd and its kin read.  Must not
+ *                  overlap the inputs.
+ *
+ * Validation order, of all three calls: dtypes, D, shape (rot, n_axes, the cache's among it), empty problem, null pointers, alignment,
+ * strides, eps, workspace, launch.
+ */
+int tiled_sdpa_qk_norm_rope(const tsdpa_rope *p, const tsdpa_rows *q, const tsdpa_rows *k, void *q_out, void *k_out, void *stream);
+
+/*
+ * The serving form: q as above, k (normed, rotated) and v (as it is) to their slots of a cache.
+ *
+ *   v                : tsdpa_rows of [B, S, Hkv, D].
+ *   slots            : device int32 [B, S] (tiled_sdpa_cache_step): token's row in the cache, page * block_rows + row in the page.  A
+ *                      token whose slot is negative or past the last page's is not written.  Tokens with the same slot: one of them
+ *                      is, row by row and which one is not said.
+ *   k_cache, v_cache : [pages, Hkv, block_rows, D] (of a dense cache [B, Hkv, Skv, D]: pages = B, block_rows = Skv); pages *
+ *                      block_rows fits an int.  Other rows are left as they are.
+ */
+int tiled_sdpa_qk_norm_rope_cache(const tsdpa_rope *p, const tsdpa_rows *q, const tsdpa_rows *k, const tsdpa_rows *v, const int *slots,
+                                  void *q_out, void *k_cache, void *v_cache, int pages, int block_rows, void *stream);
+
+/*
+ * Backward of tiled_sdpa_qk_norm_rope: given the gradients of q_out and k_out, those of q, k and the weights.  With g the gradient
+ * rotated back and r = 1 / sqrt(mean(x^2) + eps) (computed again):
+ *     dw = sum over the rows of g * x * r,     dx = r * (g * w - x * r * mean(g * w * x * r)).
+ *
+ *   dq_out, dk_out     : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned.
+ *   q, k               : as for the forward call (without weights they are not looked at).
+ *   dq, dk             : tsdpa_rows to be written, of the shapes of q and k; every element is overwritten.
+ *   dq_weight, dk_weight : [D] in weight_dtype; not looked at (may be NULL) where there is no weight.
+ *   workspace          : device, 16-byte aligned, at least tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(B, S, D) bytes; not looked at
+ *                        without weights.  Calls that may overlap on the GPU need distinct ones.
+ * The weights' sums are FP32 in a fixed order: results are deterministic.
+ */
+int tiled_sdpa_qk_norm_rope_bwd(const tsdpa_rope *p, const void *dq_out, const void *dk_out, const tsdpa_rows *q, const tsdpa_rows *k,
+                                const tsdpa_rows *dq, const tsdpa_rows *dk, void *dq_weight, void *dk_weight,
+                                void *workspace, unsigned long long workspace_bytes, void *stream);
+unsigned long long tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(int B, int S, int D);
 
 /*
  * Measurement aid, not part of the attention path: enqueue a register-resident stream of

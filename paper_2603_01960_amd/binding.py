@@ -2,7 +2,8 @@
 
 Every step of the forward pass runs in the HIP kernels behind the C-ABI declared
 in include/tiled_sdpa.h.  PyTorch supplies device memory and the current stream.
-The tensor functions (sdpa, sdpa_kv, sdpa_paged, sdpa_backward) go through native
+The tensor functions (sdpa, sdpa_kv, sdpa_paged, sdpa_backward, sdpa_tree, sdpa_tree_paged; tree_mask, cache_step,
+qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward around them) go through native
 code (csrc/torch_calls.cpp), the C-ABI itself is exposed through ctypes.
 There is no CPU fallback: if the library is missing, loading raises.
 """
@@ -12,10 +13,11 @@ import ctypes
 import math
 from pathlib import Path
 
-F16, BF16 = 0, 1
+F16, BF16, F32 = 0, 1, 2
 FLAG_LINEAR_GRID = 1
 FLAG_EXACT_MAX = 2
 FLAG_CAUSAL = 8
+FLAG_INTERLEAVED = 16
 
 _PKG = Path(__file__).resolve().parent
 _LIB_PATH = _PKG / "libtiled_sdpa.so"
@@ -37,6 +39,14 @@ EXPORTS = (
     "tiled_sdpa_fwd_kvcache",
     "tiled_sdpa_fwd_kvcache_static",
     "tiled_sdpa_fwd_paged",
+    "tiled_sdpa_fwd_tree",
+    "tiled_sdpa_fwd_tree_paged",
+    "tiled_sdpa_tree_mask",
+    "tiled_sdpa_cache_step",
+    "tiled_sdpa_qk_norm_rope",
+    "tiled_sdpa_qk_norm_rope_cache",
+    "tiled_sdpa_qk_norm_rope_bwd",
+    "tiled_sdpa_qk_norm_rope_bwd_workspace_bytes",
     "tiled_sdpa_kv_default_splits",
     "tiled_sdpa_kv_tile_splits",
     "tiled_sdpa_kv_workspace_bytes",
@@ -51,6 +61,20 @@ class TiledSdpaError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"tiled_sdpa status {status}: {text}")
         self.status = status
+
+
+class Rows(ctypes.Structure):
+    """tsdpa_rows: rows of [B, S, heads, D], strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("row", ctypes.c_longlong), ("head", ctypes.c_longlong)]
+
+
+class Rope(ctypes.Structure):
+    """tsdpa_rope: what the calls that normalise and rotate queries and keys have in common."""
+    _fields_ = [("B", ctypes.c_int), ("S", ctypes.c_int), ("H", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("rot", ctypes.c_int), ("flags", ctypes.c_uint), ("eps", ctypes.c_float), ("weight_dtype", ctypes.c_int),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("pos_batch", ctypes.c_longlong), ("pos_axis", ctypes.c_longlong), ("inv_freq", ctypes.c_void_p), ("axes", ctypes.c_void_p),
+                ("n_axes", ctypes.c_int)]
 
 
 def library_path() -> Path:
@@ -102,6 +126,23 @@ def load_library():
     lib.tiled_sdpa_bwd_workspace_bytes.argtypes = [ci, ci, ci]
     lib.tiled_sdpa_bwd_full_workspace_bytes.restype = ctypes.c_ulonglong
     lib.tiled_sdpa_bwd_full_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ctypes.c_uint]
+    lib.tiled_sdpa_fwd_tree.restype = ci
+    lib.tiled_sdpa_fwd_tree.argtypes = [vp] * 7 + [ctypes.c_longlong] + [ci] * 6 + [cf, ci, vp, ci, vp, ctypes.c_ulonglong]
+    lib.tiled_sdpa_fwd_tree_paged.restype = ci
+    lib.tiled_sdpa_fwd_tree_paged.argtypes = [vp] * 8 + [ctypes.c_longlong] + [ci] * 7 + [cf, ci, vp, ci, vp, ctypes.c_ulonglong]
+    lib.tiled_sdpa_tree_mask.restype = ci
+    lib.tiled_sdpa_tree_mask.argtypes = [vp] * 3 + [ci, ci, vp]
+    lib.tiled_sdpa_cache_step.restype = ci
+    lib.tiled_sdpa_cache_step.argtypes = [vp] * 10 + [ci] * 5 + [vp]
+    rows = ctypes.POINTER(Rows)
+    lib.tiled_sdpa_qk_norm_rope.restype = ci
+    lib.tiled_sdpa_qk_norm_rope.argtypes = [ctypes.POINTER(Rope), rows, rows, vp, vp, vp]
+    lib.tiled_sdpa_qk_norm_rope_cache.restype = ci
+    lib.tiled_sdpa_qk_norm_rope_cache.argtypes = [ctypes.POINTER(Rope), rows, rows, rows, vp, vp, vp, vp, ci, ci, vp]
+    lib.tiled_sdpa_qk_norm_rope_bwd.restype = ci
+    lib.tiled_sdpa_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(Rope), vp, vp, rows, rows, rows, rows, vp, vp, vp, ctypes.c_ulonglong, vp]
+    lib.tiled_sdpa_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_ulonglong
+    lib.tiled_sdpa_qk_norm_rope_bwd_workspace_bytes.argtypes = [ci, ci, ci]
     lib.tiled_sdpa_probe_hbm_read.restype = ci
     lib.tiled_sdpa_probe_hbm_read.argtypes = [vp, ctypes.c_ulonglong, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.tiled_sdpa_probe_mfma.restype = ci
@@ -299,6 +340,71 @@ def sdpa_paged(q, k_pages, v_pages, kv_lens, block_table, causal: bool = False, 
     (valid key rows per entry).  See tiled_sdpa_fwd_paged; otherwise as :func:`sdpa_kv`."""
     return _checked(_calls().sdpa_paged(q, k_pages, v_pages, kv_lens, block_table, causal, scale, splits, return_lse, out,
                                         workspace, tile, flags))
+
+
+def sdpa_tree(q, k, v, mask, scale=None, *, kv_lens=None, splits: int = 0, return_lse: bool = False, out=None, workspace=None):
+    """Attention of a tree of drafted tokens, q [B, H, T, D], over a dense cache k, v [B, Hkv, Skv, D] whose last T valid rows are the
+    tokens' own: each sees the rows before those and the tokens that ``mask`` names (int64 [B, T, ceil(T / 64)] of :func:`tree_mask`,
+    or [T, ceil(T / 64)] for all entries; bit j of token i's words: i sees j).  A token that sees no key comes back as zeros; what
+    it does not see does not reach it, infinities and NaN included.  See tiled_sdpa_fwd_tree; otherwise as :func:`sdpa_kv`."""
+    return _checked(_calls().sdpa_tree(q, k, v, kv_lens, None, mask, scale, splits, return_lse, out, workspace))
+
+
+def sdpa_tree_paged(q, k_pages, v_pages, kv_lens, block_table, mask, scale=None, *, splits: int = 0, return_lse: bool = False, out=None,
+                    workspace=None):
+    """:func:`sdpa_tree` over a paged cache (``k_pages``, ``v_pages``, ``kv_lens``, ``block_table`` as for :func:`sdpa_paged`)."""
+    if block_table is None:
+        raise ValueError("block_table must be a contiguous int32 tensor [B, max_blocks] on the device of q")
+    return _checked(_calls().sdpa_tree(q, k_pages, v_pages, kv_lens, block_table, mask, scale, splits, return_lse, out, workspace))
+
+
+def tree_mask(parents, *, out=None):
+    """(mask, depths) of trees of drafted tokens: ``parents`` int32 [B, T] (or [T]) names the earlier token of the tree that each token
+    follows, any other value the cached sequence.  mask int64 [B, T, ceil(T / 64)]: bit j of token i's words is set iff j is i or one of its
+    ancestors (what :func:`sdpa_tree` reads); depths int32 [B, T]: how many ancestors (what :func:`cache_step` takes).  T <= 1024."""
+    return _checked(_calls().tree_mask(parents, out))
+
+
+def cache_step(kv_lens, counts, S: int, block_rows: int, *, pages=None, depths=None, out=None):
+    """(new_lens, slots, positions, new_pool) of a serving step that appends ``counts[b]`` (0 ... S) rows to entry b of a cache, or drops
+    that many (negative: rejected drafts, finished requests).  slots and positions are int32 [B, S], an entry's new tokens at the end
+    of its row, -1 (and 0) before them: what :func:`qk_norm_rope_cache` takes.
+
+    ``pages = (block_table, free_pages, pool)`` of a paged cache: int32 [B, max_blocks] and [pool_size], changed in place, and the
+    int32 [2] that the last step returned as new_pool (at first: the number of pages in free_pages, 0).  Without it the cache is
+    dense, [B, Hkv, block_rows, D].  new_pool[1] != 0 says that the step was refused (pages or rows missing, -1: numbers that cannot
+    be) and changed nothing.  ``depths`` (of :func:`tree_mask`): the tokens of a tree have the position of their depth.
+
+    Nothing is read back by the host.  new_lens and new_pool must not be kv_lens and pool.  See tiled_sdpa_cache_step."""
+    return _checked(_calls().cache_step(kv_lens, counts, S, block_rows, pages, depths, out))
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, *, axes=None, eps: float = 1e-6, interleaved: bool = False, out=None):
+    """Queries and keys from the projection to attention in one pass: RMS norm of each head's row, weights, rotation by position, and the
+    layout.  q [B, S, H, D] and k [B, S, Hkv, D] may be views into one packed tensor (strides in multiples of 8 elements); the results are
+    [B, H, S, D] and [B, Hkv, S, D], contiguous.
+
+    ``q_weight``, ``k_weight`` [D] (float32 or the dtype of q; None: no norm of that tensor).  ``inv_freq`` float32 [rot / 2]: the angle of
+    pair i is position * inv_freq[i]; columns past rot (a multiple of 16) are not rotated; pairs are columns (i, i + rot / 2), or
+    neighbours if ``interleaved``.  ``positions`` int32 [S] or [B, S]; with several axes (time, height, width) [A, S] or [A, B, S], and
+    ``axes`` int32 [rot / 2] names each pair's.  See tiled_sdpa_qk_norm_rope."""
+    return _checked(_calls().qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, out))
+
+
+def qk_norm_rope_cache(q, k, v, q_weight, k_weight, positions, inv_freq, k_cache, v_cache, slots, *, axes=None, eps: float = 1e-6,
+                       interleaved: bool = False, out=None):
+    """:func:`qk_norm_rope` for a serving step: returns q for attention, and writes k (normed, rotated) and v [B, S, Hkv, D] (as it is) to
+    the rows ``slots`` (int32 [B, S], of :func:`cache_step`; negative: nowhere) of the cache [pages, Hkv, block_rows, D], or of a dense one
+    [B, Hkv, Skv, D].  See tiled_sdpa_qk_norm_rope_cache."""
+    return _checked(_calls().qk_norm_rope_cache(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, v, k_cache, v_cache, slots, out))
+
+
+def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_freq, *, axes=None, eps: float = 1e-6,
+                          interleaved: bool = False, workspace=None, grads=None):
+    """(dq, dk, dq_weight, dk_weight) of :func:`qk_norm_rope`, given the gradients [B, H, S, D] and [B, Hkv, S, D] of its results and its
+    arguments.  ``grads=(dq, dk)`` lets the caller own these (views into one packed tensor, for example); the weights' gradients are
+    in the weights' dtype, None where there is no weight.  See tiled_sdpa_qk_norm_rope_bwd."""
+    return _checked(_calls().qk_norm_rope_backward(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, dq_out, dk_out, workspace, grads))
 
 
 def bwd_workspace_bytes(B: int, H: int, S: int) -> int:

@@ -45,7 +45,7 @@ def extra_flags(src: Path) -> list[str]:
     name = src.name
     if name.startswith("sdpa_bwd_chain_"):
         return MFMA_VGPR
-    if name.startswith("sdpa_fwd_") and name.endswith("_tn64.hip") and "_d160_" not in name:
+    if name.startswith(("sdpa_fwd_", "sdpa_tree_")) and name.endswith("_tn64.hip") and "_d160_" not in name:
         return ILP_SCHED
     if name.startswith("sdpa_bwd_") and not name.endswith("_d128.hip"):
         return ILP_SCHED

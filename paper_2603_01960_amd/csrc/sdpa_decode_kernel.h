@@ -149,14 +149,17 @@ template <> struct DecodeRead<160> {
 #undef TSDPA_RD_WAIT
 
 // PAGED: a descriptor per tile (see the forward kernel's paged variant).  HALVES: each weight multiplied as two 16-bit halves,
-// see pick_halves (an instantiation of its own: the code alone costs the shortest calls 0.3 us).
-template <typename T, int D, int NQ, int NW, bool PAGED, bool HALVES>
+// see pick_halves (an instantiation of its own: the code alone costs the shortest calls 0.3 us).  TREE: the queries are a tree of drafted
+// tokens (see the forward kernel's); of at most 32 rows the tree has at most 32 tokens, and a row's bits are one word, which a tile
+// shifts to where its keys lie.
+template <typename T, int D, int NQ, int NW, bool PAGED, bool HALVES, bool TREE = false>
 __global__ void __launch_bounds__(NW * 64, 2)
 sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v,
                    T *o, float *__restrict__ lse, int S, int heads, float c, float tau, uint32_t qsign, int causal,
                    int Skv_cap, int splits, float *ws, int rows_per_head,
                    const int *__restrict__ kv_lens, int heads_per_batch, int batches,
-                   const int *__restrict__ block_table, int max_blocks, int block_shift, unsigned long long ticket)
+                   const int *__restrict__ block_table, int max_blocks, int block_shift, unsigned long long ticket,
+                   const uint32_t *__restrict__ tree, long long tree_batch, int tree_words)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using E = Elem16<T>;
@@ -405,8 +408,22 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
             raw ^= qsign;
             qf[nq][ks] = __builtin_bit_cast(vec8, raw);
         }
-        klim[nq] = causal ? row % rows_per_head + len - rows_per_head : len - 1;
+        klim[nq] = TREE ? len - rows_per_head - 1 : causal ? row % rows_per_head + len - rows_per_head : len - 1;
     }
+    // trees: the tokens that the lane's row sees, and of a tile (shifted by t * 4: bit b * 16 + e is for score (b, e))
+    uint32_t tree_row[TREE ? NQ : 1], sees[TREE ? NQ : 1];
+    if constexpr (TREE) {
+        const uint32_t *entry = tree + (size_t)(head / heads_per_batch) * tree_batch;
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int row = nq * 16 + l16 < S ? nq * 16 + l16 : S - 1;
+            tree_row[nq] = entry[(size_t)(row % rows_per_head) * tree_words] & (rows_per_head < 32 ? (1u << rows_per_head) - 1u : ~0u);
+        }
+    }
+    auto hidden = [&](int key0, int nq, int b, int e) __attribute__((always_inline)) {
+        if constexpr (TREE) return (sees[nq] & (1u << (b * 16 + e))) == 0;
+        else return key0 + b * 16 + e > klim[nq];
+    };
 
     // the first tile's loads go out behind Q's (whose wait then leaves them on their way)
     __builtin_amdgcn_sched_barrier(0);
@@ -449,7 +466,7 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], c, -m_ref[nq]));
-                if (key0 + b * 16 + e > klim[nq]) p = 0.f;
+                if (hidden(key0, nq, b, e)) p = 0.f;
                 sum += p;
                 pb[nq][b * 4 + e] = (T)(HALVES ? 0.5f * p : p);
                 if constexpr (HALVES) ph[nq][b * 4 + e] = (T)(p - (float)pb[nq][b * 4 + e]);
@@ -477,6 +494,18 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
                 for (int ks = 0; ks < KS; ++ks) sacc[nq][b] = E::mfma(__builtin_bit_cast(vec8, kf[b][ks]), qf[nq][ks], sacc[nq][b]);
             }
         const int key0 = (t0 + cur) * kDecodeTile + t * 4;
+        // where the tile's first key lies in the tree (below -31: all of it before the tree, as most tiles are)
+        const int in_tree = (t0 + cur) * kDecodeTile - (len - rows_per_head);
+        if constexpr (TREE) {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+                const uint32_t x = in_tree <= -32 ? ~0u : in_tree < 0 ? __builtin_amdgcn_alignbit(tree_row[nq], ~0u, in_tree & 31)
+                                 : in_tree < 32 ? tree_row[nq] >> in_tree : 0u;
+                // (a row that no key of the wavefront's tiles reached so far; the four lanes of a row have the same bits)
+                if (m_ref[nq] == -INFINITY && x != 0) m_ref[nq] = kNoWeight;
+                sees[nq] = x >> (t * 4);
+            }
+        }
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             float ps = exponentials(sacc[nq], nq, key0);
@@ -487,7 +516,7 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (key0 + b * 16 + e <= klim[nq]) mx = fmaxf(mx, sacc[nq][b][e]);
+                        if (!hidden(key0, nq, b, e)) mx = fmaxf(mx, sacc[nq][b][e]);
                 mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
                 mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
                 const float m_tile = mx * c;
@@ -510,7 +539,27 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
         load_v(s);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            const i16x8 a = __builtin_shufflevector(vf[db][0], vf[db][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            i16x8 a = __builtin_shufflevector(vf[db][0], vf[db][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (TREE) {
+                const u32x4 raw = __builtin_bit_cast(u32x4, a);
+                if (in_tree > -32 && __builtin_amdgcn_ballot_w64(NotFinite<T>::any(raw)) != 0) {
+                    u32x4 finite, up, down, seen;
+                    NotFinite<T>::take_apart(raw, finite, up, down);
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            seen[i] = (hidden(0, nq, i >> 1, (i & 1) * 2) ? 0u : NotFinite<T>::ONE & 0xffffu) |
+                                      (hidden(0, nq, i >> 1, (i & 1) * 2 + 1) ? 0u : NotFinite<T>::ONE & 0xffff0000u);
+                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                        const f32x4 ups = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), zero);
+                        const f32x4 downs = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), zero);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) oacc[nq][db][e] += NotFinite<T>::excess(ups[e], downs[e]);
+                    }
+                    a = __builtin_bit_cast(i16x8, finite);
+                }
+            }
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) {
                 oacc[nq][db] = E::mfma(__builtin_bit_cast(vec8, a), pb[nq], oacc[nq][db]);
@@ -596,9 +645,9 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
 #endif
 }
 
-template <typename T, int D, int NQ, int NW, bool PAGED, bool HALVES> int launch_decode_one(const LaunchArgs &a)
+template <typename T, int D, int NQ, int NW, bool PAGED, bool HALVES, bool TREE = false> int launch_decode_one(const LaunchArgs &a)
 {
-    auto kern = sdpa_decode_kernel<T, D, NQ, NW, PAGED, HALVES>;
+    auto kern = sdpa_decode_kernel<T, D, NQ, NW, PAGED, HALVES, TREE>;
     constexpr int lds_bytes = NW * 2 * DecodeGeom<D>::TILE;
     static_assert(NW * NQ * 16 * D * 4 <= lds_bytes, "the states of all wavefronts must fit");
     static std::once_flag once;
@@ -609,7 +658,8 @@ template <typename T, int D, int NQ, int NW, bool PAGED, bool HALVES> int launch
     if (attr_err != hipSuccess) return (int)attr_err;
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.BH * a.splits)), dim3(NW * 64), lds_bytes, a.stream,
                        (const T *)a.q, (const T *)a.k, (const T *)a.v, (T *)a.o, a.lse, a.S, a.BH, a.c, a.tau, a.qsign, a.causal,
-                       a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.heads_per_batch, a.batches, a.block_table, a.max_blocks, a.block_shift, a.ticket);
+                       a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.heads_per_batch, a.batches, a.block_table, a.max_blocks, a.block_shift, a.ticket,
+                       a.tree, a.tree_batch, a.tree_words);
     return (int)hipGetLastError();
 }
 
@@ -633,6 +683,28 @@ template <typename T> int launch_decode(int D, const LaunchArgs &a)
         case 96: return launch_decode_dim<T, 96>(a);
         case 128: return launch_decode_dim<T, 128>(a);
         default: return launch_decode_dim<T, 160>(a);
+    }
+}
+
+template <typename T, int D, int NQ> int launch_tree_decode_rows(const LaunchArgs &a)
+{
+    if (decode_waves(a.BH, a.splits, a.Skv) == 8)
+        return a.block_table ? launch_decode_one<T, D, NQ, 8, true, false, true>(a) : launch_decode_one<T, D, NQ, 8, false, false, true>(a);
+    return a.block_table ? launch_decode_one<T, D, NQ, 4, true, false, true>(a) : launch_decode_one<T, D, NQ, 4, false, false, true>(a);
+}
+
+template <typename T, int D> int launch_tree_decode_dim(const LaunchArgs &a)
+{
+    return a.S > 16 ? launch_tree_decode_rows<T, D, 2>(a) : launch_tree_decode_rows<T, D, 1>(a);
+}
+
+template <typename T> int launch_tree_decode(int D, const LaunchArgs &a)
+{
+    switch (D) {
+        case 64: return launch_tree_decode_dim<T, 64>(a);
+        case 96: return launch_tree_decode_dim<T, 96>(a);
+        case 128: return launch_tree_decode_dim<T, 128>(a);
+        default: return launch_tree_decode_dim<T, 160>(a);
     }
 }
 

@@ -21,7 +21,7 @@ constexpr int kLdsPerCU = 160 * 1024;
 // halves and move them back and forth (or to scratch) inside the loop.
 template <int D, int NW, int TN> constexpr int waves_per_simd() { return (TN == 32 && D <= 128) ? 3 : 2; }
 
-template <typename T, int D, int NW, int TN, int KV = 0, int NS = 1>     // KV: 0 square, 1 dense cache, 2 paged cache, 3 and 4 these with halved weights; NS streams
+template <typename T, int D, int NW, int TN, int KV = 0, int NS = 1>     // KV: 0 square, 1 dense cache, 2 paged cache, 3 and 4 these with halved weights, 5 and 6 with trees; NS streams
 int launch_one(const LaunchArgs &a)
 {
     constexpr int WPS = NS > 1 ? 2 : waves_per_simd<D, NW, TN>();
@@ -61,7 +61,8 @@ int launch_one(const LaunchArgs &a)
                        (const T *)a.q, (const T *)a.k, (const T *)a.v, (T *)a.o, a.lse,
                        a.S, nQ, N, a.c, a.tau, a.qsign, a.linear_grid, a.causal, order,
                        a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.heads_per_batch,
-                       a.block_table, a.max_blocks, a.block_shift, a.tile_rot, a.batches, divisor((uint32_t)(KV ? a.batches : 1)));
+                       a.block_table, a.max_blocks, a.block_shift, a.tile_rot, a.batches, divisor((uint32_t)(KV ? a.batches : 1)),
+                       a.tree, a.tree_batch, a.tree_words);
     return (int)hipGetLastError();
 }
 

@@ -181,6 +181,35 @@ constexpr float kNoWeight = -__FLT_MAX__;
 // two in front of every LDS read of the loop (one vector-ALU instruction per read).
 #define TSDPA_OPAQUE(x) asm volatile("" : "+v"(x))
 
+// Values that are not finite, in keys that only some rows see (trees of drafted tokens): the product with a weight of 0 would be NaN for
+// the rows that do not see the key.  So where a fragment of V (eight 16-bit values per lane, as A-operand) holds such a value, it
+// is taken apart: what is finite; where a +infinity or NaN stands; where a -infinity or NaN does (as ones).  A row gets +infinity
+// if it sees one of the second kind, -infinity of the third, NaN by both.
+template <typename T> struct NotFinite {
+    static constexpr bool F16 = std::is_same<T, _Float16>::value;
+    static constexpr uint32_t EXP = F16 ? 0x7c007c00u : 0x7f807f80u, STEP = F16 ? 0x04000400u : 0x00800080u;
+    static constexpr uint32_t MANT = F16 ? 0x03ff03ffu : 0x007f007fu, ONE = F16 ? 0x3c003c00u : 0x3f803f80u;
+    // 0x8000 in the halves whose exponent is all ones
+    static __device__ __forceinline__ uint32_t marks(uint32_t x) { return ((x & EXP) + STEP) & 0x80008000u; }
+    static __device__ __forceinline__ uint32_t whole(uint32_t marks) { return (marks >> 15) * 0xffffu; }
+    static __device__ __forceinline__ bool any(u32x4 x) { return (marks(x[0]) | marks(x[1]) | marks(x[2]) | marks(x[3])) != 0; }
+    static __device__ __forceinline__ void take_apart(u32x4 x, u32x4 &finite, u32x4 &up, u32x4 &down)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t m = marks(x[i]), bad = whole(m), nan = whole(((x[i] & MANT) + 0x7fff7fffu) & m), minus = whole(x[i] & 0x80008000u);
+            finite[i] = x[i] & ~bad;
+            up[i] = bad & (nan | ~minus) & ONE;
+            down[i] = bad & (nan | minus) & ONE;
+        }
+    }
+    // what is to be added for counts of such keys that a row sees
+    static __device__ __forceinline__ float excess(float up, float down)
+    {
+        return (up > 0.f ? INFINITY : 0.f) + (down > 0.f ? -INFINITY : 0.f);
+    }
+};
+
 // s_waitcnt vmcnt(0) with the other counters left at their maxima (gfx9 encoding)
 #define TSDPA_WAIT_VMCNT0() __builtin_amdgcn_s_waitcnt(0x0F70)
 
@@ -203,7 +232,10 @@ constexpr float kNoWeight = -__FLT_MAX__;
 // KVM: 0 = the paper's square problem, 1 = the general kernel over a dense cache, 2 = over a paged cache
 // (an instantiation of its own: the per-tile descriptors cost scalar registers in the loop, which the
 // latency-bound small decoding shapes of the dense path would pay for too).  3, 4: the same two, each weight multiplied
-// as two 16-bit halves, for the few query rows of a decoding step (pick_halves).
+// as two 16-bit halves, for the few query rows of a decoding step (pick_halves).  5, 6: dense and paged, the queries being a tree of
+// drafted tokens: the last Sp keys are the tokens' own, and which of them a query sees stands in its row of `tree`, tree_words
+// 32-bit words, bit j for key Skv - Sp + j.  Keys before them are seen by all, so that only the last tiles take the masked path; there a
+// lane shifts the bits of a block of 32 keys out of two words of its row.
 // TILE: rows T_N of a K/V tile, plus 1000 * (NS - 1).  NS > 1: NS streams of NW wavefronts each work on
 // the same query rows; stream s takes the tiles s, s + NS, ... into LDS slots of its own, and the streams' states (o, m,
 // l of Eqs. 2-4) are combined through the LDS at the end, in their order.  For launches of few workgroups: the chain of tiles
@@ -217,10 +249,10 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                 int Skv_arg, int splits_arg, float *__restrict__ ws, int rows_per_head,
                 const int *__restrict__ kv_lens, int heads_per_batch,
                 const int *__restrict__ block_table, int max_blocks, int block_shift, int tile_rot,
-                int batches, Divisor by_batches)
+                int batches, Divisor by_batches, const uint32_t *__restrict__ tree, long long tree_batch, int tree_words)
 {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass only needs the launch stub; the body uses device-only types
-    constexpr bool KV = KVM != 0, PAGED = KVM == 2 || KVM == 4, HALVES = KVM >= 3;
+    constexpr bool KV = KVM != 0, TREE = KVM >= 5, PAGED = KVM == 2 || KVM == 4 || KVM == 6, HALVES = KVM == 3 || KVM == 4;
     constexpr int TN = TILE % 1000, NS = 1 + TILE / 1000;
     using E = Elem<T>;
     using vec8 = typename E::vec8;
@@ -334,7 +366,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     const int reach = pos_hi + koff;
     const int nTw = causal ? ((KV && reach < 0) ? 0 : reach / TN + 1) : nT;
     const int klim = causal ? pos_own + koff : Skv - 1;
-    const int nfull = ((causal ? pos_lo + koff : Skv - 1) + 1) / TN;
+    const int nfull = TREE ? (koff > 0 ? koff : 0) / TN : ((causal ? pos_lo + koff : Skv - 1) + 1) / TN;
     // this workgroup's run of tiles [t0, t1): all nTw of them unless the key range is split
     const int per_split = (nTw + splits - 1) / splits;
     const int t0 = KV ? sp * per_split : 0;
@@ -483,7 +515,46 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // neither the maximum nor the rescale.  tau = 0 raises the reference on every new maximum (any
     // weight above 1 makes the sum exceed 1), which is Eq. 2 literally, at the price of recomputing
     // most tiles.
-    float m_ref = !KV || klim >= t0 * TN ? kNoWeight : -INFINITY;      // (-inf: no key of this run reaches the row)
+    float m_ref = !KV || (TREE ? koff - 1 : klim) >= t0 * TN ? kNoWeight : -INFINITY;      // (-inf: no key of this run reaches the row)
+    // trees: bit (i / 4) * 8 + i % 4 of sees[nb] is for the lane's score i of block nb of the tile (set by tree_words_of, tree_bits_of)
+    uint32_t sees[TREE ? NB : 1], word[TREE ? NB + 1 : 1];
+    const uint32_t *tree_entry = nullptr;
+    uint32_t tree_row = 0;
+    if constexpr (TREE) {
+        tree_entry = tree + (size_t)(head / heads_per_batch) * tree_batch;
+        tree_row = (uint32_t)pos_own * (uint32_t)tree_words;
+    }
+    // the words of the row that hold the tile's bits: all ones before the tree, zeros behind it
+    auto tree_words_of = [&](int row0) __attribute__((always_inline)) {
+        const int first = (row0 - koff) >> 5;
+#pragma unroll
+        for (int i = 0; i <= NB; ++i) {
+            const int at = first + i;
+            word[i] = tree_entry[tree_row + (at < 0 ? 0 : at < tree_words ? at : tree_words - 1)];
+        }
+    };
+    auto tree_bits_of = [&](int row0) __attribute__((always_inline)) {
+        const int first = (row0 - koff) >> 5;
+        uint32_t all = 0;
+#pragma unroll
+        for (int i = 0; i <= NB; ++i) word[i] = first + i < 0 ? ~0u : first + i < tree_words ? word[i] : 0u;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int left = Skv - (row0 + nb * 32);      // keys of the block (bits past the last token's are not looked at)
+            const uint32_t x = __builtin_amdgcn_alignbit(word[nb + 1], word[nb], (row0 - koff) & 31);
+            sees[nb] = left >= 32 ? x : left > 0 ? x & ((1u << left) - 1u) : 0u;
+            all |= sees[nb];
+        }
+        // (a row that no key of the run reached so far; the two lanes of a row have the same bits)
+        if (m_ref == -INFINITY && all != 0) m_ref = kNoWeight;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) sees[nb] >>= g * 4;
+    };
+    // whether the lane's row does not see the key of its score i in block nb
+    auto hidden = [&](int key0, int nb, int i) __attribute__((always_inline)) {
+        if constexpr (TREE) return (sees[nb] & (1u << ((i >> 2) * 8 + (i & 3)))) == 0;
+        else return key0 + nb * 32 + (i >> 2) * 8 + (i & 3) > klim;
+    };
     const float lazy_limit = __builtin_amdgcn_exp2f(tau);
     float l_run = 0.f;         // this lane's share of the normaliser (lane^32 holds the rest)
 
@@ -547,7 +618,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (key0 + nb * 32 + (i >> 2) * 8 + (i & 3) > klim) sacc[nb][i] = -INFINITY;
+                    if (hidden(key0, nb, i)) sacc[nb][i] = -INFINITY;
         }
         float mx = sacc[0][0];
 #pragma unroll
@@ -582,7 +653,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
             for (int i = 0; i < 16; ++i) {
                 float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[nb][i], c, -m_ref));
                 if constexpr (MASK) {
-                    if (key0 + nb * 32 + (i >> 2) * 8 + (i & 3) > klim) p = 0.f;
+                    if (hidden(key0, nb, i)) p = 0.f;
                 }
                 if (nb == 0 && i < 4) psum[i] = p;        // four partial sums: short dependency chains
                 else psum[i & 3] += p;
@@ -593,7 +664,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     };
 
     // Eq. 4: O^T += V^T P^T
-    auto accumulate = [&](int vslot, const vec8 (&pb)[NB][2]) __attribute__((always_inline)) {
+    auto accumulate = [&](int vslot, const vec8 (&pb)[NB][2], auto mask_tag) __attribute__((always_inline)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -605,6 +676,25 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                     i16x4 lo = lds_read_tr16(p0);
                     i16x4 hi = lds_read_tr16(p0 + 8 * G::ROW);
                     i16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    if constexpr (TREE && decltype(mask_tag)::value) {
+                        const u32x4 raw = __builtin_bit_cast(u32x4, a);
+                        if (__builtin_amdgcn_ballot_w64(NotFinite<T>::any(raw)) != 0) {
+                            u32x4 finite, up, down, seen;
+                            NotFinite<T>::take_apart(raw, finite, up, down);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                seen[i] = (hidden(0, nb, ks * 8 + 2 * i) ? 0u : NotFinite<T>::ONE & 0xffffu) |
+                                          (hidden(0, nb, ks * 8 + 2 * i + 1) ? 0u : NotFinite<T>::ONE & 0xffff0000u);
+                            f32x16 zero;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+                            const f32x16 ups = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), zero);
+                            const f32x16 downs = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), zero);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) oacc[db][i] += NotFinite<T>::excess(ups[i], downs[i]);
+                            a = __builtin_bit_cast(i16x8, finite);
+                        }
+                    }
                     oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), pb[nb][ks], oacc[db]);
                     if constexpr (HALVES) oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), ph[nb][ks], oacc[db]);
                 }
@@ -642,7 +732,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // keep hitting the same memory channels.  The order of the unmasked tiles is free (Eqs. 2-4 do not
     // care), so each workgroup starts its sweep at a tile of its own and wraps around.
     int rot = 0;
-    if constexpr (KVM == 1 && NS == 1) {
+    if constexpr ((KVM == 1 || KVM == 5) && NS == 1) {
         const int nf = fast_end - t0;
         if (tile_rot != 0 && nf > 2) rot = (int)((((unsigned)hs * 2654435761u) >> 12) % (unsigned)nf);
     }
@@ -702,6 +792,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
             // (halves strictly one after the other: the scheduler would otherwise start the scores of the
             // second beside the softmax of the first and hold both sets of score accumulators)
             if (sub > 0) __builtin_amdgcn_sched_barrier(0);
+            if constexpr (TREE && decltype(mask_tag)::value) tree_words_of(j * TN + sub * TNS);
             __builtin_amdgcn_s_setprio(1);
             scores((PAR ? KSLOT1 : KSLOT0) + sub * TNS * G::ROW, sacc, [&](int kk) __attribute__((always_inline)) {
                 if constexpr (SPREAD) {
@@ -714,16 +805,17 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                 }
             });
             __builtin_amdgcn_s_setprio(0);
+            if constexpr (TREE && decltype(mask_tag)::value) tree_bits_of(j * TN + sub * TNS);
             softmax_tile(j * TN + sub * TNS, mask_tag);
             __builtin_amdgcn_s_setprio(2);
-            accumulate((PAR ? VSLOT1 : VSLOT0) + sub * TNS * G::ROW, pb);
+            accumulate((PAR ? VSLOT1 : VSLOT0) + sub * TNS * G::ROW, pb, mask_tag);
             __builtin_amdgcn_s_setprio(0);
         }
         TSDPA_WAIT_VMCNT0();
         if constexpr (NW > 1) __syncthreads();
     };
     int j = s0;
-    if constexpr (KVM == 1 && NS == 1) {
+    if constexpr ((KVM == 1 || KVM == 5) && NS == 1) {
         // unmasked tiles in rotated order: t0+rot ... fast_end-1, t0 ... t0+rot-1, then on to fast_end
         int cur = t0 + rot;
         for (; j < fast_end; j += 2) {

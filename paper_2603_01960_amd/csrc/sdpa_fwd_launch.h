@@ -29,6 +29,11 @@ struct LaunchArgs {
     unsigned long long ticket; // decoding kernel, splits > 1: a number of this call alone (never 0) if it combines the runs itself, else 0
     int streams;       // kv = 0: streams of K/V tiles per workgroup (0 or 1: the plain form)
     int rows_per_head; // kv = 1: query positions per query head; S / rows_per_head query heads are folded into the S rows
+    // kv = 1: NULL, or which of the last rows_per_head keys each query sees (trees of drafted tokens): tree_words 32-bit words per query
+    // position, tree_batch of them from one batch entry's to the next (0: one tree for all)
+    const uint32_t *tree;
+    long long tree_batch;
+    int tree_words;
     hipStream_t stream;
 };
 
@@ -132,6 +137,19 @@ int launch_bf16_d160(int tile_m, int tile_n, const LaunchArgs &a);
 // Decoding steps (a.S <= 32 query rows per key/value head; sdpa_decode_kernel.h).
 int launch_decode_f16(int D, const LaunchArgs &a);
 int launch_decode_bf16(int D, const LaunchArgs &a);
+
+// Trees of drafted tokens (a.tree): the forward kernel's streams or its plain form on 64 or 128 rows (sdpa_tree_inst.h), and the
+// decoding kernel's.
+int launch_tree_f16_d64(int tile_m, const LaunchArgs &a);
+int launch_tree_f16_d96(int tile_m, const LaunchArgs &a);
+int launch_tree_f16_d128(int tile_m, const LaunchArgs &a);
+int launch_tree_f16_d160(int tile_m, const LaunchArgs &a);
+int launch_tree_bf16_d64(int tile_m, const LaunchArgs &a);
+int launch_tree_bf16_d96(int tile_m, const LaunchArgs &a);
+int launch_tree_bf16_d128(int tile_m, const LaunchArgs &a);
+int launch_tree_bf16_d160(int tile_m, const LaunchArgs &a);
+int launch_tree_decode_f16(int D, const LaunchArgs &a);
+int launch_tree_decode_bf16(int D, const LaunchArgs &a);
 
 // Backward pass: dQ (queries resident) and dK + dV (keys resident) in one grid after the row statistics, or one after the other with
 // the statistics on the way, or whole heads in one launch (sdpa_bwd_pick.h).

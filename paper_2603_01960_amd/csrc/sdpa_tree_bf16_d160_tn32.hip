@@ -1,0 +1,6 @@
+// Trees of drafted tokens: element type bf16, head dim 160, plain form (32-row K/V tiles).
+#include "sdpa_tree_inst.h"
+
+namespace tsdpa {
+int launch_tree_bf16_d160_tn32(int tile_m, const LaunchArgs &a) { return launch_tree_plain<__bf16, 160>(tile_m, a); }
+}  // namespace tsdpa

@@ -355,11 +355,26 @@ void pick_tile_kv(long long heads, int Sq, int Skv, int D, int *tm, int *tn)
 
 }  // namespace
 
+// Which keys the queries of a tree of drafted tokens see (mask of tiled_sdpa_fwd_tree); NULL: no tree.
+struct Tree { const long long *mask = nullptr; long long batch = 0; };
+
 static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, float *lse, const int *kv_lens,
                        const int *block_table, int max_blocks, int block_shift,
                        int B, int H, int Hkv, int Sq, int Skv, int D, float scale, int dtype, void *stream,
                        int tile_m, int tile_n, unsigned flags,
-                       int splits, void *workspace, unsigned long long workspace_bytes);
+                       int splits, void *workspace, unsigned long long workspace_bytes, const Tree &tree = {});
+
+// Pages of 64 << n rows, so that a K/V tile of 32 or 64 rows never straddles two pages: n, and the capacity of max_blocks of
+// them; false if these are no such pages.
+static bool paged_capacity(int max_blocks, int block_rows, int *shift, int *cap)
+{
+    *shift = 6;
+    while (*shift < 20 && (1 << *shift) != block_rows) ++*shift;
+    if (max_blocks < 0 || (1 << *shift) != block_rows) return false;
+    if ((int64_t)max_blocks * block_rows > (int64_t)std::numeric_limits<int>::max()) return false;
+    *cap = max_blocks * block_rows;
+    return true;
+}
 
 // Combines the states of a call's splits (a.BH heads of a.S rows).  Each kernel in the form that loads no more than the splits
 // need: see its header.
@@ -402,6 +417,8 @@ const char *tiled_sdpa_status_string(int status)
         case TSDPA_ERR_STATIC_SCRATCH:
             return "split states exceed the library's static scratch buffer (or its address is unavailable): "
                    "use tiled_sdpa_fwd_kvcache with a workspace of the caller's, or fewer splits";
+        case TSDPA_ERR_BAD_EPS: return "bad eps: must be finite and not negative";
+        case TSDPA_ERR_BAD_STRIDE: return "bad stride: rows need strides that are multiples of 8 elements, and must not overlap where they are written";
         default: return "unknown status";
     }
 }
@@ -610,18 +627,51 @@ int tiled_sdpa_fwd_paged(const void *q, const void *k_pages, const void *v_pages
                          float scale, int dtype, void *stream, int tile_m, int tile_n, unsigned flags,
                          int splits, void *workspace, unsigned long long workspace_bytes)
 {
-    // pages of 64 << n rows, so that a K/V tile of 32 or 64 rows never straddles two pages
-    int shift = 6;
-    while (shift < 20 && (1 << shift) != block_rows) ++shift;
-    if (max_blocks < 0 || (1 << shift) != block_rows) return TSDPA_ERR_BAD_SHAPE;
-    if ((int64_t)max_blocks * block_rows > (int64_t)std::numeric_limits<int>::max()) return TSDPA_ERR_BAD_SHAPE;
-    const int cap = max_blocks * block_rows;
+    int shift, cap;
+    if (!paged_capacity(max_blocks, block_rows, &shift, &cap)) return TSDPA_ERR_BAD_SHAPE;
     const int st = validate_shape_kv(B, H, Sq, cap, D, dtype, flags);
     if (st != TSDPA_OK) return st;
     if ((int64_t)B * H * Sq != 0 && (!kv_lens || !block_table)) return TSDPA_ERR_NULL_PTR;
     if (((uintptr_t)block_table & 3u) != 0) return TSDPA_ERR_MISALIGNED;
     return fwd_kv_impl(q, k_pages, v_pages, o, lse, kv_lens, block_table, max_blocks, shift, B, H, Hkv, Sq, cap, D,
                        scale, dtype, stream, tile_m, tile_n, flags, splits, workspace, workspace_bytes);
+}
+
+// The checks that the mask of a tree adds, behind those of the shape: the bits of one entry's tree are addressed in 32 bits.
+static int check_tree(int B, int H, int T, const long long *mask, long long mask_batch)
+{
+    const int64_t words = ((int64_t)T + 63) / 64;
+    if (T > 65536 || (mask_batch != 0 && mask_batch < T * words)) return TSDPA_ERR_BAD_SHAPE;
+    if ((int64_t)B * H * T == 0) return TSDPA_OK;
+    if (!mask) return TSDPA_ERR_NULL_PTR;
+    return ((uintptr_t)mask & 7u) != 0 ? TSDPA_ERR_MISALIGNED : TSDPA_OK;
+}
+
+int tiled_sdpa_fwd_tree(const void *q, const void *k, const void *v, void *o, float *lse, const int *kv_lens,
+                        const long long *mask, long long mask_batch, int B, int H, int Hkv, int T, int Skv, int D,
+                        float scale, int dtype, void *stream, int splits, void *workspace, unsigned long long workspace_bytes)
+{
+    int st = validate_shape_kv(B, H, T, Skv, D, dtype, 0);
+    if (st == TSDPA_OK) st = check_tree(B, H, T, mask, mask_batch);
+    if (st != TSDPA_OK) return st;
+    return fwd_kv_impl(q, k, v, o, lse, kv_lens, nullptr, 0, 0, B, H, Hkv, T, Skv, D, scale, dtype, stream, 0, 0, 0, splits, workspace,
+                       workspace_bytes, Tree{mask, mask_batch});
+}
+
+int tiled_sdpa_fwd_tree_paged(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,
+                              const int *kv_lens, const int *block_table, const long long *mask, long long mask_batch,
+                              int B, int H, int Hkv, int T, int max_blocks, int block_rows, int D,
+                              float scale, int dtype, void *stream, int splits, void *workspace, unsigned long long workspace_bytes)
+{
+    int shift, cap;
+    if (!paged_capacity(max_blocks, block_rows, &shift, &cap)) return TSDPA_ERR_BAD_SHAPE;
+    int st = validate_shape_kv(B, H, T, cap, D, dtype, 0);
+    if (st == TSDPA_OK) st = check_tree(B, H, T, mask, mask_batch);
+    if (st != TSDPA_OK) return st;
+    if ((int64_t)B * H * T != 0 && (!kv_lens || !block_table)) return TSDPA_ERR_NULL_PTR;
+    if (((uintptr_t)block_table & 3u) != 0) return TSDPA_ERR_MISALIGNED;
+    return fwd_kv_impl(q, k_pages, v_pages, o, lse, kv_lens, block_table, max_blocks, shift, B, H, Hkv, T, cap, D, scale, dtype, stream,
+                       0, 0, 0, splits, workspace, workspace_bytes, Tree{mask, mask_batch});
 }
 
 }  // extern "C"
@@ -632,7 +682,7 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
                        const int *block_table, int max_blocks, int block_shift,
                        int B, int H, int Hkv, int Sq, int Skv, int D, float scale, int dtype, void *stream,
                        int tile_m, int tile_n, unsigned flags,
-                       int splits, void *workspace, unsigned long long workspace_bytes)
+                       int splits, void *workspace, unsigned long long workspace_bytes, const Tree &tree)
 {
     int st = validate_shape_kv(B, H, Sq, Skv, D, dtype, flags);
     if (st != TSDPA_OK) return st;
@@ -675,7 +725,7 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
     // 54.9 / 33.3, 4096 keys 188 / 113; 13 of 4900, D = 96, 4096 keys 159 / 93; 52 of 1100, D = 160, 4096 keys 253 / 154; one
     // round of either, 16 of 3900, D = 128, 4096 keys 111.9 / 113.1).
     const int64_t wide = (int64_t)B * Hkv * ((rows + 255) / 256);
-    if (heuristic_tile && splits == 1 && block_table == nullptr && kv_lens == nullptr &&
+    if (heuristic_tile && splits == 1 && block_table == nullptr && kv_lens == nullptr && !tree.mask &&
         !(flags & TSDPA_FLAG_CAUSAL) && D >= 96 && rows >= (D == 160 ? 1024 : D == 96 ? 4096 : 2048) &&
         (wide == 256 || (wide > 256 && (int64_t)B * Hkv * ((rows + 127) / 128) >= 512))) {
         tile_m = 256;
@@ -712,6 +762,9 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
     a.Skv = Skv;
     a.splits = splits;
     a.ws = (float *)workspace;
+    a.tree = (const uint32_t *)tree.mask;
+    a.tree_batch = 2 * tree.batch;
+    a.tree_words = 2 * ((Sq + 63) / 64);
     a.stream = (hipStream_t)stream;
 
     int err;
@@ -724,7 +777,7 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
         }
     }
     const bool decode = heuristic_tile && rows <= kDecodeRows && a.streams <= 1;
-    a.halves = (decode || a.streams > 1) && pick_halves(a.BH, rows, Skv, D, splits, a.streams) ? 1 : 0;
+    a.halves = !tree.mask && (decode || a.streams > 1) && pick_halves(a.BH, rows, Skv, D, splits, a.streams) ? 1 : 0;
     // The decoding kernel combines the runs itself while they are few: a mark (8 bytes) per run must fit a head's part of o,
     // and past 32 states per head, eight rows, or four columns for each thread, the one workgroup that does it is slower than the
     // merge kernel's many (time with the marks / with two kernels, over 300 shapes: one row 0.95 at 2 runs, 0.97 at 8, 1.04 at 20;
@@ -733,7 +786,23 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
     if (decode && splits > 1 && rows <= 8 && splits * rows <= 32 && splits <= rows * D / 4 &&
         rows * D <= 256 * tsdpa::decode_waves(a.BH, splits, Skv))
         a.ticket = call_ticket();
-    if (decode) {
+    if (tree.mask && decode) {
+        err = dtype == TSDPA_F16 ? tsdpa::launch_tree_decode_f16(D, a) : tsdpa::launch_tree_decode_bf16(D, a);
+    } else if (tree.mask && dtype == TSDPA_F16) {
+        switch (D) {
+            case 64: err = tsdpa::launch_tree_f16_d64(tile_m, a); break;
+            case 96: err = tsdpa::launch_tree_f16_d96(tile_m, a); break;
+            case 128: err = tsdpa::launch_tree_f16_d128(tile_m, a); break;
+            default: err = tsdpa::launch_tree_f16_d160(tile_m, a); break;
+        }
+    } else if (tree.mask) {
+        switch (D) {
+            case 64: err = tsdpa::launch_tree_bf16_d64(tile_m, a); break;
+            case 96: err = tsdpa::launch_tree_bf16_d96(tile_m, a); break;
+            case 128: err = tsdpa::launch_tree_bf16_d128(tile_m, a); break;
+            default: err = tsdpa::launch_tree_bf16_d160(tile_m, a); break;
+        }
+    } else if (decode) {
         err = dtype == TSDPA_F16 ? tsdpa::launch_decode_f16(D, a) : tsdpa::launch_decode_bf16(D, a);
     } else if (dtype == TSDPA_F16) {
         switch (D) {

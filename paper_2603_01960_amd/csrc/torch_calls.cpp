@@ -1,5 +1,5 @@
-// The tensor entry points of the Python package (sdpa, sdpa_kv, sdpa_paged, sdpa_backward) in native code: argument
-// checks, output and workspace tensors from torch's allocator, the current stream, and one call into the C-ABI of
+// The tensor entry points of the Python package (sdpa, sdpa_kv, sdpa_paged, sdpa_backward, sdpa_tree, sdpa_tree_paged, and those around
+// attention: tree_mask, cache_step, qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward) in native code: argument checks, output and workspace tensors from torch's allocator, the current stream, and one call into the C-ABI of
 // include/tiled_sdpa.h.
 //
 // Why native: a short call is bound by the host.  One forward call of a small problem (B=1 H=2 S=128 D=64, a kernel of
@@ -480,11 +480,390 @@ PyObject *call_sdpa_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// An int32 tensor on the device of `like`, contiguous, of the given shape.
+const int *int_data(PyObject *obj, at::IntArrayRef shape, const at::Device &device, const char *complaint)
+{
+    if (!THPVariable_Check(obj)) fail(complaint);
+    const at::Tensor &t = THPVariable_Unpack(obj);
+    if (t.scalar_type() != at::kInt || t.device() != device || t.sizes() != shape || !t.is_contiguous()) fail(complaint);
+    return (const int *)data(t);
+}
+
+// The mask of a tree: int64 [T, W] for all entries, or [B, T, W].
+struct TreeMask { const long long *data; long long batch; };
+TreeMask tree_mask_of(PyObject *obj, int64_t B, int64_t T, const at::Tensor &q)
+{
+    static const char text[] = "mask must be a contiguous int64 tensor [T, ceil(T / 64)] or [B, T, ceil(T / 64)] on the device of q";
+    if (!THPVariable_Check(obj)) fail(text);
+    const at::Tensor &m = THPVariable_Unpack(obj);
+    const int64_t W = (T + 63) / 64;
+    if (m.scalar_type() != at::kLong || m.device() != q.device() || !m.is_contiguous() || (m.dim() != 2 && m.dim() != 3)) fail(text);
+    const at::IntArrayRef s = m.sizes();
+    if (s[s.size() - 2] != T || s[s.size() - 1] != W || (m.dim() == 3 && s[0] != B)) fail(text);
+    return TreeMask{(const long long *)data(m), m.dim() == 3 ? (long long)(T * W) : 0};
+}
+
+// sdpa_tree(q, k, v, kv_lens, block_table, mask, scale, splits, return_lse, out, workspace): dense (block_table None, kv_lens may be) or paged
+PyObject *call_sdpa_tree(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 11);
+        const at::Tensor &q = heads_tensor(args[0], "q"), &k = heads_tensor(args[1], "k"), &v = heads_tensor(args[2], "v");
+        const bool paged = args[4] != Py_None;
+        const float scale = as_scale(args[6]);
+        int splits = args[7] == Py_None ? 0 : as_int(args[7]);
+        const bool with_lse = as_bool(args[8]);
+        same_type(q, k, v);
+        const at::IntArrayRef s = q.sizes(), t = k.sizes();
+        if (!same_sizes(k, v) || s[3] != t[3] || (!paged && s[0] != t[0]))
+            fail(paged ? "k_pages, v_pages must be [P, Hkv, block_rows, D]" : "q must be [B, H, T, D] and k, v [B, Hkv, Skv, D]");
+        if (t[1] == 0 || s[1] % t[1] != 0) fail("the number of query heads must be a multiple of the number of key/value heads");
+        if (k.device() != q.device() || v.device() != q.device()) fail("q, k, v must be on one device");
+        const int *lens = nullptr, *table = nullptr;
+        if (paged || args[3] != Py_None) lens = int_data(args[3], s.slice(0, 1), q.device(), "kv_lens must be a contiguous int32 tensor [B] on the device of q");
+        const int B = (int)s[0], H = (int)s[1], T = (int)s[2], D = (int)s[3], Hkv = (int)t[1], dtype = element_type(q);
+        int max_blocks = 0;
+        int64_t cap = t[2];
+        if (paged) {
+            static const char text[] = "block_table must be a contiguous int32 tensor [B, max_blocks] on the device of q";
+            if (!THPVariable_Check(args[4])) fail(text);
+            const at::Tensor &x = THPVariable_Unpack(args[4]);
+            if (x.dim() != 2) fail(text);
+            table = int_data(args[4], {s[0], x.size(1)}, q.device(), text);
+            if (x.size(1) > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+            max_blocks = (int)x.size(1);
+            cap = (int64_t)max_blocks * t[2];
+        }
+        if (cap > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        const TreeMask mask = tree_mask_of(args[5], s[0], s[2], q);
+        at::Tensor out = output(args[9], q, "out must match q in shape, dtype, device and be contiguous"), lse;
+        if (with_lse) lse = empty(s.slice(0, 3), at::kFloat, q);
+        const bool heuristic = splits == 0;
+        if (heuristic) {
+            const int st = heuristic_splits(B, H, Hkv, T, cap > 1 || !paged ? (int)cap : 1, D, dtype, 0, false, Tile{}, &splits);
+            if (st != TSDPA_OK) return PyLong_FromLong(st);
+        }
+        const Workspace ws(args[10], tiled_sdpa_kv_workspace_bytes(B, H, T, D, splits), q);
+        if (heuristic && args[10] != Py_None) splits = 0;
+        const Launch on(q);
+        float *const lse_data = with_lse ? (float *)data(lse) : nullptr;
+        const int st = paged ? without_gil(tiled_sdpa_fwd_tree_paged, data(q), data(k), data(v), data(out), lse_data, lens, table, mask.data, mask.batch,
+                                           B, H, Hkv, T, max_blocks, (int)t[2], D, scale, dtype, on.stream, splits, ws.ptr, ws.bytes)
+                             : without_gil(tiled_sdpa_fwd_tree, data(q), data(k), data(v), data(out), lse_data, lens, mask.data, mask.batch,
+                                           B, H, Hkv, T, (int)cap, D, scale, dtype, on.stream, splits, ws.ptr, ws.bytes);
+        return result(st, args[9], out, with_lse, Py_None, lse);
+    });
+}
+
+// A tuple of the tensors given, or the status code.
+PyObject *tuple_of(int status, std::initializer_list<const at::Tensor *> tensors)
+{
+    if (status != TSDPA_OK) return PyLong_FromLong(status);
+    PyObject *all = PyTuple_New((Py_ssize_t)tensors.size());
+    if (!all) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor *t : tensors) {
+        PyObject *obj;
+        if (t->defined()) {
+            obj = THPVariable_Wrap(*t);
+        } else {
+            Py_INCREF(Py_None);
+            obj = Py_None;
+        }
+        if (!obj) {
+            Py_DECREF(all);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(all, i++, obj);
+    }
+    return all;
+}
+
+// The objects of a caller's tuple of `count`, given to `take` one after another (which keeps what it needs of them: a sequence made for
+// the call ends here).
+template <typename F> void each_of(PyObject *obj, Py_ssize_t count, const char *complaint, F &&take)
+{
+    PyObject *seq = PySequence_Fast(obj, complaint);
+    if (!seq) throw PyFail{};
+    try {
+        if (PySequence_Fast_GET_SIZE(seq) != count) fail(complaint);
+        for (Py_ssize_t i = 0; i < count; ++i) take(i, PySequence_Fast_GET_ITEM(seq, i));
+    } catch (...) {
+        Py_DECREF(seq);
+        throw;
+    }
+    Py_DECREF(seq);
+}
+
+// The tensors of a caller's tuple, or undefined ones.
+template <int N> struct Given {
+    at::Tensor t[N];
+    Given(PyObject *obj, const char *complaint)
+    {
+        if (obj == Py_None) return;
+        each_of(obj, N, complaint, [&](Py_ssize_t i, PyObject *x) {
+            if (!THPVariable_Check(x)) fail(complaint);
+            t[i] = THPVariable_Unpack(x);
+        });
+    }
+};
+
+// An output of the caller's, or a new tensor.
+at::Tensor made(const at::Tensor &t, at::IntArrayRef shape, at::ScalarType type, const at::Tensor &like, const char *complaint)
+{
+    if (!t.defined()) return empty(shape, type, like);
+    if (t.sizes() != shape || t.scalar_type() != type || !t.is_contiguous() || t.device() != like.device()) fail(complaint);
+    return t;
+}
+
+// tree_mask(parents, out)
+PyObject *call_tree_mask(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 2);
+        const at::Tensor &parents = device_tensor(args[0], "parents");
+        if (parents.scalar_type() != at::kInt || !parents.is_contiguous() || (parents.dim() != 1 && parents.dim() != 2))
+            fail("parents must be contiguous int32 [T] or [B, T]");
+        const at::IntArrayRef s = parents.sizes();
+        const int64_t T = s[s.size() - 1], B = s.size() == 2 ? s[0] : 1;
+        if (T > std::numeric_limits<int>::max() || B > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        const int64_t words[3] = {B, T, (T + 63) / 64};
+        const at::IntArrayRef shape(s.size() == 2 ? words : words + 1, s.size() + 1);
+        static const char text[] = "out must be (mask, depths): contiguous int64 [..., T, ceil(T / 64)] and int32 [..., T] on the device of parents";
+        const Given<2> given(args[1], text);
+        const at::Tensor mask = made(given.t[0], shape, at::kLong, parents, text), depths = made(given.t[1], s, at::kInt, parents, text);
+        const Launch on(parents);
+        const int st = without_gil(tiled_sdpa_tree_mask, (const int *)data(parents), (long long *)data(mask), (int *)data(depths), (int)B, (int)T, on.stream);
+        return tuple_of(st, {&mask, &depths});
+    });
+}
+
+// cache_step(kv_lens, counts, S, block_rows, pages, depths, out)
+PyObject *call_cache_step(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 7);
+        const at::Tensor &lens = device_tensor(args[0], "kv_lens");
+        if (lens.scalar_type() != at::kInt || lens.dim() != 1 || !lens.is_contiguous()) fail("kv_lens must be contiguous int32 [B]");
+        const at::Device device = lens.device();
+        const int *counts = int_data(args[1], lens.sizes(), device, "counts must be contiguous int32 [B] on the device of kv_lens");
+        const int S = as_int(args[2]), block_rows = as_int(args[3]);
+        if (S < 0) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        const int64_t B = lens.size(0);
+        int *table = nullptr, *free_pages = nullptr;
+        const int *pool = nullptr;
+        int64_t max_blocks = 0, pool_size = 0;
+        if (args[4] != Py_None) {
+            static const char text[] = "pages must be (block_table, free_pages, pool): contiguous int32 [B, max_blocks], [pool_size] and [2] on the device of kv_lens";
+            each_of(args[4], 3, text, [&](Py_ssize_t i, PyObject *x) {
+                if (!THPVariable_Check(x)) fail(text);
+                const at::Tensor &t = THPVariable_Unpack(x);
+                if (t.scalar_type() != at::kInt || t.device() != device || !t.is_contiguous() || t.dim() != (i == 0 ? 2 : 1)) fail(text);
+                if (i == 0) {
+                    if (t.size(0) != B) fail(text);
+                    max_blocks = t.size(1);
+                    table = (int *)data(t);
+                } else if (i == 1) {
+                    pool_size = t.size(0);
+                    free_pages = (int *)data(t);
+                } else {
+                    if (t.size(0) != 2) fail(text);
+                    pool = (const int *)data(t);
+                }
+            });
+            const int64_t most = std::numeric_limits<int>::max();
+            if (max_blocks > most || pool_size > most) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+            // (an empty tensor has no address: any that is not looked at says that there is a table)
+            if (!table) table = (int *)pool;
+            if (!free_pages) free_pages = (int *)pool;
+        }
+        const int *depths = nullptr;
+        if (args[5] != Py_None) depths = int_data(args[5], {B, S}, device, "depths must be contiguous int32 [B, S] on the device of kv_lens");
+        static const char text[] = "out must be (new_lens, slots, positions, new_pool): contiguous int32 [B], [B, S], [B, S] and [2] on the device of kv_lens";
+        const Given<4> given(args[6], text);
+        const at::Tensor new_lens = made(given.t[0], lens.sizes(), at::kInt, lens, text), slots = made(given.t[1], {B, S}, at::kInt, lens, text),
+                         positions = made(given.t[2], {B, S}, at::kInt, lens, text), new_pool = made(given.t[3], {2}, at::kInt, lens, text);
+        if ((B > 0 && data(new_lens) == data(lens)) || data(new_pool) == (const void *)pool) fail("new_lens and new_pool must be other tensors than kv_lens and pool");
+        if (B > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        const Launch on(lens);
+        const int st = without_gil(tiled_sdpa_cache_step, (const int *)data(lens), counts, depths, table, free_pages, pool, (int *)data(new_lens), (int *)data(slots),
+                                   (int *)data(positions), (int *)data(new_pool), (int)B, S, (int)max_blocks, block_rows, (int)pool_size, on.stream);
+        return tuple_of(st, {&new_lens, &slots, &positions, &new_pool});
+    });
+}
+
+// ---- norm and rotation of queries and keys
+
+const at::Tensor &rows_tensor(PyObject *obj, const char *name)
+{
+    const at::Tensor &t = device_tensor(obj, name);
+    if (t.dim() != 4 || (t.size(3) > 1 && t.stride(3) != 1)) fail_named(name, "must be [B, S, heads, D] with adjacent values in a row");
+    return t;
+}
+
+tsdpa_rows rows_of(const at::Tensor &t) { return tsdpa_rows{data(t), (long long)t.stride(0), (long long)t.stride(1), (long long)t.stride(2)}; }
+
+// What the three calls have in common: q, k, the weights, positions and frequencies, from the arguments that begin at args[0] (q, k,
+// q_weight, k_weight, positions, inv_freq, axes, eps, interleaved).
+struct Rope {
+    tsdpa_rope p{};
+    at::Tensor q, k;
+    at::Tensor weight[2];
+    explicit Rope(PyObject *const *args)
+    {
+        q = rows_tensor(args[0], "q");
+        k = rows_tensor(args[1], "k");
+        p.dtype = element_type(q);
+        const at::IntArrayRef s = q.sizes(), t = k.sizes();
+        if (k.scalar_type() != q.scalar_type() || k.device() != q.device() || t[0] != s[0] || t[1] != s[1] || t[3] != s[3])
+            fail("q and k must be [B, S, H, D] and [B, S, Hkv, D] of one dtype and device");
+        for (int i = 0; i < 4; ++i)
+            if (s[i] > std::numeric_limits<int>::max() || t[i] > std::numeric_limits<int>::max()) fail("q and k are too large");
+        p.B = (int)s[0];
+        p.S = (int)s[1];
+        p.H = (int)s[2];
+        p.Hkv = (int)t[2];
+        p.D = (int)s[3];
+        p.weight_dtype = p.dtype;
+        for (int i = 0; i < 2; ++i) {
+            static const char text[] = "q_weight and k_weight must be contiguous [D] in float32 or the dtype of q, both the same, on the device of q (or None)";
+            if (args[2 + i] == Py_None) continue;
+            if (!THPVariable_Check(args[2 + i])) fail(text);
+            const at::Tensor &w = THPVariable_Unpack(args[2 + i]);
+            if (w.dim() != 1 || w.size(0) != s[3] || !w.is_contiguous() || w.device() != q.device() ||
+                (w.scalar_type() != at::kFloat && w.scalar_type() != q.scalar_type()) ||
+                (i == 1 && weight[0].defined() && w.scalar_type() != weight[0].scalar_type()))
+                fail(text);
+            weight[i] = w;
+            if (w.scalar_type() == at::kFloat) p.weight_dtype = TSDPA_F32;
+        }
+        if (weight[0].defined()) p.q_weight = data(weight[0]);
+        if (weight[1].defined()) p.k_weight = data(weight[1]);
+        if (!THPVariable_Check(args[5])) fail("inv_freq must be contiguous float32 [rot / 2] on the device of q");
+        const at::Tensor &f = THPVariable_Unpack(args[5]);
+        if (f.scalar_type() != at::kFloat || f.dim() != 1 || !f.is_contiguous() || f.device() != q.device() || f.size(0) > s[3])
+            fail("inv_freq must be contiguous float32 [rot / 2] on the device of q");
+        p.rot = 2 * (int)f.size(0);
+        p.inv_freq = (const float *)data(f);
+        const bool several = args[6] != Py_None;
+        {
+            static const char text[] = "positions must be contiguous int32 [S] or [B, S] on the device of q, with axes [A, S] or [A, B, S]";
+            if (!THPVariable_Check(args[4])) fail(text);
+            const at::Tensor &x = THPVariable_Unpack(args[4]);
+            const int64_t lead = several ? 1 : 0, dims = x.dim() - lead;
+            if (x.scalar_type() != at::kInt || !x.is_contiguous() || x.device() != q.device() || (dims != 1 && dims != 2) ||
+                x.size(x.dim() - 1) != s[1] || (dims == 2 && x.size(lead) != s[0]))
+                fail(text);
+            if (several && (x.size(0) < 1 || x.size(0) > std::numeric_limits<int>::max())) fail(text);
+            p.positions = (const int *)data(x);
+            p.pos_batch = dims == 2 ? (long long)s[1] : 0;
+            p.pos_axis = dims == 2 ? (long long)(s[0] * s[1]) : (long long)s[1];
+            p.n_axes = several ? (int)x.size(0) : 1;
+        }
+        if (several) p.axes = int_data(args[6], f.sizes(), q.device(), "axes must be contiguous int32 [rot / 2] on the device of q");
+        const double eps = PyFloat_AsDouble(args[7]);
+        if (eps == -1.0 && PyErr_Occurred()) throw PyFail{};
+        p.eps = (float)eps;
+        p.flags = as_bool(args[8]) ? (unsigned)TSDPA_FLAG_INTERLEAVED : 0u;
+    }
+    // [B, heads, S, D], as attention reads them
+    at::Tensor heads_out(const at::Tensor &given, const at::Tensor &x, const char *complaint) const
+    {
+        return made(given, {x.size(0), x.size(2), x.size(1), x.size(3)}, q.scalar_type(), q, complaint);
+    }
+};
+
+// qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, out)
+PyObject *call_qk_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 10);
+        const Rope r(args);
+        static const char text[] = "out must be (q_out, k_out): contiguous [B, H, S, D] and [B, Hkv, S, D] like q and k";
+        const Given<2> given(args[9], text);
+        const at::Tensor q_out = r.heads_out(given.t[0], r.q, text), k_out = r.heads_out(given.t[1], r.k, text);
+        const tsdpa_rows q = rows_of(r.q), k = rows_of(r.k);
+        const Launch on(r.q);
+        const int st = without_gil(tiled_sdpa_qk_norm_rope, &r.p, &q, &k, data(q_out), data(k_out), on.stream);
+        return tuple_of(st, {&q_out, &k_out});
+    });
+}
+
+// qk_norm_rope_cache(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, v, k_cache, v_cache, slots, out)
+PyObject *call_qk_norm_rope_cache(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 14);
+        const Rope r(args);
+        const at::Tensor &v = rows_tensor(args[9], "v"), &kc = heads_tensor(args[10], "k_cache"), &vc = heads_tensor(args[11], "v_cache");
+        if (!same_sizes(v, r.k) || v.scalar_type() != r.k.scalar_type() || v.device() != r.k.device()) fail("v must match k in shape, dtype and device");
+        const at::IntArrayRef c = kc.sizes();
+        if (!same_sizes(kc, vc) || kc.scalar_type() != r.q.scalar_type() || vc.scalar_type() != r.q.scalar_type() || kc.device() != r.q.device() ||
+            vc.device() != r.q.device() || c[1] != r.p.Hkv || c[3] != r.p.D)
+            fail("k_cache, v_cache must be [pages, Hkv, block_rows, D] of the dtype and device of q");
+        if (c[0] > std::numeric_limits<int>::max() || c[2] > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        const int *slots = int_data(args[12], r.q.sizes().slice(0, 2), r.q.device(), "slots must be contiguous int32 [B, S] on the device of q");
+        static const char text[] = "out must be contiguous [B, H, S, D] like q";
+        if (args[13] != Py_None && !THPVariable_Check(args[13])) fail(text);
+        const at::Tensor q_out = r.heads_out(args[13] == Py_None ? at::Tensor() : THPVariable_Unpack(args[13]), r.q, text);
+        const tsdpa_rows q = rows_of(r.q), k = rows_of(r.k), vr = rows_of(v);
+        const Launch on(r.q);
+        const int st = without_gil(tiled_sdpa_qk_norm_rope_cache, &r.p, &q, &k, &vr, slots, data(q_out), data(kc), data(vc), (int)c[0], (int)c[2], on.stream);
+        if (st != TSDPA_OK) return PyLong_FromLong(st);
+        return give(args[13], q_out);
+    });
+}
+
+// qk_norm_rope_backward(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, dq_out, dk_out, workspace, grads)
+PyObject *call_qk_norm_rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 13);
+        const Rope r(args);
+        const at::Tensor &dq_out = heads_tensor(args[9], "dq_out"), &dk_out = heads_tensor(args[10], "dk_out");
+        auto agree = [&](const at::Tensor &g, const at::Tensor &x) {
+            const int64_t shape[4] = {x.size(0), x.size(2), x.size(1), x.size(3)};
+            if (g.sizes() != at::IntArrayRef(shape, 4) || g.scalar_type() != x.scalar_type() || g.device() != x.device())
+                fail("dq_out and dk_out must be [B, H, S, D] and [B, Hkv, S, D] of the dtype and device of q and k");
+        };
+        agree(dq_out, r.q);
+        agree(dk_out, r.k);
+        at::Tensor dx[2], dw[2];
+        if (args[12] == Py_None) {
+            dx[0] = empty(r.q.sizes(), r.q.scalar_type(), r.q);
+            dx[1] = empty(r.k.sizes(), r.q.scalar_type(), r.q);
+        } else {
+            static const char text[] = "grads must be (dq, dk): [B, S, heads, D] like q and k, with adjacent values in a row";
+            const Given<2> given(args[12], text);
+            for (int i = 0; i < 2; ++i) {
+                const at::Tensor &t = given.t[i], &like = i == 0 ? r.q : r.k;
+                if (!same_sizes(t, like) || t.scalar_type() != like.scalar_type() || t.device() != like.device() || (t.size(3) > 1 && t.stride(3) != 1)) fail(text);
+                dx[i] = t;
+            }
+        }
+        for (int i = 0; i < 2; ++i)
+            if (r.weight[i].defined()) dw[i] = empty(r.weight[i].sizes(), r.weight[i].scalar_type(), r.q);
+        const bool norms = dw[0].defined() || dw[1].defined();
+        const Workspace ws(args[11], norms ? tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(r.p.B, r.p.S, r.p.D) : 0, r.q);
+        const tsdpa_rows q = rows_of(r.q), k = rows_of(r.k), dq = rows_of(dx[0]), dk = rows_of(dx[1]);
+        const Launch on(r.q);
+        const int st = without_gil(tiled_sdpa_qk_norm_rope_bwd, &r.p, (const void *)data(dq_out), (const void *)data(dk_out), &q, &k, &dq, &dk,
+                                   dw[0].defined() ? data(dw[0]) : nullptr, dw[1].defined() ? data(dw[1]) : nullptr, ws.ptr, ws.bytes, on.stream);
+        return tuple_of(st, {&dx[0], &dx[1], &dw[0], &dw[1]});
+    });
+}
+
 PyMethodDef methods[] = {
     {"sdpa", (PyCFunction)(void (*)(void))call_sdpa, METH_FASTCALL, nullptr},
     {"sdpa_kv", (PyCFunction)(void (*)(void))call_sdpa_kv, METH_FASTCALL, nullptr},
     {"sdpa_paged", (PyCFunction)(void (*)(void))call_sdpa_paged, METH_FASTCALL, nullptr},
     {"sdpa_backward", (PyCFunction)(void (*)(void))call_sdpa_backward, METH_FASTCALL, nullptr},
+    {"sdpa_tree", (PyCFunction)(void (*)(void))call_sdpa_tree, METH_FASTCALL, nullptr},
+    {"tree_mask", (PyCFunction)(void (*)(void))call_tree_mask, METH_FASTCALL, nullptr},
+    {"cache_step", (PyCFunction)(void (*)(void))call_cache_step, METH_FASTCALL, nullptr},
+    {"qk_norm_rope", (PyCFunction)(void (*)(void))call_qk_norm_rope, METH_FASTCALL, nullptr},
+    {"qk_norm_rope_cache", (PyCFunction)(void (*)(void))call_qk_norm_rope_cache, METH_FASTCALL, nullptr},
+    {"qk_norm_rope_backward", (PyCFunction)(void (*)(void))call_qk_norm_rope_backward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

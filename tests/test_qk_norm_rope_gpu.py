@@ -1,0 +1,271 @@
+"""Norm and rotation of queries and keys on the GPU against their definition in 64 bits.
+
+Tolerances.  Forward: one rounding to the result's type, U * |y|, and the FP32 arithmetic in front of it.  That is at most: sum of squares and
+root 24 roundings, which reach y as 12 * 2^-24 of it; products with r and w 3; sine and cosine, which the library has to 2^-22 of
+a full turn's amplitude, and the two products and the sum of a pair 3 more: below 2^-19 of the greatest |y| of the row before rotation
+(times sqrt(2) for a pair).  Backward: the same, twice (r and the mean of D <= 160 products in FP32): 2^-17 of the terms' sizes.
+Weights' gradients: a sum of `rows` terms in FP32, of which a register takes rows / 16 and the trees after it 32 steps: (rows + 64) *
+2^-24 of the sum of their sizes, and 2^-18 of it for the terms themselves, and one rounding."""
+import math
+
+import pytest
+import torch
+
+import reference64 as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2603_01960_amd import binding
+    binding.load_library()
+    return binding
+
+
+def case(B, S, H, Hkv, D, dtype, rot=None, axes=0, weights="own", seed=0, far=0, shared=False, packed=True):
+    g = torch.Generator("cuda").manual_seed(seed)
+    rot = D if rot is None else rot
+    if packed:
+        q, k, v = torch.randn(B, S, H + 2 * Hkv, D, device="cuda", generator=g).to(dtype).split([H, Hkv, Hkv], dim=2)
+    else:
+        q, k, v = (torch.randn(B, S, n, D, device="cuda", generator=g).to(dtype) for n in (H, Hkv, Hkv))
+    wd = {"own": dtype, "f32": torch.float32}.get(weights)
+    w = [None if wd is None else (1 + 0.2 * torch.randn(D, device="cuda", generator=g)).to(wd) for _ in range(2)]
+    A = max(1, axes)
+    shape = ([A] if axes else []) + ([] if shared else [B]) + [S]
+    pos = torch.randint(far, far + 5000, shape, device="cuda", generator=g).to(torch.int32)
+    f = (10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64) / max(1, rot // 2))).float().cuda()
+    ax = torch.randint(0, A, (rot // 2,), device="cuda", generator=g).to(torch.int32) if axes else None
+    return q, k, v, w[0], w[1], pos, f, ax
+
+
+def check(got, want, size, rel):
+    want, size = want.cpu(), size.cpu()
+    bound = ref.U[got.dtype] * want.abs() * 1.001 + rel * size + (2.0 ** -25 if got.dtype == torch.float16 else 0.0)
+    err = (got.cpu().double() - want).abs()
+    assert bool((err <= bound).all()), f"error {float((err - bound).max())} past the bound, {float(err.max())}"
+
+
+def check_forward(lib, q, k, qw, kw, pos, f, ax, interleaved, eps, got):
+    phi = ref.angles(pos, f, None if ax is None else ax.tolist(), q.shape[0], q.shape[1])
+    for y, x, w in ((got[0], q, qw), (got[1], k, kw)):
+        size = ref.norm_rope(x, w, phi[..., :0], eps, False).abs().amax(-1, keepdim=True) * math.sqrt(2) if x.numel() else torch.zeros(1)
+        check(y, ref.norm_rope(x, w, phi, eps, interleaved), size, 2.0 ** -19)
+
+
+SHAPES = [(1, 1, 1, 1, 64), (2, 7, 3, 1, 96), (1, 5, 12, 12, 64), (3, 17, 8, 2, 128), (2, 33, 5, 5, 160), (1, 130, 33, 1, 128), (2, 1, 17, 4, 96)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,S,H,Hkv,D", SHAPES)
+def test_forward(lib, B, S, H, Hkv, D, dtype):
+    for i, (rot, axes, weights, interleaved) in enumerate([(D, 0, "own", False), (D, 0, "f32", True), (D // 2 // 16 * 16, 2, "own", True), (16, 3, None, False),
+                                                           (0, 0, "f32", False)]):
+        q, k, _, qw, kw, pos, f, ax = case(B, S, H, Hkv, D, dtype, rot, axes, weights, seed=i, shared=i == 1)
+        got = lib.qk_norm_rope(q, k, qw, kw, pos, f, axes=ax, interleaved=interleaved)
+        assert got[0].shape == (B, H, S, D) and got[1].shape == (B, Hkv, S, D) and got[0].is_contiguous() and got[0].dtype == dtype
+        check_forward(lib, q, k, qw, kw, pos, f, ax, interleaved, 1e-6, got)
+
+
+def test_strides_outputs_and_one_weight(lib):
+    """Heads in front of tokens, entries that share rows, every other token, and the caller's own results."""
+    base = torch.randn(2, 6, 40, 128, device="cuda").to(torch.bfloat16)
+    q, k = base.transpose(1, 2), base[:1, 0:3].transpose(1, 2).expand(2, -1, -1, -1)
+    q, k = q[:, ::2], k[:, ::2]
+    w = (1 + 0.1 * torch.randn(128, device="cuda")).to(torch.bfloat16)
+    pos = torch.arange(20, dtype=torch.int32, device="cuda")
+    f = torch.rand(64, device="cuda")
+    out = torch.full((2, 6, 20, 128), 7.0, device="cuda", dtype=torch.bfloat16), torch.full((2, 3, 20, 128), 7.0, device="cuda", dtype=torch.bfloat16)
+    for qw, kw in ((w, None), (None, w)):
+        got = lib.qk_norm_rope(q, k, qw, kw, pos, f, out=out)
+        assert got[0] is out[0] and got[1] is out[1]
+        check_forward(lib, q, k, qw, kw, pos, f, None, False, 1e-6, got)
+
+
+def test_far_positions_and_negative_ones(lib):
+    """Angles of positions around 2^31: 64 bits of them are needed before a turn's fraction is left."""
+    for far in (2 ** 31 - 5001, -2 ** 31, 10 ** 6):
+        q, k, _, qw, kw, pos, f, ax = case(1, 40, 4, 2, 128, torch.float16, seed=3, far=far)
+        check_forward(lib, q, k, qw, kw, pos, f, ax, False, 1e-6, lib.qk_norm_rope(q, k, qw, kw, pos, f))
+
+
+def test_axes_out_of_range_are_clamped(lib):
+    q, k, _, qw, kw, pos, f, ax = case(2, 9, 2, 1, 64, torch.float16, axes=2)
+    wild, tame = ax.clone(), ax.clone()
+    wild[:3] = torch.tensor([-5, 2, 2 ** 30])
+    tame[:3] = torch.tensor([0, 1, 1])
+    for a, b in zip(lib.qk_norm_rope(q, k, qw, kw, pos, f, axes=wild), lib.qk_norm_rope(q, k, qw, kw, pos, f, axes=tame)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 160])
+def test_rows_of_zeros_infinities_and_nan(lib, D):
+    """A row's values reach no other row; a row of zeros stays one."""
+    q, k, _, qw, kw, pos, f, _ = case(2, 5, 9, 3, D, torch.float16)
+    clean = lib.qk_norm_rope(q, k, qw, kw, pos, f)
+    q2, k2 = q.clone(), k.clone()
+    q2[0, 1, 2] = 0
+    q2[1, 3, 8, D - 1] = math.inf
+    k2[1, 4, 0, 0] = math.nan
+    k2[0, 0, 2] = torch.finfo(torch.float16).min
+    got = lib.qk_norm_rope(q2, k2, qw, kw, pos, f)
+    assert bool((got[0][0, 2, 1] == 0).all()) and bool(torch.isnan(got[0][1, 8, 3]).any()) and bool(torch.isnan(got[1][1, 0, 4]).all())
+    check_forward(lib, q2[:1], k2[:1], qw, kw, pos[:1], f, None, False, 1e-6, [x[:1] for x in got])
+    got[0][0, 2, 1], got[0][1, 8, 3], got[1][1, 0, 4], got[1][0, 2, 0] = clean[0][0, 2, 1], clean[0][1, 8, 3], clean[1][1, 0, 4], clean[1][0, 2, 0]
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+
+
+def test_eps(lib):
+    q, k, _, qw, kw, pos, f, _ = case(1, 8, 4, 2, 64, torch.bfloat16)
+    for eps in (0.0, 0.5):
+        got = lib.qk_norm_rope(q * 1e-3, k * 1e-3, qw, kw, pos, f, eps=eps)
+        check_forward(lib, q * 1e-3, k * 1e-3, qw, kw, pos, f, None, False, eps, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,S,H,Hkv,D", SHAPES + [(2, 700, 8, 2, 64)])
+def test_backward(lib, B, S, H, Hkv, D, dtype):
+    for i, (rot, axes, weights, interleaved) in enumerate([(D, 0, "own", False), (D, 2, "f32", True), (D // 2 // 16 * 16, 0, "f32", False), (D, 0, None, False)]):
+        q, k, _, qw, kw, pos, f, ax = case(B, S, H, Hkv, D, dtype, rot, axes, weights, seed=10 + i)
+        dy = [torch.randn(B, n, S, D, device="cuda").to(dtype) for n in (H, Hkv)]
+        got = lib.qk_norm_rope_backward(*dy, q, k, qw, kw, pos, f, axes=ax, interleaved=interleaved)
+        phi = ref.angles(pos, f, None if ax is None else ax.tolist(), B, S)
+        for which, (g, x, w) in enumerate(((dy[0], q, qw), (dy[1], k, kw))):
+            dx, dw, size, dw_size = ref.norm_rope_backward(g, x, w, phi, 1e-6, interleaved)
+            check(got[which], dx, size * math.sqrt(2), 2.0 ** -17)
+            if w is None:
+                assert got[2 + which] is None
+            else:
+                assert got[2 + which].dtype == w.dtype
+                check(got[2 + which], dw, dw_size, (B * S * x.shape[2] + 64) * 2.0 ** -24 + 2.0 ** -18)
+
+
+def test_backward_against_differences(lib):
+    """The derivative of sum(dy * forward), by differences of the 64-bit forward, at a few elements of x and w."""
+    q, k, _, qw, kw, pos, f, _ = case(1, 6, 3, 2, 64, torch.float16, weights="f32", seed=5)
+    dy = torch.randn(1, 3, 6, 64, device="cuda").to(torch.float16)
+    got = lib.qk_norm_rope_backward(dy, torch.zeros(1, 2, 6, 64, device="cuda", dtype=torch.float16), q, k, qw, kw, pos, f)
+    phi = ref.angles(pos, f, None, 1, 6)
+    loss = lambda x, w: float((ref.norm_rope(x, w, phi, 1e-6, False) * dy.double().cpu()).sum())
+    x0, w0, h = q.double().cpu(), qw.double().cpu(), 1e-6
+    for s, head, d in ((0, 0, 0), (2, 1, 31), (5, 2, 63), (3, 0, 40)):
+        up, down = x0.clone(), x0.clone()
+        up[0, s, head, d] += h
+        down[0, s, head, d] -= h
+        want = (loss(up, w0) - loss(down, w0)) / (2 * h)
+        assert abs(float(got[0][0, s, head, d]) - want) <= 2.0 ** -11 * abs(want) + 1e-4
+        up, down = w0.clone(), w0.clone()
+        up[d] += h
+        down[d] -= h
+        want = (loss(x0, up) - loss(x0, down)) / (2 * h)
+        assert abs(float(got[2][d]) - want) <= 1e-4 * max(1.0, abs(want))
+    assert bool((got[1] == 0).all()) and bool((got[3] == 0).all())
+
+
+def test_backward_into_a_packed_gradient_repeats_its_bits(lib):
+    B, S, H, Hkv, D = 2, 37, 6, 2, 96
+    q, k, _, qw, kw, pos, f, _ = case(B, S, H, Hkv, D, torch.bfloat16, seed=7)
+    dy = [torch.randn(B, n, S, D, device="cuda").to(torch.bfloat16) for n in (H, Hkv)]
+    want = lib.qk_norm_rope_backward(*dy, q, k, qw, kw, pos, f)
+    packed = torch.full((B, S, H + 2 * Hkv, D), 3.0, device="cuda", dtype=torch.bfloat16)
+    dq, dk, dv = packed.split([H, Hkv, Hkv], dim=2)
+    ws = torch.full((lib.load_library().tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(B, S, D) // 4,), math.nan, device="cuda")
+    got = lib.qk_norm_rope_backward(*dy, q, k, qw, kw, pos, f, grads=(dq, dk), workspace=ws)
+    assert got[0] is dq and got[1] is dk and bool((dv == 3.0).all())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_no_tokens(lib):
+    """Nothing to do, but the weights' gradients are sums of nothing."""
+    for B, S in ((0, 5), (2, 0)):
+        q, k, _, qw, kw, pos, f, _ = case(B, S, 4, 2, 64, torch.float16)
+        assert [x.shape for x in lib.qk_norm_rope(q, k, qw, kw, pos, f)] == [(B, 4, S, 64), (B, 2, S, 64)]
+        grads = lib.qk_norm_rope_backward(q.transpose(1, 2).contiguous(), k.transpose(1, 2).contiguous(), q, k, qw, kw, pos, f)
+        assert bool((grads[2] == 0).all()) and bool((grads[3] == 0).all())
+
+
+@pytest.mark.parametrize("D,R", [(64, 64), (96, 37), (128, 128), (160, 1)])
+def test_cache(lib, D, R):
+    B, S, H, Hkv, P = 3, 21, 7, 3, 150
+    q, k, v, qw, kw, pos, f, _ = case(B, S, H, Hkv, D, torch.bfloat16, seed=9)
+    slots = torch.randperm(P * R, device="cuda")[:B * S].to(torch.int32).view(B, S) if P * R >= B * S else None
+    slots[0, :4], slots[2, 20], slots[1, 3], slots[1, 4] = -1, P * R, -2 ** 31, 2 ** 31 - 1
+    caches = [torch.randn(P, Hkv, R, D, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    before = [c.clone() for c in caches]
+    got = lib.qk_norm_rope_cache(q, k, v, qw, kw, pos, f, *caches, slots)
+    want = lib.qk_norm_rope(q, k, qw, kw, pos, f)
+    assert torch.equal(got, want[0])
+    for b in range(B):
+        for s in range(S):
+            slot = int(slots[b, s])
+            if 0 <= slot < P * R:
+                before[0][slot // R, :, slot % R] = want[1][b, :, s]
+                before[1][slot // R, :, slot % R] = v[b, s]
+    assert torch.equal(caches[0], before[0]) and torch.equal(caches[1], before[1])
+
+
+def test_the_same_slot_twice(lib):
+    """Whole rows of one of the tokens, whichever."""
+    q, k, v, qw, kw, pos, f, _ = case(1, 6, 2, 1, 64, torch.float16)
+    kc, vc = torch.zeros(1, 1, 64, 64, device="cuda", dtype=torch.float16), torch.zeros(1, 1, 64, 64, device="cuda", dtype=torch.float16)
+    lib.qk_norm_rope_cache(q, k, v, qw, kw, pos, f, kc, vc, torch.full((1, 6), 9, dtype=torch.int32, device="cuda"))
+    want = lib.qk_norm_rope(q, k, qw, kw, pos, f)[1]
+    assert any(torch.equal(kc[0, 0, 9], want[0, 0, s]) for s in range(6)) and any(torch.equal(vc[0, 0, 9], v[0, s, 0]) for s in range(6))
+    kc[0, 0, 9] = 0
+    assert bool((kc == 0).all())
+
+
+def test_tensors_past_2_to_the_31(lib):
+    """More than 2^31 elements in q and in its result, and in a cache."""
+    S, H, D = 140000, 128, 128
+    x = torch.empty(1, S, H + 1, D, device="cuda", dtype=torch.bfloat16)
+    pick = torch.tensor([0, 1, 70001, S - 2, S - 1])
+    x[:, pick] = torch.randn(1, 5, H + 1, D, device="cuda").to(torch.bfloat16)
+    x[:, :1] = x[:, :1]
+    q, k = x.split([H, 1], dim=2)
+    pos, f = torch.arange(S, dtype=torch.int32, device="cuda"), torch.rand(64, device="cuda")
+    got = lib.qk_norm_rope(q, k, None, None, pos, f)
+    assert got[0].numel() > 2 ** 31
+    few = lib.qk_norm_rope(q[:, pick].contiguous(), k[:, pick].contiguous(), None, None, pick.to(torch.int32).cuda(), f)
+    assert torch.equal(got[0][:, :, pick], few[0]) and torch.equal(got[1][:, :, pick], few[1])
+    del got, x, q, k
+    R = 2 ** 20
+    kc = torch.zeros(3, 8, R, D, device="cuda", dtype=torch.bfloat16)
+    vc = torch.zeros_like(kc)
+    assert kc.numel() > 2 ** 31
+    q, k, v, qw, kw, pos, f, _ = case(1, 2, 8, 8, D, torch.bfloat16)
+    slots = torch.tensor([[3 * R - 1, 2 * R + 5]], dtype=torch.int32, device="cuda")
+    lib.qk_norm_rope_cache(q, k, v, qw, kw, pos, f, kc, vc, slots)
+    want = lib.qk_norm_rope(q, k, qw, kw, pos, f)[1]
+    assert torch.equal(kc[2, :, R - 1], want[0, :, 0]) and torch.equal(kc[2, :, 5], want[0, :, 1]) and torch.equal(vc[2, :, R - 1], v[0, 0])
+
+
+def test_captured_and_on_another_stream(lib):
+    q, k, v, qw, kw, pos, f, _ = case(2, 50, 8, 4, 128, torch.bfloat16)
+    dy = [torch.randn(2, n, 50, 128, device="cuda").to(torch.bfloat16) for n in (8, 4)]
+    kc, vc = (torch.zeros(4, 4, 64, 128, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    slots = torch.randperm(256, device="cuda")[:100].to(torch.int32).view(2, 50)
+
+    def work():
+        return (*lib.qk_norm_rope(q, k, qw, kw, pos, f), *lib.qk_norm_rope_backward(*dy, q, k, qw, kw, pos, f),
+                lib.qk_norm_rope_cache(q, k, v, qw, kw, pos, f, kc, vc, slots), kc, vc)
+
+    want = [x.clone() for x in work()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = [x.clone() for x in work()]
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work()
+    for seed in range(3):
+        q.copy_(torch.randn(q.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(seed)).to(q.dtype))
+        kc.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        have = [x.clone() for x in got]
+        assert all(torch.equal(a, b) for a, b in zip(have, work()))
