@@ -138,7 +138,7 @@ int tiled_sdpa_qk_norm_rope_cache(const tsdpa_rope *p, const tsdpa_rows *q, cons
 unsigned long long tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(int B, int S, int D)
 {
     if (B < 0 || S < 0 || D < 0) return 0;
-    return (unsigned long long)tsdpa::rope_bwd_groups((long long)B * S) * 2 * D * sizeof(float);
+    return (unsigned long long)tsdpa::kRopeBwdMost * D * sizeof(float);
 }
 
 int tiled_sdpa_qk_norm_rope_bwd(const tsdpa_rope *p, const void *dq_out, const void *dk_out, const tsdpa_rows *q, const tsdpa_rows *k,
