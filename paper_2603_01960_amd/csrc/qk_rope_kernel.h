@@ -12,7 +12,7 @@
 // built for wide loads, many of them in flight, and whole lines written:
 //   * a lane holds two 16-byte pieces of a row, which between them hold both columns of each of its pairs (columns i and i +
 //     rot / 2 as pairs: pieces rot / 16 apart; neighbouring columns: any two), so that nothing but the sum of squares
-//     crosses lanes.  D / 16 lanes make a row (of 4, 8, 8 or 16 that a row gets, so that the sum is DPP steps);
+//     crosses lanes.  D / 16 lanes make a row;
 //   * a wavefront stays with one token and goes through its heads, so that the angles are computed once for all of them:
 //     in 64 bits up to whole turns (a position of 2^31 has no fraction left in 32), then sine and cosine of the rest;
 //   * all rows of a batch of heads are requested before the first is used.
@@ -45,19 +45,19 @@ struct RopeArgs {
     void *out[3];                                  // q [B, H, S, D]; k the same or the cache; v's cache
     const int *slots;                              // cache form: [B, S]
     int cache_rows, block_rows;                    // rows of all pages (slots past it go nowhere), rows of a page
-    Divisor by_rows, by_s, by_spans;
-    int spans, units_per_span;                     // parts of a token that a wavefront each takes; their row groups
-    int waves;                                     // wavefronts of the launch
-    // backward, for q and k: workgroups (those of q first), parts of a token that a wavefront each takes, heads of a part
-    int bwd_groups[2], bwd_spans[2], bwd_heads[2];
-    Divisor bwd_by_spans[2];
+    Divisor by_rows, by_s;
+    // of q, and of k (and v): parts of a token that a wavefront each takes, heads of a part; backward: workgroups (those of q first)
+    int spans[2], part[2];
+    Divisor by_spans[2];
+    int groups[2];
+    int waves;                                     // forward: wavefronts of the launch
     float *partial;                                // backward: [workgroups][D], sums of a weight's gradient
     hipStream_t stream;
 };
 
 template <int D> struct RopeGeom {
-    static constexpr int LANES = D == 64 ? 4 : D == 160 ? 16 : 8;        // lanes of a row, of which D / 16 hold something
-    static constexpr int ROWS = 64 / LANES;                              // rows of a wavefront at a time
+    static constexpr int LANES = D / 16;           // lanes of a row
+    static constexpr int ROWS = 64 / LANES;        // rows of a wavefront at a time: 16, 10, 8 and 6 (the last 4 lanes are idle at D = 96, 160)
 };
 
 int launch_rope_f16(int D, bool cache, const RopeArgs &a);
@@ -65,14 +65,11 @@ int launch_rope_bf16(int D, bool cache, const RopeArgs &a);
 int launch_rope_bwd_f16(int D, const RopeArgs &a);
 int launch_rope_bwd_bf16(int D, const RopeArgs &a);
 
-#ifndef ROPE_BOCC
-#define ROPE_BATCH 2
-#define ROPE_OCC 4
-#define ROPE_BBATCH 1
-#define ROPE_BOCC 4
-#endif
-// Backward: most workgroups of a launch (as many as the GPU holds); each leaves a row of partial sums.
-constexpr int kRopeBwdMost = ROPE_BOCC * 256;
+// Wavefronts per SIMD that the kernels are built for, and launches of no more: they are persistent.  One row group at a time and one
+// on its way needs few registers.  (us, forward at 4 / 5 / 6 wavefronts: B=2 S=8192 H=32+8 D=128 BF16 64.2 / 63.5 / 63.5, B=4 S=512 of it
+// into a cache 11.2 / 10.8 / 10.8; backward at 2 / 3 / 4: 93.0 / 98.1 / 99.4, B=4 S=2048 H=16+4 D=160 FP16 37.7 / 38.2 / 43.4: more rows of
+// partial sums, and no registers to spare.  Two row groups at a time: forward 65.1, backward 98.8 and 40.6.)
+constexpr int kRopeWaves = 5 * 1024, kRopeBwdMost = 2 * 256;   // wavefronts; workgroups, each of which leaves a row of partial sums
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
@@ -85,16 +82,6 @@ template <int CTRL> __device__ __forceinline__ float rope_dpp_add(float x)
     const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true);
     return x + __builtin_bit_cast(float, y);
 }
-// the sum over the lanes of a row, in each of them
-template <int LANES> __device__ __forceinline__ float rope_row_sum(float x)
-{
-    x = rope_dpp_add<0xB1>(x);                     // lane ^ 1
-    x = rope_dpp_add<0x4E>(x);                     // lane ^ 2
-    if constexpr (LANES >= 8) x = rope_dpp_add<0x141>(x);       // mirrored within 8 lanes
-    if constexpr (LANES >= 16) x = rope_dpp_add<0x140>(x);      // ... within 16
-    return x;
-}
-
 // The two pieces of a row as 16 FP32 values, x and y: pair i is (x[i], y[i]).  Half a rotation apart that is what the pieces are; of
 // neighbouring columns (INTER) x takes the even ones of both pieces and y the odd ones.
 template <typename T, bool INTER> struct RopePairs {
@@ -143,15 +130,22 @@ template <typename T, bool INTER> struct RopePairs {
 // What a lane has of every row.
 template <int D, bool INTER> struct RopeLane {
     int row, col[2];                               // row within the wavefront's; first columns of the two pieces
-    bool active;                                   // the lane has something of the row
+    bool active;                                   // the lane has a row
     int first;                                     // its first pair, of the D / 2 that the lanes of a row have
+    int other[4];                                  // D = 96, 160: lanes that row_sum takes (times 4)
     __device__ __forceinline__ RopeLane(int rot, int lane)
     {
         using G = RopeGeom<D>;
         row = lane / G::LANES;
-        const int own = lane % G::LANES, j = own < D / 16 ? own : D / 16 - 1;
-        active = own < D / 16;
+        const int j = lane % G::LANES;
+        active = row < G::ROWS;
         first = j * 8;
+        constexpr int H = G::LANES / 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int distance = i == 0 ? H : i == 1 ? 1 : i == 2 ? 2 : H - 1;
+            other[i] = (lane - j + (j + distance) % G::LANES) * 4;
+        }
         col[0] = columns(rot, j, 0);
         col[1] = columns(rot, j, 1);
     }
@@ -163,7 +157,24 @@ template <int D, bool INTER> struct RopeLane {
     }
     // the column of x[i] (p = 0) or y[i], from the first columns of the pieces
     static __device__ __forceinline__ int column(int c0, int c1, int p, int i) { return !INTER ? (p ? c1 : c0) + i : (i < 4 ? c0 + 2 * i : c1 + 2 * i - 8) + p; }
-    __device__ __forceinline__ float row_sum(float x) const { return rope_row_sum<RopeGeom<D>::LANES>(RopeGeom<D>::LANES * 16 == D || active ? x : 0.f); }
+    static __device__ __forceinline__ float from(float x, int lane4) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(lane4, __builtin_bit_cast(int, x))); }
+    // The sum over the lanes of a row, in each of them.  A row of 4 or 8 lanes: DPP steps.  Of 6 or 10: the two lanes half a row apart, then
+    // H = 3 or 5 such pairs, one after another (the lanes add them in different orders, which may differ in the last bit).
+    __device__ __forceinline__ float row_sum(float x) const
+    {
+        if constexpr (RopeGeom<D>::LANES == 4 || RopeGeom<D>::LANES == 8) {
+            x = rope_dpp_add<0xB1>(x);             // lane ^ 1
+            x = rope_dpp_add<0x4E>(x);             // lane ^ 2
+            if constexpr (RopeGeom<D>::LANES == 8) x = rope_dpp_add<0x141>(x);       // mirrored within 8 lanes
+            return x;
+        } else {
+            const float pair = x + from(x, other[0]);
+            const float two = pair + from(pair, other[1]);
+            if constexpr (RopeGeom<D>::LANES == 6) return two + from(pair, other[2]);
+            const float four = two + from(two, other[2]);
+            return four + from(pair, other[3]);
+        }
+    }
     // 1 / sqrt(mean of squares + eps) of the row
     __device__ __forceinline__ float scale(const float (&x)[8], const float (&y)[8], float eps) const
     {
@@ -175,13 +186,13 @@ template <int D, bool INTER> struct RopeLane {
 };
 
 // The angles of a token's pairs: computed once per wavefront, a lane a pair, and handed to the lanes that need them through the LDS
-// (a wavefront's own part, whose accesses are in order).  Tables of D / 2 values, V of them per token: cosine and sine of each pair,
-// or (forward) both times the weights of its two columns, for q and for k.
-template <typename T, int D, bool INTER, int V> struct RopeTable {
+// (a wavefront's own part, whose accesses are in order).  Tables of D / 2 values: cosine and sine of each pair, or (FOLD) both times the
+// weights of its two columns.
+template <typename T, int D, bool INTER> struct RopeTable {
     static constexpr int EACH = (D / 2 + 63) / 64;       // pairs of a lane
     double step[EACH];                             // turns per position
-    int axis[EACH];
-    float w[EACH][2][2];                           // weights of q and k for the pair's columns
+    long long axis[EACH];                          // where its axis's positions begin
+    int column[EACH][2];
     float *mine;
     __device__ __forceinline__ RopeTable(const RopeArgs &a, int lane, float *wave_sh) : mine(wave_sh + lane)
     {
@@ -193,41 +204,48 @@ template <typename T, int D, bool INTER, int V> struct RopeTable {
             const bool turns = j < a.rot / 16;
             step[e] = turns ? (double)a.inv_freq[pair] * 0.15915494309189533577 : 0.0;
             int x = turns && a.axes != nullptr ? a.axes[pair] : 0;
-            axis[e] = x < 0 ? 0 : x < a.n_axes ? x : a.n_axes - 1;
+            x = x < 0 ? 0 : x < a.n_axes ? x : a.n_axes - 1;
+            axis[e] = x * a.pos_axis;
 #pragma unroll
-            for (int which = 0; which < 2; ++which)
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int col = RopeLane<D, INTER>::column(c0, c1, p, i);
-                    w[e][which][p] = a.weight[which] == nullptr ? 1.f : a.weight32 ? ((const float *)a.weight[which])[col] : (float)((const T *)a.weight[which])[col];
-                }
+            for (int p = 0; p < 2; ++p) column[e][p] = RopeLane<D, INTER>::column(c0, c1, p, i);
         }
     }
-    // v_sin and v_cos take whole turns: off by at most 2^-22.9 over one
-    __device__ __forceinline__ void fill(const RopeArgs &a, int b, int s) const
+    // whether the lane has an e-th pair
+    __device__ __forceinline__ bool has(int e) const { return (D / 2) % 64 == 0 || (int)(threadIdx.x & 63) + e * 64 < D / 2; }
+    __device__ __forceinline__ void positions(const RopeArgs &a, int b, int s, int (&to)[EACH]) const
     {
         const int *at = a.positions + ((long long)b * a.pos_batch + s);
-        const int position = a.rot > 0 ? *at : 0;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) to[e] = a.rot > 0 ? at[axis[e]] : 0;
+    }
+    template <bool FOLD> __device__ __forceinline__ void fill(const int (&position)[EACH], const float (&w)[EACH][2]) const
+    {
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const double p = a.axes == nullptr || a.rot == 0 ? (double)position : (double)at[(long long)axis[e] * a.pos_axis], x = p * step[e];
+            const double x = (double)position[e] * step[e];
+            // v_sin and v_cos take whole turns: off by at most 2^-22.9 over one
             const float t = (float)(x - __builtin_rint(x)), c = __builtin_amdgcn_cosf(t), sn = __builtin_amdgcn_sinf(t);
-            if ((D / 2) % 64 != 0 && (int)(threadIdx.x & 63) + e * 64 >= D / 2) continue;
+            if (!has(e)) continue;
             float *to = mine + e * 64;
-            if constexpr (V == 2) {
+            if constexpr (FOLD) {
+                to[0] = w[e][0] * c;
+                to[D / 2] = w[e][0] * sn;
+                to[2 * (D / 2)] = w[e][1] * c;
+                to[3 * (D / 2)] = w[e][1] * sn;
+            } else {
                 to[0] = c;
                 to[D / 2] = sn;
-            } else {
-#pragma unroll
-                for (int which = 0; which < 2; ++which) {
-                    to[(which * 4 + 0) * (D / 2)] = w[e][which][0] * c;
-                    to[(which * 4 + 1) * (D / 2)] = w[e][which][0] * sn;
-                    to[(which * 4 + 2) * (D / 2)] = w[e][which][1] * c;
-                    to[(which * 4 + 3) * (D / 2)] = w[e][which][1] * sn;
-                }
             }
         }
         __builtin_amdgcn_wave_barrier();
+    }
+    // the weights of its pairs' columns (1 without a norm)
+    __device__ __forceinline__ void weights(const void *at, int weight32, float (&w)[EACH][2]) const
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) w[e][p] = at == nullptr ? 1.f : weight32 ? ((const float *)at)[column[e][p]] : (float)((const T *)at)[column[e][p]];
     }
 };
 __device__ __forceinline__ void rope_table_read(float (&x)[8], const float *at)
@@ -238,139 +256,171 @@ __device__ __forceinline__ void rope_table_read(float (&x)[8], const float *at)
     for (int i = 0; i < 8; ++i) x[i] = i < 4 ? lo[i & 3] : hi[i & 3];
 }
 
-// A lane's two pieces of a row group, at base + scalar offset; lanes without one keep what is in the registers, which nothing uses.
-template <typename T> struct RopePointers {
-    const T *at[2];
-    __device__ __forceinline__ RopePointers(const void *base, long long row, const int (&col)[2])
-    {
-        at[0] = (const T *)base + row + col[0];
-        at[1] = (const T *)base + row + col[1];
+// A lane's two pieces of a row group; lanes without one keep what is in the registers, which nothing uses.  STREAM: past the caches.
+template <bool STREAM, typename T> __device__ __forceinline__ void rope_load(rope_u32x4 (&raw)[2], const T *at, const int (&col)[2], bool mine)
+{
+    asm("" : "=v"(raw[0]), "=v"(raw[1]));
+    if (!mine) return;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const rope_u32x4 *from = (const rope_u32x4 *)(at + col[p]);
+        if constexpr (STREAM) raw[p] = __builtin_nontemporal_load(from);
+        else raw[p] = *from;
     }
-    __device__ __forceinline__ void load(rope_u32x4 (&raw)[2], long long offset, bool mine) const
-    {
-        asm("" : "=v"(raw[0]), "=v"(raw[1]));
-        if (!mine) return;
-        raw[0] = *(const rope_u32x4 *)(at[0] + offset);
-        raw[1] = *(const rope_u32x4 *)(at[1] + offset);
+}
+template <bool STREAM, typename T> __device__ __forceinline__ void rope_store(const rope_u32x4 (&raw)[2], T *at, const int (&col)[2])
+{
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        rope_u32x4 *to = (rope_u32x4 *)(at + col[p]);
+        if constexpr (STREAM) __builtin_nontemporal_store(raw[p], to);
+        else *to = raw[p];
     }
-    __device__ __forceinline__ void store(const rope_u32x4 (&raw)[2], long long offset) const
-    {
-        *(rope_u32x4 *)(at[0] + offset) = raw[0];
-        *(rope_u32x4 *)(at[1] + offset) = raw[1];
-    }
-};
+}
 #endif
 
-// Row groups (of RopeGeom::ROWS heads) whose rows are requested together.
-constexpr int kRopeBatch = ROPE_BATCH, kRopeWaves = ROPE_OCC * 1024;
-
-template <typename T, int D, bool CACHE, bool INTER> __global__ void __launch_bounds__(256, ROPE_OCC) rope_kernel(RopeArgs a)
+// An item is a tensor's heads of one token, or some of them; first those of q, then of k, then of v.  While one row group (of
+// RopeGeom::ROWS heads) is worked on, the next one's loads are on their way, the next item's first one among them.
+template <typename T, int D, bool CACHE, bool INTER, bool STREAM> __global__ void __launch_bounds__(256, 5) rope_kernel(RopeArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using G = RopeGeom<D>;
     using P = RopePairs<T, INTER>;
-    __shared__ __attribute__((aligned(16))) float table_sh[4][8 * (D / 2)];
+    using Table = RopeTable<T, D, INTER>;
+    __shared__ __attribute__((aligned(16))) float table_sh[4][4 * (D / 2)];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const int items = a.B * a.S * a.spans;
+    const int tokens = a.B * a.S;
+    const int items_q = tokens * a.spans[0], items_qk = items_q + tokens * a.spans[1], items = items_qk + (CACHE ? tokens * a.spans[1] : 0);
     if (wave >= items) return;
     const RopeLane<D, INTER> me(a.rot, lane);
     float *const table = table_sh[threadIdx.x >> 6];
-    const RopeTable<T, D, INTER, 8> pairs(a, lane, table);
-    for (int item = wave; item < items; item += a.waves) {
-        const int token = rope_divide(item, a.by_spans), span = item - token * a.spans;
-        const int b = rope_divide(token, a.by_s), s = token - b * a.S;
-        long long cache_row = -1;                  // the slot's row for head 0
-        if constexpr (CACHE) {
-            const int slot = __builtin_amdgcn_readfirstlane(a.slots[token]);
-            if (slot >= 0 && slot < a.cache_rows) {
-                const int page = rope_divide(slot, a.by_rows);
-                cache_row = (long long)page * a.heads[1] * a.block_rows + (slot - page * a.block_rows);
-            }
+    const Table pairs(a, lane, table);
+    float weights[2][Table::EACH][2];
+    pairs.weights(a.weight[0], a.weight32, weights[0]);
+    pairs.weights(a.weight[1], a.weight32, weights[1]);
+
+    struct Item { int which, b, s, token, first, last; };      // (first and last head)
+    auto item_at = [&](int i) __attribute__((always_inline)) {
+        Item x;
+        x.which = i < items_q ? 0 : !CACHE || i < items_qk ? 1 : 2;
+        const int n = i - (x.which == 0 ? 0 : x.which == 1 ? items_q : items_qk);
+        x.token = x.which == 0 ? rope_divide(n, a.by_spans[0]) : rope_divide(n, a.by_spans[1]);
+        const int part = x.which == 0 ? a.part[0] : a.part[1], heads = x.which == 0 ? a.heads[0] : a.heads[1];
+        x.first = (n - x.token * (x.which == 0 ? a.spans[0] : a.spans[1])) * part;
+        x.last = x.first + part < heads ? x.first + part : heads;
+        x.b = rope_divide(x.token, a.by_s);
+        x.s = x.token - x.b * a.S;
+        return x;
+    };
+    auto load = [&](const Item &x, int h0, rope_u32x4 (&raw)[2]) __attribute__((always_inline)) {
+        const RopeRows in = x.which == 0 ? a.x[0] : !CACHE || x.which == 1 ? a.x[1] : a.x[2];
+        const T *from = (const T *)in.data + (long long)x.b * in.batch + (long long)x.s * in.row + h0 * in.head;
+        rope_load<STREAM>(raw, from + me.row * in.head, me.col, me.active && h0 + me.row < x.last);
+    };
+
+    // (two sets of registers that take turns: a copy from one to the other would wait for the loads)
+    struct Rows { rope_u32x4 raw[2]; int position[Table::EACH]; };
+    Item cur = item_at(wave);
+    int next_item = wave + a.waves, h0 = cur.first;
+    bool fresh = true;
+    Rows one, two;
+    pairs.positions(a, cur.b, cur.s, one.position);
+    load(cur, h0, one.raw);
+    // works on `now` and requests the next row group into `then`; false after the last
+    auto turn = [&](Rows &now, Rows &then) __attribute__((always_inline)) {
+        Item next = cur;
+        int next_h0 = h0 + G::ROWS;
+        const bool steps = next_h0 >= cur.last, more = !steps || next_item < items;
+        if (steps && more) {
+            next = item_at(next_item);
+            next_h0 = next.first;
+            next_item += a.waves;
+            pairs.positions(a, next.b, next.s, then.position);
         }
-        pairs.fill(a, b, s);
-        int unit0 = 0;                             // first row group of the tensor
-#pragma unroll
-        for (int which = 0; which < (CACHE ? 3 : 2); ++which) {
-            const int heads = a.heads[which], groups = (heads + G::ROWS - 1) / G::ROWS;
-            // this span's row groups of the tensor
-            int g0 = span * a.units_per_span - unit0, g1 = g0 + a.units_per_span;
-            unit0 += groups;
-            g0 = g0 > 0 ? g0 : 0;
-            g1 = g1 < groups ? g1 : groups;
-            if (g0 >= g1 || (CACHE && which > 0 && cache_row < 0)) continue;
-            const bool norm = which < 2 && a.weight[which & 1] != nullptr;
-            // rows are x_a (w_a cos), x_b (w_b sin) and so on, times the row's 1 / root
-            float cx[8], sx[8], cy[8], sy[8];
-            if (which < 2) {
-                const float *at = table + which * 4 * (D / 2) + me.first;
-                rope_table_read(cx, at);
-                rope_table_read(sx, at + D / 2);
-                rope_table_read(cy, at + 2 * (D / 2));
-                rope_table_read(sy, at + 3 * (D / 2));
-            }
-            const RopeRows &in = a.x[which];
-            const RopePointers<T> from((const T *)in.data + (long long)b * in.batch + (long long)s * in.row, me.row * in.head, me.col);
-            const bool cached = CACHE && which > 0;
-            const long long to_head = (long long)(cached ? a.block_rows : a.S) * D;
-            const RopePointers<T> to((const T *)a.out[which] + (cached ? cache_row * D : ((long long)b * heads * a.S + s) * D), me.row * to_head, me.col);
-            for (int g = g0; g < g1; g += kRopeBatch) {
-                rope_u32x4 raw[kRopeBatch][2];
-#pragma unroll
-                for (int u = 0; u < kRopeBatch; ++u)
-                    if (u == 0 || g + u < g1) from.load(raw[u], (long long)(g + u) * G::ROWS * in.head, (g + u) * G::ROWS + me.row < heads);
-#pragma unroll
-                for (int u = 0; u < kRopeBatch; ++u) {
-                    if (u > 0 && g + u >= g1) continue;
-                    if (which < 2) {
-                        float x[8], y[8], r = 1.f;
-                        P::read(x, y, raw[u]);
-                        if (norm) r = me.scale(x, y, a.eps);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float x0 = x[i], y0 = y[i];
-                            x[i] = r * __builtin_fmaf(x0, cx[i], -(y0 * sy[i]));
-                            y[i] = r * __builtin_fmaf(y0, cy[i], x0 * sx[i]);
-                        }
-                        P::write(raw[u], x, y);
-                    }
-                    if (me.active && (g + u) * G::ROWS + me.row < heads) to.store(raw[u], (long long)(g + u) * G::ROWS * to_head);
-                }
-            }
+        if (more) load(next, next_h0, then.raw);
+        if (fresh && (!CACHE || cur.which < 2)) {
+            if (cur.which == 0) pairs.template fill<true>(now.position, weights[0]);
+            else pairs.template fill<true>(now.position, weights[1]);
         }
-    }
+        const int heads = cur.which == 0 ? a.heads[0] : a.heads[1];
+        T *to;
+        long long to_head = (long long)a.S * D;
+        bool written = true;
+        if (CACHE && cur.which > 0) {
+            const int slot = __builtin_amdgcn_readfirstlane(a.slots[cur.token]);
+            written = slot >= 0 && slot < a.cache_rows;
+            const int page = rope_divide(written ? slot : 0, a.by_rows);
+            to_head = (long long)a.block_rows * D;
+            to = (T *)(cur.which == 1 ? a.out[1] : a.out[2]) + ((long long)page * heads * a.block_rows + (slot - page * a.block_rows)) * D;
+        } else {
+            to = (T *)(cur.which == 0 ? a.out[0] : a.out[1]) + ((long long)cur.b * heads * a.S + cur.s) * D;
+        }
+        to += h0 * to_head;
+        // rows are x_a (w_a cos), x_b (w_b sin) and so on, times the row's 1 / root
+        float cx[8], sx[8], cy[8], sy[8];
+        const bool norm = (cur.which == 0 ? a.weight[0] : a.weight[1]) != nullptr, copy = CACHE && cur.which == 2;
+        if (!copy) {
+            const float *at = table + me.first;
+            rope_table_read(cx, at);
+            rope_table_read(sx, at + D / 2);
+            rope_table_read(cy, at + 2 * (D / 2));
+            rope_table_read(sy, at + 3 * (D / 2));
+        }
+        if (!copy) {
+            float x[8], y[8], r = 1.f;
+            P::read(x, y, now.raw);
+            if (norm) r = me.scale(x, y, a.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x0 = x[i], y0 = y[i];
+                x[i] = r * __builtin_fmaf(x0, cx[i], -(y0 * sy[i]));
+                y[i] = r * __builtin_fmaf(y0, cy[i], x0 * sx[i]);
+            }
+            P::write(now.raw, x, y);
+        }
+        if (written && me.active && h0 + me.row < cur.last) rope_store<STREAM>(now.raw, to + me.row * to_head, me.col);
+        fresh = steps;
+        cur = next;
+        h0 = next_h0;
+        return more;
+    };
+    while (turn(one, two) && turn(two, one)) {}
 #endif
 }
 
 // Backward.  A workgroup has one of the two tensors: its wavefronts take every so manieth token (or part of one) and keep the sums of
 // their columns' weight gradients in registers; the workgroup's are added in the LDS, in a fixed order, and written to its row of
-// partial sums.
-constexpr int kRopeBwdBatch = ROPE_BBATCH;
-template <typename T, int D, bool INTER> __global__ void __launch_bounds__(256, ROPE_BOCC) rope_bwd_kernel(RopeArgs a)
+// partial sums.  The loads run ahead as in the forward kernel.
+template <typename T, int D, bool INTER, bool STREAM> __global__ void __launch_bounds__(256, 2) rope_bwd_kernel(RopeArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using G = RopeGeom<D>;
     using P = RopePairs<T, INTER>;
+    using Table = RopeTable<T, D, INTER>;
     __shared__ __attribute__((aligned(16))) float table_sh[4][2 * (D / 2)], weight_sh[2][D / 2];
-    __shared__ float sums_sh[4][D];
+    __shared__ float sums_sh[4 * G::ROWS][D];
     const int lane = threadIdx.x & 63, wave_in = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool is_k = (int)blockIdx.x >= a.bwd_groups[0];
-    const int groups = is_k ? a.bwd_groups[1] : a.bwd_groups[0], wave = (blockIdx.x - (is_k ? a.bwd_groups[0] : 0)) * 4 + wave_in;
-    const int heads = is_k ? a.heads[1] : a.heads[0], spans = is_k ? a.bwd_spans[1] : a.bwd_spans[0], part = is_k ? a.bwd_heads[1] : a.bwd_heads[0];
-    const Divisor by_spans = is_k ? a.bwd_by_spans[1] : a.bwd_by_spans[0];
+    const bool is_k = (int)blockIdx.x >= a.groups[0];
+    const int groups = is_k ? a.groups[1] : a.groups[0], wave = (blockIdx.x - (is_k ? a.groups[0] : 0)) * 4 + wave_in;
+    const int heads = is_k ? a.heads[1] : a.heads[0], spans = is_k ? a.spans[1] : a.spans[0], part = is_k ? a.part[1] : a.part[0];
+    const Divisor by_spans = is_k ? a.by_spans[1] : a.by_spans[0];
     const RopeRows in = is_k ? a.x[1] : a.x[0], out = is_k ? a.grad[1] : a.grad[0];
     const T *const grads = (const T *)(is_k ? a.dy[1] : a.dy[0]);
-    const bool norm = (is_k ? a.weight[1] : a.weight[0]) != nullptr;
+    const void *const weight = is_k ? a.weight[1] : a.weight[0];
+    const bool norm = weight != nullptr;
     const long long dy_head = (long long)a.S * D;
     const RopeLane<D, INTER> me(a.rot, lane);
     float *const table = table_sh[wave_in];
-    const RopeTable<T, D, INTER, 2> pairs(a, lane, table);
+    const Table pairs(a, lane, table);
+    float w[Table::EACH][2];
+    pairs.weights(weight, a.weight32, w);
     if (wave_in == 0)
 #pragma unroll
-        for (int e = 0; e < pairs.EACH; ++e)
+        for (int e = 0; e < Table::EACH; ++e)
 #pragma unroll
             for (int p = 0; p < 2; ++p)
-                if (lane + e * 64 < D / 2) weight_sh[p][lane + e * 64] = is_k ? pairs.w[e][1][p] : pairs.w[e][0][p];
+                if (pairs.has(e)) weight_sh[p][lane + e * 64] = w[e][p];
     __syncthreads();
     float wx[8], wy[8], dwx[8], dwy[8];
     rope_table_read(wx, weight_sh[0] + me.first);
@@ -378,77 +428,103 @@ template <typename T, int D, bool INTER> __global__ void __launch_bounds__(256, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) dwx[i] = dwy[i] = 0.f;
     const int items = a.B * a.S * spans;
-    for (int item = wave; item < items; item += groups * 4) {
-        const int token = rope_divide(item, by_spans), b = rope_divide(token, a.by_s), s = token - b * a.S;
-        const int first = (item - token * spans) * part, last = first + part < heads ? first + part : heads;
-        const RopePointers<T> dy(grads + ((long long)b * heads * a.S + s) * D, me.row * dy_head, me.col);
-        const RopePointers<T> from((const T *)in.data + (long long)b * in.batch + (long long)s * in.row, me.row * in.head, me.col);
-        const RopePointers<T> to((const T *)out.data + (long long)b * out.batch + (long long)s * out.row, me.row * out.head, me.col);
-        pairs.fill(a, b, s);
+
+    struct Item { int b, s, first, last; };
+    auto item_at = [&](int i) __attribute__((always_inline)) {
+        Item x;
+        const int token = rope_divide(i, by_spans);
+        x.b = rope_divide(token, a.by_s);
+        x.s = token - x.b * a.S;
+        x.first = (i - token * spans) * part;
+        x.last = x.first + part < heads ? x.first + part : heads;
+        return x;
+    };
+    auto load = [&](const Item &x, int h0, rope_u32x4 (&draw)[2], rope_u32x4 (&raw)[2]) __attribute__((always_inline)) {
+        const T *dy = grads + ((long long)x.b * heads * a.S + x.s) * D + h0 * dy_head;
+        const T *from = (const T *)in.data + (long long)x.b * in.batch + (long long)x.s * in.row + h0 * in.head;
+        const bool mine = me.active && h0 + me.row < x.last;
+        rope_load<STREAM>(draw, dy + me.row * dy_head, me.col, mine);
+        rope_load<STREAM>(raw, from + me.row * in.head, me.col, norm && mine);
+    };
+    struct Rows { rope_u32x4 draw[2], raw[2]; int position[Table::EACH]; };
+    Item cur{};
+    int next_item = wave + groups * 4, h0 = 0;
+    bool fresh = true;
+    Rows one, two;
+    auto turn = [&](Rows &now, Rows &then) __attribute__((always_inline)) {
+        Item next = cur;
+        int next_h0 = h0 + G::ROWS;
+        const bool steps = next_h0 >= cur.last, more = !steps || next_item < items;
+        if (steps && more) {
+            next = item_at(next_item);
+            next_h0 = next.first;
+            next_item += groups * 4;
+            pairs.positions(a, next.b, next.s, then.position);
+        }
+        if (more) load(next, next_h0, then.draw, then.raw);
+        if (fresh) pairs.template fill<false>(now.position, w);
         float c[8], sn[8];
         rope_table_read(c, table + me.first);
         rope_table_read(sn, table + D / 2 + me.first);
-        for (int h0 = first; h0 < last; h0 += kRopeBwdBatch * G::ROWS) {
-            rope_u32x4 draw[kRopeBwdBatch][2], raw[kRopeBwdBatch][2];
+        T *to = (T *)out.data + (long long)cur.b * out.batch + (long long)cur.s * out.row + h0 * out.head;
+        const bool mine = me.active && h0 + me.row < cur.last;
+        float g[8], h[8];
+        P::read(g, h, now.draw);
 #pragma unroll
-            for (int u = 0; u < kRopeBwdBatch; ++u) {
-                const int h1 = h0 + u * G::ROWS;
-                if (u > 0 && h1 >= last) continue;
-                dy.load(draw[u], h1 * dy_head, h1 + me.row < last);
-                from.load(raw[u], h1 * in.head, norm && h1 + me.row < last);
+        for (int i = 0; i < 8; ++i) {                  // rotated back
+            const float g0 = g[i];
+            g[i] = __builtin_fmaf(g0, c[i], h[i] * sn[i]);
+            h[i] = __builtin_fmaf(h[i], c[i], -(g0 * sn[i]));
+        }
+        if (norm) {
+            float x[8], y[8], dot = 0.f;
+            P::read(x, y, now.raw);
+            const float r = me.scale(x, y, a.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float gx = g[i] * x[i], hy = h[i] * y[i];
+                if (mine) {                    // (rows and columns that are not this lane's add nothing)
+                    dwx[i] = __builtin_fmaf(r, gx, dwx[i]);
+                    dwy[i] = __builtin_fmaf(r, hy, dwy[i]);
+                }
+                dot = __builtin_fmaf(wx[i], gx, __builtin_fmaf(wy[i], hy, dot));
             }
+            const float back = r * r * (me.row_sum(dot) * (1.f / D));
 #pragma unroll
-            for (int u = 0; u < kRopeBwdBatch; ++u) {
-                const int h1 = h0 + u * G::ROWS;
-                if (u > 0 && h1 >= last) continue;
-                const bool mine = me.active && h1 + me.row < last;
-                float g[8], h[8];
-                P::read(g, h, draw[u]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {              // rotated back
-                    const float g0 = g[i];
-                    g[i] = __builtin_fmaf(g0, c[i], h[i] * sn[i]);
-                    h[i] = __builtin_fmaf(h[i], c[i], -(g0 * sn[i]));
-                }
-                if (norm) {
-                    float x[8], y[8], dot = 0.f;
-                    P::read(x, y, raw[u]);
-                    const float r = me.scale(x, y, a.eps);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float gx = g[i] * x[i], hy = h[i] * y[i];
-                        if (mine) {                // (rows and columns that are not this lane's add nothing)
-                            dwx[i] = __builtin_fmaf(r, gx, dwx[i]);
-                            dwy[i] = __builtin_fmaf(r, hy, dwy[i]);
-                        }
-                        dot = __builtin_fmaf(wx[i], gx, __builtin_fmaf(wy[i], hy, dot));
-                    }
-                    const float back = r * r * (me.row_sum(dot) * (1.f / D));
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        g[i] = r * __builtin_fmaf(-back, x[i], wx[i] * g[i]);
-                        h[i] = r * __builtin_fmaf(-back, y[i], wy[i] * h[i]);
-                    }
-                }
-                P::write(draw[u], g, h);
-                if (mine) to.store(draw[u], h1 * out.head);
+            for (int i = 0; i < 8; ++i) {
+                g[i] = r * __builtin_fmaf(-back, x[i], wx[i] * g[i]);
+                h[i] = r * __builtin_fmaf(-back, y[i], wy[i] * h[i]);
             }
         }
+        P::write(now.draw, g, h);
+        if (mine) rope_store<STREAM>(now.draw, to + me.row * out.head, me.col);
+        fresh = steps;
+        cur = next;
+        h0 = next_h0;
+        return more;
+    };
+    if (wave < items) {
+        cur = item_at(wave);
+        h0 = cur.first;
+        pairs.positions(a, cur.b, cur.s, one.position);
+        load(cur, h0, one.draw, one.raw);
+        while (turn(one, two) && turn(two, one)) {}
     }
     if (!norm) return;
-    // over the wavefront's rows (lanes a row's length apart), then over the wavefronts
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
+    // over the rows of all wavefronts
+    if (me.active)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float x = p == 0 ? dwx[i] : dwy[i];
-#pragma unroll
-            for (int d = G::LANES; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-            if (me.row == 0 && me.active) sums_sh[wave_in][me.column(me.col[0], me.col[1], p, i)] = x;
+            sums_sh[wave_in * G::ROWS + me.row][me.column(me.col[0], me.col[1], 0, i)] = dwx[i];
+            sums_sh[wave_in * G::ROWS + me.row][me.column(me.col[0], me.col[1], 1, i)] = dwy[i];
         }
     __syncthreads();
-    for (int i = threadIdx.x; i < D; i += 256)
-        a.partial[(size_t)blockIdx.x * D + i] = (sums_sh[0][i] + sums_sh[1][i]) + (sums_sh[2][i] + sums_sh[3][i]);
+    for (int i = threadIdx.x; i < D; i += 256) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4 * G::ROWS; ++r) sum += sums_sh[r][i];
+        a.partial[(size_t)blockIdx.x * D + i] = sum;
+    }
 #endif
 }
 
@@ -478,24 +554,37 @@ rope_bwd_sum_kernel(const float *__restrict__ partial, int groups_q, int groups_
 #endif
 }
 
+// Whether rows go past the caches: where a call's own bytes are more than the 256 MB of the last level, so that they would only push
+// each other out (and the rest).
+inline bool rope_streams(long long bytes) { return bytes > (256ll << 20); }
+
+// A wavefront for all heads of a token's q (or k, or v), or several where the tokens are few: up to `most` wavefronts in all.
+template <int D> void rope_spans(RopeArgs &a, long long tokens, int most)
+{
+    using G = RopeGeom<D>;
+    for (int i = 0; i < 2; ++i) {
+        const int units = (a.heads[i] + G::ROWS - 1) / G::ROWS;
+        long long spans = tokens > 0 ? most / tokens : 1;
+        spans = spans < 1 ? 1 : spans > units ? (units > 0 ? units : 1) : spans;
+        const int per = (int)((units + spans - 1) / spans);
+        a.part[i] = per * G::ROWS;
+        a.spans[i] = per > 0 ? (units + per - 1) / per : 0;
+        a.by_spans[i] = divisor((uint32_t)(a.spans[i] > 0 ? a.spans[i] : 1));
+    }
+}
+
 template <typename T, int D> int launch_rope_dim(bool cache, const RopeArgs &a0)
 {
     RopeArgs a = a0;
-    using G = RopeGeom<D>;
-    int units = 0;
-    for (int i = 0; i < (cache ? 3 : 2); ++i) units += (a.heads[i] + G::ROWS - 1) / G::ROWS;
     const long long tokens = (long long)a.B * a.S;
-    // a wavefront for all heads of a token, or several where the tokens are few
-    const int most = kRopeWaves;
-    const long long want = most / tokens;
-    a.units_per_span = want >= units ? 1 : want <= 1 ? units : (int)((units + want - 1) / want);
-    a.spans = (units + a.units_per_span - 1) / a.units_per_span;
-    a.by_spans = divisor((uint32_t)a.spans);
-    const long long items = tokens * a.spans;
-    const unsigned grid = (unsigned)(((items < most ? items : most) + 3) / 4);
+    rope_spans<D>(a, tokens, kRopeWaves);
+    const long long items = tokens * (a.spans[0] + (cache ? 2 : 1) * a.spans[1]);
+    const unsigned grid = (unsigned)(((items < kRopeWaves ? items : kRopeWaves) + 3) / 4);
     a.waves = (int)grid * 4;
-    const auto kernel = cache ? (a.interleaved ? rope_kernel<T, D, true, true> : rope_kernel<T, D, true, false>)
-                              : (a.interleaved ? rope_kernel<T, D, false, true> : rope_kernel<T, D, false, false>);
+    const bool stream = rope_streams(2 * tokens * (a.heads[0] + a.heads[1]) * D * (long long)sizeof(T));
+    const auto kernel = cache ? (a.interleaved ? rope_kernel<T, D, true, true, false> : rope_kernel<T, D, true, false, false>)
+                      : stream ? (a.interleaved ? rope_kernel<T, D, false, true, true> : rope_kernel<T, D, false, false, true>)
+                               : (a.interleaved ? rope_kernel<T, D, false, true, false> : rope_kernel<T, D, false, false, false>);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, a.stream, a);
     return (int)hipGetLastError();
 }
@@ -504,39 +593,32 @@ template <typename T, int D> int launch_rope_bwd_dim(const RopeArgs &a0, void *d
 {
     RopeArgs a = a0;
     using G = RopeGeom<D>;
-    // A wavefront for all heads of a token, or several where the tokens are few; and workgroups for as many, up to what the GPU holds, which
-    // the tensors share as they share the rows.
+    // Workgroups for as many wavefronts, up to what the GPU holds, which the tensors share as they share the rows.
     const long long tokens = (long long)a.B * a.S;
-    long long wanted[2];
-    int units[2];
-    for (int i = 0; i < 2; ++i) {
-        units[i] = (a.heads[i] + G::ROWS - 1) / G::ROWS;
-        long long spans = tokens > 0 ? kRopeBwdMost * 2 / tokens : 1;
-        spans = spans < 1 ? 1 : spans > units[i] ? (units[i] > 0 ? units[i] : 1) : spans;
-        const int per = (int)((units[i] + spans - 1) / spans);
-        a.bwd_heads[i] = per * G::ROWS;
-        a.bwd_spans[i] = per > 0 ? (units[i] + per - 1) / per : 0;
-        a.bwd_by_spans[i] = divisor((uint32_t)(a.bwd_spans[i] > 0 ? a.bwd_spans[i] : 1));
-        wanted[i] = (tokens * a.bwd_spans[i] + 3) / 4;
-    }
+    rope_spans<D>(a, tokens, kRopeBwdMost * 4);
+    const long long wanted[2] = {(tokens * a.spans[0] + 3) / 4, (tokens * a.spans[1] + 3) / 4};
+    const int units[2] = {(a.heads[0] + G::ROWS - 1) / G::ROWS, (a.heads[1] + G::ROWS - 1) / G::ROWS};
     if (wanted[0] + wanted[1] <= kRopeBwdMost) {
-        a.bwd_groups[0] = (int)wanted[0];
-        a.bwd_groups[1] = (int)wanted[1];
+        a.groups[0] = (int)wanted[0];
+        a.groups[1] = (int)wanted[1];
     } else {
         long long share = (long long)kRopeBwdMost * units[0] / (units[0] + units[1]);
         if (share < 1 && units[0] > 0) share = 1;
         if (share >= kRopeBwdMost && units[1] > 0) share = kRopeBwdMost - 1;
-        a.bwd_groups[0] = (int)(share < wanted[0] ? share : wanted[0]);
-        a.bwd_groups[1] = (int)(kRopeBwdMost - share < wanted[1] ? kRopeBwdMost - share : wanted[1]);
+        a.groups[0] = (int)(share < wanted[0] ? share : wanted[0]);
+        a.groups[1] = (int)(kRopeBwdMost - share < wanted[1] ? kRopeBwdMost - share : wanted[1]);
     }
-    const int groups = a.bwd_groups[0] + a.bwd_groups[1];
+    const int groups = a.groups[0] + a.groups[1];
     int err = 0;
     if (groups > 0) {
-        hipLaunchKernelGGL((a.interleaved ? rope_bwd_kernel<T, D, true> : rope_bwd_kernel<T, D, false>), dim3((unsigned)groups), dim3(256), 0, a.stream, a);
+        const bool stream = rope_streams(3 * tokens * (a.heads[0] + a.heads[1]) * D * (long long)sizeof(T));
+        const auto kernel = stream ? (a.interleaved ? rope_bwd_kernel<T, D, true, true> : rope_bwd_kernel<T, D, false, true>)
+                                   : (a.interleaved ? rope_bwd_kernel<T, D, true, false> : rope_bwd_kernel<T, D, false, false>);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, a.stream, a);
         err = (int)hipGetLastError();
     }
     if (err != 0 || (dqw == nullptr && dkw == nullptr)) return err;
-    hipLaunchKernelGGL((rope_bwd_sum_kernel<T>), dim3(D / 4, 2), dim3(256), 0, a.stream, (const float *)a.partial, a.bwd_groups[0], a.bwd_groups[1], D, dqw,
+    hipLaunchKernelGGL((rope_bwd_sum_kernel<T>), dim3(D / 4, 2), dim3(256), 0, a.stream, (const float *)a.partial, a.groups[0], a.groups[1], D, dqw,
                        dkw, a.weight32);
     return (int)hipGetLastError();
 }
