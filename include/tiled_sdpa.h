@@ -279,7 +279,8 @@ int tiled_sdpa_fwd_paged(const void *q, const void *k_pages, const void *v_pages
  *
  * A token that sees no key gets O = 0 and LSE = -infinity.  Values of keys that a token does not see do not reach it, whatever they
  * are: rows of k or v of other tokens may hold infinities and NaN.  T <= 65536; everything else as for the two calls named
- * (the tile is the library's choice; split counts and workspace as for grouped heads there).
+ * (the tile is the library's choice).  With splits = 0 and a workspace of tiled_sdpa_kv_workspace_bytes(B, H, T, D, n), n being what
+ * tiled_sdpa_tree_default_splits reports (Skv: the capacity), the call takes the form that runs best; with less, what runs best in that.
  */
 int tiled_sdpa_fwd_tree(const void *q, const void *k, const void *v, void *o, float *lse, const int *kv_lens,
                         const long long *mask, long long mask_batch, int B, int H, int Hkv, int T, int Skv, int D,
@@ -288,6 +289,8 @@ int tiled_sdpa_fwd_tree_paged(const void *q, const void *k_pages, const void *v_
                               const int *kv_lens, const int *block_table, const long long *mask, long long mask_batch,
                               int B, int H, int Hkv, int T, int max_blocks, int block_rows, int D,
                               float scale, int dtype, void *stream, int splits, void *workspace, unsigned long long workspace_bytes);
+
+int tiled_sdpa_tree_default_splits(int B, int H, int Hkv, int T, int Skv, int D, int dtype, int *splits);
 
 /* Splits the heuristic picks (1 when the query tiles alone fill the GPU); returns a status code. */
 int tiled_sdpa_kv_default_splits(int B, int H, int Sq, int Skv, int D, int dtype, unsigned flags, int *splits);

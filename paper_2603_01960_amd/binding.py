@@ -41,6 +41,7 @@ EXPORTS = (
     "tiled_sdpa_fwd_paged",
     "tiled_sdpa_fwd_tree",
     "tiled_sdpa_fwd_tree_paged",
+    "tiled_sdpa_tree_default_splits",
     "tiled_sdpa_tree_mask",
     "tiled_sdpa_cache_step",
     "tiled_sdpa_qk_norm_rope",
@@ -130,6 +131,8 @@ def load_library():
     lib.tiled_sdpa_fwd_tree.argtypes = [vp] * 7 + [ctypes.c_longlong] + [ci] * 6 + [cf, ci, vp, ci, vp, ctypes.c_ulonglong]
     lib.tiled_sdpa_fwd_tree_paged.restype = ci
     lib.tiled_sdpa_fwd_tree_paged.argtypes = [vp] * 8 + [ctypes.c_longlong] + [ci] * 7 + [cf, ci, vp, ci, vp, ctypes.c_ulonglong]
+    lib.tiled_sdpa_tree_default_splits.restype = ci
+    lib.tiled_sdpa_tree_default_splits.argtypes = [ci] * 7 + [ctypes.POINTER(ci)]
     lib.tiled_sdpa_tree_mask.restype = ci
     lib.tiled_sdpa_tree_mask.argtypes = [vp] * 3 + [ci, ci, vp]
     lib.tiled_sdpa_cache_step.restype = ci

@@ -293,6 +293,30 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // query tile fastest, then split, then head: neighbours share one run of K/V tiles.  Under the causal mask the work
     // of a query tile grows with its index, and the long ones of all heads are started first (causal_tile).
     int hs, qt;
+    if constexpr (TREE) {
+        // The query tiles of a run of keys next to each other on one XCD; the runs dealt over the XCDs, those of the longest entries first,
+        // so that no XCD and no CU has more of them than another (and of up to two workgroups per CU, where all start at once, the
+        // second ones in reverse: the longest beside the shortest).
+        const int runs = N / nQ, whole = runs & ~7, x = blockIdx.x & 7, y = blockIdx.x >> 3;
+        const int left = (int)blockIdx.x - whole * nQ;            // >= 0: the runs that do not fill all XCDs
+        const int r = divide(left < 0 ? y : left, order.by_tiles);
+        int u = left < 0 ? x + 8 * r : whole + r;
+        qt = (left < 0 ? y : left) - r * nQ;
+        hs = u;
+        if (kv_lens != nullptr && batches > 1 && batches <= 64 && N > 256) {
+            if (N <= 512 && u >= 256 / nQ) u = runs + 256 / nQ - 1 - u;
+            const int per = heads_per_batch * splits;
+            const int mine = lane < batches ? kv_lens[lane] : -1;
+            int rank = 0;
+            for (int j = 0; j < batches; ++j) {
+                const int other = __builtin_amdgcn_readlane(mine, j);
+                rank += other > mine || (other == mine && j < lane) ? 1 : 0;
+            }
+            const int want = u / per;
+            const int entry = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == want && lane < batches));
+            hs = entry * per + (u - want * per);
+        }
+    } else
     if (causal && !linear_grid && order.heads > 0) {
         const CausalTile ct = causal_tile(blockIdx.x, nQ, order, N);
         hs = ct.head;
@@ -312,7 +336,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // every entry (head by head, the XCD with the longest entry finishes last).  Not with one query tile per head, where nobody
     // shares a head's keys: BF16, 32 entries of 16 heads, 64 queries, 410 ... 4096 keys in pages, 126 us head by head, 133 dealt
     // (with 16 tiles per head, 4 entries of 8 heads, 4096 ... 8192 keys, 217 / 187).
-    if (KV && kv_lens != nullptr && nQ > 1) {
+    if (KV && !TREE && kv_lens != nullptr && nQ > 1) {
         const int h = divide(head, by_batches);
         head = (head - h * batches) * heads_per_batch + h;
     }

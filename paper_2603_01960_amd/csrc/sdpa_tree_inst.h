@@ -1,5 +1,5 @@
 // Instantiates the forward kernel for trees of drafted tokens over a cache (KV = 5, 6) for one (element type, head dim): the
-// forms that pick_streams_kv and pick_tile_kv (tiled_sdpa.hip) choose, with one K/V tile height per head dim in the plain form.
+// forms that pick_tree and, up to 32 rows, pick_streams_kv (tiled_sdpa.hip) choose.
 #pragma once
 #include "sdpa_fwd_inst.h"
 
@@ -10,8 +10,8 @@ constexpr int tree_tile_n(int D) { return D == 160 ? 32 : 64; }
 template <typename T, int D> int launch_tree_plain(int tile_m, const LaunchArgs &a)
 {
     constexpr int TN = tree_tile_n(D);
-    if (a.block_table != nullptr) return tile_m == 64 ? launch_one<T, D, 2, TN, 6>(a) : launch_one<T, D, 4, TN, 6>(a);
-    return tile_m == 64 ? launch_one<T, D, 2, TN, 5>(a) : launch_one<T, D, 4, TN, 5>(a);
+    if (tile_m != 128) return (int)hipErrorInvalidValue;
+    return a.block_table ? launch_one<T, D, 4, TN, 6>(a) : launch_one<T, D, 4, TN, 5>(a);
 }
 
 template <typename T, int D, int KV> int launch_tree_streams(int tile_m, const LaunchArgs &a)
@@ -19,12 +19,6 @@ template <typename T, int D, int KV> int launch_tree_streams(int tile_m, const L
     switch (tile_m * 10 + a.streams) {
         case 324: return launch_one<T, D, 1, 32, KV, 4>(a);
         case 642: return launch_one<T, D, 2, 32, KV, 2>(a);
-        case 643:
-            if constexpr (D == 160) return launch_one<T, D, 2, 32, KV, 3>(a);
-            break;
-        case 644:
-            if constexpr (D < 160) return launch_one<T, D, 2, 32, KV, 4>(a);
-            break;
     }
     return (int)hipErrorInvalidValue;
 }

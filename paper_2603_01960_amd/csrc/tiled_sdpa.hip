@@ -318,6 +318,49 @@ int default_splits(int BH, int rows, int Skv, int D, bool fewest = false)
     return pick_splits(BH, rows, Skv, D, tm, tn, fewest);
 }
 
+// Trees of drafted tokens with more than 32 rows per key/value head: 32 or 64 rows in four or two streams, or 128 rows on 64-row K/V tiles
+// (32-row ones at D = 160), and the split count, whichever is the least by a model of the time in us,
+//     start + rounds * (prologue + steps * (q0 + q1 * D / 128)) + (splits > 1: merge + states in MB * byte),
+// steps of 32 keys per stream; a round is as many workgroups as the GPU holds, a last one that is not half full counts as `alone`.  The
+// constants are fits to 90 shapes (1 ... 64 entries, 36 ... 1600 rows per head, 256 ... 32256 keys, lengths from all, half and a tenth
+// of the capacity on; BF16), each timed in every form at up to 11 split counts.  Mean time over them, the best form and count of each
+// being 1: this 1.04, the rule for blocks of queries without a tree (pick_streams_kv, default_splits) 1.11; us, that rule / this:
+// 8 heads of 256 rows, 8192 keys D = 128 26.9 / 24.6; 128 of 64, 4096 keys D = 64 43 / 33; 256 of 60 rows, 2048 ... 8192 keys D = 128 in
+// pages 159 / 141; 133 of 184, 1408 keys D = 96 39 / 32.  (64 rows in four streams, 64 rows on 64-row tiles and 128 in two streams were
+// the best by 1 % on average, and are not built.  32 rows beyond two workgroups per CU: what they read of the keys is then too much for
+// the L2.)
+struct TreeForm { int rows, streams, splits; };
+TreeForm pick_tree(int heads, int rows, int Skv, int D, int splits, unsigned long long workspace)
+{
+    struct Cost { int rows, streams; double start, prologue, q0, q1, alone, merge, byte; };
+    static const Cost costs[] = {{32, 4, 4.6, 3.4, 0.16, 0.61, 0.94, 1.1, 0.77},
+                                 {64, 2, 6.9, 0.2, 0.20, 0.77, 0.83, 1.3, 0.66},
+                                 {128, 1, 8.2, 2.2, 0.03, 0.70, 0.71, 0.9, 0.44}};
+    TreeForm best{64, 2, splits > 0 ? splits : 1};
+    double least = -1.0;
+    for (const Cost &c : costs) {
+        const int64_t tiles = (int64_t)heads * ((rows + c.rows - 1) / c.rows);
+        const int64_t held = c.rows == 32 && D > 64 ? 256 : 512;      // (four streams' tiles: the LDS of a CU from D = 96 on)
+        if (c.rows == 128 && rows <= 64) continue;
+        for (int n = splits > 0 ? splits : 1; n <= (splits > 0 ? splits : 64); ++n) {
+            const int64_t grid = tiles * n;
+            if (splits == 0 && n > 1 && (grid > 1100 || Skv / n < 128)) break;
+            if (splits == 0 && c.rows == 32 && grid > 512) break;
+            const double states = n > 1 ? (double)heads * rows * n * (D + 2) * sizeof(float) : 0.0;
+            if (splits == 0 && states > (double)workspace) break;
+            const int64_t rest = grid % held;
+            const double rounds = (double)(grid / held) + (2 * rest > held ? 1.0 : rest > 0 ? c.alone : 0.0);
+            const double steps = Skv / (32.0 * c.streams * n);
+            const double cost = c.start + rounds * (c.prologue + steps * (c.q0 + c.q1 * D / 128)) + (n > 1 ? c.merge + states * 1e-6 * c.byte : 0.0);
+            if (least < 0.0 || cost < least) {
+                best = TreeForm{c.rows, c.streams, n};
+                least = cost;
+            }
+        }
+    }
+    return best;
+}
+
 int validate_shape_kv(int B, int H, int Sq, int Skv, int D, int dtype, unsigned flags)
 {
     if (dtype != TSDPA_F16 && dtype != TSDPA_BF16) return TSDPA_ERR_BAD_DTYPE;
@@ -647,6 +690,20 @@ static int check_tree(int B, int H, int T, const long long *mask, long long mask
     return ((uintptr_t)mask & 7u) != 0 ? TSDPA_ERR_MISALIGNED : TSDPA_OK;
 }
 
+int tiled_sdpa_tree_default_splits(int B, int H, int Hkv, int T, int Skv, int D, int dtype, int *splits)
+{
+    if (!splits) return TSDPA_ERR_NULL_PTR;
+    const int st = validate_shape_kv(B, H, T, Skv, D, dtype, 0);
+    if (st != TSDPA_OK) return st;
+    if (Hkv < 0 || (H > 0 && (Hkv == 0 || H % Hkv != 0))) return TSDPA_ERR_BAD_SHAPE;
+    *splits = 1;
+    if ((int64_t)B * H * T == 0) return TSDPA_OK;
+    const int64_t rows = (int64_t)(H / Hkv) * T;
+    if (rows > (int64_t)std::numeric_limits<int>::max()) return TSDPA_ERR_BAD_SHAPE;
+    *splits = rows > kDecodeRows ? pick_tree(B * Hkv, (int)rows, Skv, D, 0, ~0ull).splits : default_splits(B * Hkv, (int)rows, Skv, D);
+    return TSDPA_OK;
+}
+
 int tiled_sdpa_fwd_tree(const void *q, const void *k, const void *v, void *o, float *lse, const int *kv_lens,
                         const long long *mask, long long mask_batch, int B, int H, int Hkv, int T, int Skv, int D,
                         float scale, int dtype, void *stream, int splits, void *workspace, unsigned long long workspace_bytes)
@@ -704,7 +761,12 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
     if (std::isnan(scale)) scale = 1.0f / std::sqrt((float)D);
     if (std::isinf(scale)) return TSDPA_ERR_BAD_SCALE;
     if (splits < 0 || splits > TSDPA_MAX_SPLITS) return TSDPA_ERR_BAD_SPLITS;
-    if (splits == 0) {
+    const bool wide_tree = tree.mask && rows > kDecodeRows;
+    TreeForm form{};
+    if (wide_tree) {
+        form = pick_tree(B * Hkv, rows, Skv, D, splits, workspace ? workspace_bytes : 0);
+        splits = form.splits;
+    } else if (splits == 0) {
         splits = default_splits(B * Hkv, rows, Skv, D);
         if (!heuristic_tile) {
             // the tile's own count, unless the workspace holds the states of the default count only (a caller may have sized it by
@@ -752,7 +814,7 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
     a.block_table = block_table;
     a.max_blocks = max_blocks;
     a.block_shift = block_shift;
-    a.tile_rot = (block_table == nullptr && rows <= tile_m) ? 1 : 0;    // one query tile per head: see the kernel
+    a.tile_rot = (block_table == nullptr && rows <= (wide_tree ? form.rows : tile_m)) ? 1 : 0;    // one query tile per head: see the kernel
     a.c = std::fabs(scale) * 1.44269504088896340736f;
     a.tau = (flags & TSDPA_FLAG_EXACT_MAX) ? 0.0f : 8.0f;
     a.qsign = std::signbit(scale) && scale != 0.0f ? 0x80008000u : 0u;
@@ -768,7 +830,10 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
     a.stream = (hipStream_t)stream;
 
     int err;
-    if (heuristic_tile) {
+    if (wide_tree) {
+        tile_m = form.rows;
+        a.streams = form.streams;
+    } else if (heuristic_tile) {
         int rows_per_wg;
         a.streams = pick_streams_kv((long long)B * Hkv, rows, Skv, D, &rows_per_wg);
         if (a.streams > 1) {

@@ -540,7 +540,7 @@ PyObject *call_sdpa_tree(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (with_lse) lse = empty(s.slice(0, 3), at::kFloat, q);
         const bool heuristic = splits == 0;
         if (heuristic) {
-            const int st = heuristic_splits(B, H, Hkv, T, cap > 1 || !paged ? (int)cap : 1, D, dtype, 0, false, Tile{}, &splits);
+            const int st = tiled_sdpa_tree_default_splits(B, H, Hkv, T, (int)cap, D, dtype, &splits);
             if (st != TSDPA_OK) return PyLong_FromLong(st);
         }
         const Workspace ws(args[10], tiled_sdpa_kv_workspace_bytes(B, H, T, D, splits), q);
