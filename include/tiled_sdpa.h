@@ -416,7 +416,7 @@ int tiled_sdpa_cache_step(const int *kv_lens, const int *counts, const int *dept
                           int B, int S, int max_blocks, int block_rows, int pool_size, void *stream);
 
 /* Rows of D values of [B, S, heads, D], strides in elements: a projection's output, or a view into a packed one.  data is 16-byte
- * aligned, the values of a row are adjacent, the strides are multiples of 8. */
+ * aligned, the values of a row are adjacent, the strides are multiples of 8 (that of a dimension of one or none is not looked at). */
 typedef struct {
     void *data;
     long long batch, row, head;

@@ -29,9 +29,10 @@ bool misaligned(const void *at, uintptr_t bytes) { return ((uintptr_t)at & (byte
 // A row's strides: what a 16-byte load needs, and (for rows that are written) no two of them in one place.
 bool bad_strides(const tsdpa_rows &r, int B, int S, int heads, int D, bool written)
 {
-    if (r.batch < 0 || r.row < 0 || r.head < 0 || ((r.batch | r.row | r.head) & 7) != 0) return true;
-    if (!written) return false;
     struct Dim { long long stride; int size; } d[3] = {{r.batch, B}, {r.row, S}, {r.head, heads}};
+    for (const Dim &x : d)
+        if (x.size > 1 && (x.stride < 0 || (x.stride & 7) != 0)) return true;      // (one row has no stride)
+    if (!written) return false;
     for (int i = 0; i < 2; ++i)
         for (int j = 0; j < 2 - i; ++j)
             if (d[j].stride > d[j + 1].stride) {

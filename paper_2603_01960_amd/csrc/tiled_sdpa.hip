@@ -779,6 +779,7 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
         if (tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, splits) > given) {
             const int few = heuristic_tile ? default_splits(B * Hkv, rows, Skv, D, true) : pick_splits(B * Hkv, rows, Skv, D, tile_m, tile_n, true);
             if (tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, few) <= given) splits = few;
+            else if (tree.mask) splits = 1;
         }
     }
     // Long query blocks against a dense cache of one length, no mask, no split: the 256-row query tile of the

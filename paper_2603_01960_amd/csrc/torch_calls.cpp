@@ -608,6 +608,26 @@ template <int N> struct Given {
     }
 };
 
+// New tensors that share one allocation, each at a multiple of 64 bytes of it (four allocations of a few bytes take 2.5 us, more than the
+// kernel that fills them).
+class Carver {
+    c10::Storage storage;
+    int64_t at = 0;
+
+public:
+    static int64_t room(int64_t count, int64_t size) { return (count * size + 63) / 64 * 64; }
+    Carver(int64_t bytes, const at::Tensor &like) : storage(empty({bytes}, at::kByte, like).storage()) {}
+    at::Tensor next(at::IntArrayRef shape, at::ScalarType type)
+    {
+        at::Tensor t = at::detail::make_tensor<at::TensorImpl>(c10::Storage(storage), c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(type));
+        const int64_t size = c10::elementSize(type);
+        t.unsafeGetTensorImpl()->set_storage_offset(at / size);
+        t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+        at += room(t.numel(), size);
+        return t;
+    }
+};
+
 // An output of the caller's, or a new tensor.
 at::Tensor made(const at::Tensor &t, at::IntArrayRef shape, at::ScalarType type, const at::Tensor &like, const char *complaint)
 {
@@ -626,12 +646,20 @@ PyObject *call_tree_mask(PyObject *, PyObject *const *args, Py_ssize_t n)
             fail("parents must be contiguous int32 [T] or [B, T]");
         const at::IntArrayRef s = parents.sizes();
         const int64_t T = s[s.size() - 1], B = s.size() == 2 ? s[0] : 1;
-        if (T > std::numeric_limits<int>::max() || B > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        if (T > 1024 || B > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
         const int64_t words[3] = {B, T, (T + 63) / 64};
         const at::IntArrayRef shape(s.size() == 2 ? words : words + 1, s.size() + 1);
         static const char text[] = "out must be (mask, depths): contiguous int64 [..., T, ceil(T / 64)] and int32 [..., T] on the device of parents";
-        const Given<2> given(args[1], text);
-        const at::Tensor mask = made(given.t[0], shape, at::kLong, parents, text), depths = made(given.t[1], s, at::kInt, parents, text);
+        at::Tensor mask, depths;
+        if (args[1] == Py_None) {
+            Carver carve(Carver::room(B * T * words[2], 8) + Carver::room(B * T, 4), parents);
+            mask = carve.next(shape, at::kLong);
+            depths = carve.next(s, at::kInt);
+        } else {
+            const Given<2> given(args[1], text);
+            mask = made(given.t[0], shape, at::kLong, parents, text);
+            depths = made(given.t[1], s, at::kInt, parents, text);
+        }
         const Launch on(parents);
         const int st = without_gil(tiled_sdpa_tree_mask, (const int *)data(parents), (long long *)data(mask), (int *)data(depths), (int)B, (int)T, on.stream);
         return tuple_of(st, {&mask, &depths});
@@ -650,6 +678,7 @@ PyObject *call_cache_step(PyObject *, PyObject *const *args, Py_ssize_t n)
         const int S = as_int(args[2]), block_rows = as_int(args[3]);
         if (S < 0) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
         const int64_t B = lens.size(0);
+        if (B * S > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
         int *table = nullptr, *free_pages = nullptr;
         const int *pool = nullptr;
         int64_t max_blocks = 0, pool_size = 0;
@@ -680,9 +709,20 @@ PyObject *call_cache_step(PyObject *, PyObject *const *args, Py_ssize_t n)
         const int *depths = nullptr;
         if (args[5] != Py_None) depths = int_data(args[5], {B, S}, device, "depths must be contiguous int32 [B, S] on the device of kv_lens");
         static const char text[] = "out must be (new_lens, slots, positions, new_pool): contiguous int32 [B], [B, S], [B, S] and [2] on the device of kv_lens";
-        const Given<4> given(args[6], text);
-        const at::Tensor new_lens = made(given.t[0], lens.sizes(), at::kInt, lens, text), slots = made(given.t[1], {B, S}, at::kInt, lens, text),
-                         positions = made(given.t[2], {B, S}, at::kInt, lens, text), new_pool = made(given.t[3], {2}, at::kInt, lens, text);
+        at::Tensor new_lens, slots, positions, new_pool;
+        if (args[6] == Py_None) {
+            Carver carve(2 * Carver::room(B * S, 4) + Carver::room(B, 4) + Carver::room(2, 4), lens);
+            new_lens = carve.next(lens.sizes(), at::kInt);
+            slots = carve.next({B, S}, at::kInt);
+            positions = carve.next({B, S}, at::kInt);
+            new_pool = carve.next({2}, at::kInt);
+        } else {
+            const Given<4> given(args[6], text);
+            new_lens = made(given.t[0], lens.sizes(), at::kInt, lens, text);
+            slots = made(given.t[1], {B, S}, at::kInt, lens, text);
+            positions = made(given.t[2], {B, S}, at::kInt, lens, text);
+            new_pool = made(given.t[3], {2}, at::kInt, lens, text);
+        }
         if ((B > 0 && data(new_lens) == data(lens)) || data(new_pool) == (const void *)pool) fail("new_lens and new_pool must be other tensors than kv_lens and pool");
         if (B > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
         const Launch on(lens);

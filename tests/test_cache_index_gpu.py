@@ -42,6 +42,9 @@ def test_tree_mask(lib, T):
     one_mask, one_depths = lib.tree_mask(i32(parents[2]))
     assert one_mask.shape == (T, (T + 63) // 64) and torch.equal(one_mask, mask[2]) and torch.equal(one_depths, depths[2])
     out = torch.empty_like(mask), torch.empty_like(depths)
+    mask.fill_(-1)                               # (the results of a call do not overlap)
+    assert bool((depths == lib.tree_mask(i32(parents))[1]).all())
+    mask = lib.tree_mask(i32(parents))[0]
     got = lib.tree_mask(i32(parents), out=out)
     assert got[0] is out[0] and got[1] is out[1] and torch.equal(out[0], mask)
 
@@ -116,6 +119,15 @@ def test_dropping_what_was_appended_restores_the_pool(lib):
     assert pool.free[:pool.have] == free[:pool.have]
     first = pool.gpu[1].clone()
     assert pool.step(counts, 70) == 0 and torch.equal(first, pool.gpu[1])
+
+
+def test_the_results_of_a_call_do_not_overlap(lib):
+    got = lib.cache_step(i32([3, 4, 5]), i32([7, 0, 2]), 7, 64)
+    want = [x.clone() for x in got]
+    for i, x in enumerate(got):
+        x.fill_(77)
+        assert all(torch.equal(a, b) for a, b in zip(got[i + 1:], want[i + 1:]))
+        assert bool((x == 77).all())
 
 
 def test_refused_steps_change_nothing(lib):

@@ -83,6 +83,20 @@ def test_strides_outputs_and_one_weight(lib):
         check_forward(lib, q, k, qw, kw, pos, f, None, False, 1e-6, got)
 
 
+def test_a_dimension_of_one_has_no_stride(lib):
+    """One entry of rows that are not a multiple of 8 apart, one token, one head."""
+    x = torch.randn(64 * 9 + 40, device="cuda").to(torch.float16)
+    f = torch.rand(32, device="cuda")
+    for shape, stride, S in (((1, 3, 2, 64), (13, 192, 64), 3), ((2, 1, 2, 64), (128, 5, 64), 1), ((2, 3, 1, 64), (192, 64, 3), 3)):
+        q = x.as_strided(shape, (*stride, 1))
+        pos = torch.arange(S, dtype=torch.int32, device="cuda")
+        got, want = lib.qk_norm_rope(q, q, None, None, pos, f), lib.qk_norm_rope(q.contiguous(), q.contiguous(), None, None, pos, f)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        dq = [torch.zeros_like(x).as_strided(shape, (*stride, 1)) for _ in range(2)]
+        lib.qk_norm_rope_backward(*got, q, q, None, None, pos, f, grads=dq)
+        assert torch.equal(dq[0], dq[1]) and float((dq[0] - q).abs().max()) < 1e-2
+
+
 def test_far_positions_and_negative_ones(lib):
     """Angles of positions around 2^31: 64 bits of them are needed before a turn's fraction is left."""
     for far in (2 ** 31 - 5001, -2 ** 31, 10 ** 6):

@@ -139,6 +139,22 @@ def test_infinities_and_nan_of_tokens_that_a_token_does_not_see(lib, H, Hkv, T, 
         assert bool((got[:, :, blind, 0] == -math.inf).all()) and bool(torch.isnan(got[:, :, ~blind, 0]).all())
 
 
+@pytest.mark.parametrize("H,Hkv,T,n,D", [(8, 2, 3, 3000, 128), (8, 8, 20, 4000, 64), (16, 2, 30, 6000, 96)])
+def test_any_workspace_serves(lib, H, Hkv, T, n, D):
+    """The size that is reported, less, and next to nothing; a split count that needs more is refused."""
+    q, k, v = inputs(1, H, Hkv, T, n, D, torch.float16, T)
+    tree = a_tree(T, random.Random(T))
+    mask, _ = lib.tree_mask(i32([tree]))
+    want = lib.sdpa_tree(q, k, v, mask)
+    for nbytes in (1 << 26, 300000, 16):
+        o, lse = lib.sdpa_tree(q, k, v, mask, workspace=torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda"), return_lse=True)
+        check(lib, q, k, v, [n], [ref.ancestors(tree)[0]], o, lse)
+        if nbytes == 1 << 26:
+            assert torch.equal(o, want)
+    with pytest.raises(lib.TiledSdpaError):
+        lib.sdpa_tree(q, k, v, mask, splits=8, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+
+
 def test_a_chain_is_the_causal_mask(lib):
     """A tree that is a chain sees what the last positions of a sequence see."""
     for H, Hkv, T, n, D in ((8, 2, 8, 900, 128), (4, 4, 64, 700, 64), (2, 1, 150, 400, 96)):
