@@ -22,34 +22,37 @@ __global__ void __launch_bounds__(kMostNodes)
 tree_mask_kernel(const int *__restrict__ parents, unsigned long long *__restrict__ mask, int *__restrict__ depths, int T, int words)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    // (two of each: a round writes what the next but one overwrites, so that one barrier per round is enough)
+    // (two of each: a round writes what the next but one overwrites, so that one barrier per round is enough; and three flags: the one
+    // that a round clears for the next was last read in front of the barrier before)
     __shared__ unsigned long long set_sh[2][kMostNodes];
-    __shared__ int above_sh[2][kMostNodes], steps_sh[2][kMostNodes], more_sh[2][kMostNodes / 64];
-    const int entry = blockIdx.x, word = blockIdx.y, node = threadIdx.x, waves = blockDim.x >> 6;
-    int above = -1, steps = 0;
+    __shared__ int chain_sh[2][kMostNodes], more_sh[3];
+    const int entry = blockIdx.x, word = blockIdx.y, node = threadIdx.x;
+    // steps to the ancestor that the node has reached, and that ancestor + 1 (0: it has reached a root) in the low half
+    int chain = 0;
     unsigned long long set = 0;
     if (node < T) {
         const int p = parents[(size_t)entry * T + node];
-        above = p >= 0 && p < node ? p : -1;
-        steps = above >= 0 ? 1 : 0;
+        if (p >= 0 && p < node) chain = 1 << 16 | (p + 1);
         if (node >> 6 == word) set = 1ull << (node & 63);
     }
-    for (int turn = 0;; turn ^= 1) {
-        set_sh[turn][node] = set;
-        above_sh[turn][node] = above;
-        steps_sh[turn][node] = steps;
-        if ((node & 63) == 0) more_sh[turn][node >> 6] = 0;
-        if (above >= 0) more_sh[turn][node >> 6] = 1;
+    if (node < 3) more_sh[node] = 0;
+    __syncthreads();
+    for (int round = 0, flag = 0;; round ^= 1) {
+        const int next = flag == 2 ? 0 : flag + 1;
+        set_sh[round][node] = set;
+        chain_sh[round][node] = chain;
+        if ((chain & 0xffff) != 0) more_sh[flag] = 1;
+        if (node == 0) more_sh[next] = 0;
         __syncthreads();
-        int more = 0;
-        for (int w = 0; w < waves; ++w) more |= more_sh[turn][w];
-        if (!more) break;                          // (the same in every thread; `above` falls in every round)
-        if (above >= 0) {
-            set |= set_sh[turn][above];
-            steps += steps_sh[turn][above];
-            above = above_sh[turn][above];
+        if (more_sh[flag] == 0) break;             // (the same in every thread; the ancestors reached fall in every round)
+        const int at = (chain & 0xffff) - 1;
+        if (at >= 0) {
+            set |= set_sh[round][at];
+            chain = (chain & ~0xffff) + chain_sh[round][at];
         }
+        flag = next;
     }
+    const int steps = chain >> 16;
     if (node >= T) return;
     mask[((size_t)entry * T + node) * words + word] = set;
     if (word == 0 && depths != nullptr) depths[(size_t)entry * T + node] = steps;
