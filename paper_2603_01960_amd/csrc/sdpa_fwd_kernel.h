@@ -210,8 +210,91 @@ template <typename T> struct NotFinite {
     }
 };
 
+// The operand reads of a 32-row tile and the wait for them, in one block of inline assembly each: for the streams of the trees, whose next
+// loads are on their way into the LDS meanwhile.  (Left to the compiler, which cannot tell the slots apart, a read waits for all of those.
+// One block, outputs early clobbers: see DecodeRead in sdpa_decode_kernel.h.)
+//   keys:   half of a row's 16-byte chunks (all of them at once are registers that spill): x[i] = 16 bytes at p[i] + AT
+//   values: x[db][half] = transposing read at p[db] + AT + half * 8 rows
+#define TSDPA_RD_K(i, a, n) "ds_read_b128 %" #i ", %" #a " offset:%" #n "\n\t"
+#define TSDPA_RD_V(i, a, n) "ds_read_b64_tr_b16 %" #i ", %" #a " offset:%" #n "\n\t"
+#define TSDPA_RD_WAIT "s_waitcnt lgkmcnt(0)"
+template <int D> struct StreamRead;
+template <> struct StreamRead<64> {
+    template <int AT> static __device__ __forceinline__ void keys(u32x4 (&x)[2], const uint32_t *p)
+    {
+        asm volatile(TSDPA_RD_K(0, 2, 4) TSDPA_RD_K(1, 3, 4) TSDPA_RD_WAIT
+                     : "=&v"(x[0]), "=&v"(x[1])
+                     : "v"(p[0]), "v"(p[1]), "n"(AT)
+                     : "memory");
+    }
+    template <int AT> static __device__ __forceinline__ void values(i16x4 (&x)[2][2], const uint32_t (&p)[2])
+    {
+        asm volatile(TSDPA_RD_V(0, 4, 6) TSDPA_RD_V(1, 4, 7) TSDPA_RD_V(2, 5, 6) TSDPA_RD_V(3, 5, 7) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
+                     : "v"(p[0]), "v"(p[1]), "n"(AT), "n"(AT + 1024)
+                     : "memory");
+    }
+};
+template <> struct StreamRead<96> {
+    template <int AT> static __device__ __forceinline__ void keys(u32x4 (&x)[3], const uint32_t *p)
+    {
+        asm volatile(TSDPA_RD_K(0, 3, 6) TSDPA_RD_K(1, 4, 6) TSDPA_RD_K(2, 5, 6) TSDPA_RD_WAIT
+                     : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "n"(AT)
+                     : "memory");
+    }
+    template <int AT> static __device__ __forceinline__ void values(i16x4 (&x)[3][2], const uint32_t (&p)[3])
+    {
+        asm volatile(TSDPA_RD_V(0, 6, 9) TSDPA_RD_V(1, 6, 10) TSDPA_RD_V(2, 7, 9) TSDPA_RD_V(3, 7, 10) TSDPA_RD_V(4, 8, 9) TSDPA_RD_V(5, 8, 10)
+                     TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "n"(AT), "n"(AT + 1536)
+                     : "memory");
+    }
+};
+template <> struct StreamRead<128> {
+    template <int AT> static __device__ __forceinline__ void keys(u32x4 (&x)[4], const uint32_t *p)
+    {
+        asm volatile(TSDPA_RD_K(0, 4, 8) TSDPA_RD_K(1, 5, 8) TSDPA_RD_K(2, 6, 8) TSDPA_RD_K(3, 7, 8) TSDPA_RD_WAIT
+                     : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT)
+                     : "memory");
+    }
+    template <int AT> static __device__ __forceinline__ void values(i16x4 (&x)[4][2], const uint32_t (&p)[4])
+    {
+        asm volatile(TSDPA_RD_V(0, 8, 12) TSDPA_RD_V(1, 8, 13) TSDPA_RD_V(2, 9, 12) TSDPA_RD_V(3, 9, 13) TSDPA_RD_V(4, 10, 12)
+                     TSDPA_RD_V(5, 10, 13) TSDPA_RD_V(6, 11, 12) TSDPA_RD_V(7, 11, 13) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[3][0]), "=&v"(x[3][1])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT), "n"(AT + 2048)
+                     : "memory");
+    }
+};
+template <> struct StreamRead<160> {
+    template <int AT> static __device__ __forceinline__ void keys(u32x4 (&x)[5], const uint32_t *p)
+    {
+        asm volatile(TSDPA_RD_K(0, 5, 10) TSDPA_RD_K(1, 6, 10) TSDPA_RD_K(2, 7, 10) TSDPA_RD_K(3, 8, 10) TSDPA_RD_K(4, 9, 10) TSDPA_RD_WAIT
+                     : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "n"(AT)
+                     : "memory");
+    }
+    template <int AT> static __device__ __forceinline__ void values(i16x4 (&x)[5][2], const uint32_t (&p)[5])
+    {
+        asm volatile(TSDPA_RD_V(0, 10, 15) TSDPA_RD_V(1, 10, 16) TSDPA_RD_V(2, 11, 15) TSDPA_RD_V(3, 11, 16) TSDPA_RD_V(4, 12, 15)
+                     TSDPA_RD_V(5, 12, 16) TSDPA_RD_V(6, 13, 15) TSDPA_RD_V(7, 13, 16) TSDPA_RD_V(8, 14, 15) TSDPA_RD_V(9, 14, 16) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[3][0]),
+                     "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "n"(AT), "n"(AT + 2560)
+                     : "memory");
+    }
+};
+#undef TSDPA_RD_K
+#undef TSDPA_RD_V
+#undef TSDPA_RD_WAIT
+
 // s_waitcnt vmcnt(0) with the other counters left at their maxima (gfx9 encoding)
 #define TSDPA_WAIT_VMCNT0() __builtin_amdgcn_s_waitcnt(0x0F70)
+// ... vmcnt(n), n < 64
+#define TSDPA_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(0x0F70 | ((n) & 15) | ((n) >> 4) << 14)
 
 // KV = false is the paper's problem: S query rows against the same S key rows, one workgroup per
 // (head, query tile), final output.  KV = true generalises it for the decoding shapes of the paper's
@@ -687,6 +770,27 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
         return (psum[0] + psum[1]) + (psum[2] + psum[3]);
     };
 
+    // trees, masked tiles: what is not finite in the fragment a of V (columns db * 32 ..., keys of block nb, half ks) goes to the rows that see
+    // it, and out of a
+    auto take_not_finite = [&](i16x8 &a, int db, int nb, int ks) __attribute__((always_inline)) {
+        const u32x4 raw = __builtin_bit_cast(u32x4, a);
+        if (__builtin_amdgcn_ballot_w64(NotFinite<T>::any(raw)) == 0) return;
+        u32x4 finite, up, down, seen;
+        NotFinite<T>::take_apart(raw, finite, up, down);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            seen[i] = (hidden(0, nb, ks * 8 + 2 * i) ? 0u : NotFinite<T>::ONE & 0xffffu) |
+                      (hidden(0, nb, ks * 8 + 2 * i + 1) ? 0u : NotFinite<T>::ONE & 0xffff0000u);
+        f32x16 zero;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+        const f32x16 ups = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), zero);
+        const f32x16 downs = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), zero);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[db][i] += NotFinite<T>::excess(ups[i], downs[i]);
+        a = __builtin_bit_cast(i16x8, finite);
+    };
+
     // Eq. 4: O^T += V^T P^T
     auto accumulate = [&](int vslot, const vec8 (&pb)[NB][2], auto mask_tag) __attribute__((always_inline)) {
 #pragma unroll
@@ -700,25 +804,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                     i16x4 lo = lds_read_tr16(p0);
                     i16x4 hi = lds_read_tr16(p0 + 8 * G::ROW);
                     i16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    if constexpr (TREE && decltype(mask_tag)::value) {
-                        const u32x4 raw = __builtin_bit_cast(u32x4, a);
-                        if (__builtin_amdgcn_ballot_w64(NotFinite<T>::any(raw)) != 0) {
-                            u32x4 finite, up, down, seen;
-                            NotFinite<T>::take_apart(raw, finite, up, down);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                seen[i] = (hidden(0, nb, ks * 8 + 2 * i) ? 0u : NotFinite<T>::ONE & 0xffffu) |
-                                          (hidden(0, nb, ks * 8 + 2 * i + 1) ? 0u : NotFinite<T>::ONE & 0xffff0000u);
-                            f32x16 zero;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) zero[i] = 0.f;
-                            const f32x16 ups = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), zero);
-                            const f32x16 downs = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), zero);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) oacc[db][i] += NotFinite<T>::excess(ups[i], downs[i]);
-                            a = __builtin_bit_cast(i16x8, finite);
-                        }
-                    }
+                    if constexpr (TREE && decltype(mask_tag)::value) take_not_finite(a, db, nb, ks);
                     oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), pb[nb][ks], oacc[db]);
                     if constexpr (HALVES) oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), ph[nb][ks], oacc[db]);
                 }
@@ -784,6 +870,99 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
             return;
         }
     }
+    // Trees, streams: a tile's K is requested when the K two tiles before it has been read, and its V likewise, so that each has one and a half
+    // steps to arrive instead of one (the slots are the same).  In step j: K(j) has landed; scores, V(j+1)'s loads between them; weights; V(j)
+    // has landed; products, K(j+2)'s loads between them.  Behind K(j) V(j) and K(j+1) may be on their way, behind V(j) K(j+1) and V(j+1): two
+    // tiles' worth of loads either way.  With several wavefronts to a stream a barrier follows each wait: the tile is there, and what was read
+    // before it may be overwritten.  (us: 64 rows in two streams, 4 entries of 8 heads, 4096 keys D = 128 27.1 -> 24.8; 32 entries of
+    // 2048 ... 8192 keys in pages, one split 187 -> 140, two 150 -> 139; 32 rows in four, which the L2 bounds, 1 entry, 8192 keys, 25.0 -> 24.3.)
+    constexpr bool AHEAD = TREE && NS > 1;
+    if constexpr (AHEAD) {
+        static_assert(TN == 32 && NSUB == 1 && U % NW == 0 && 2 * NLD < 64, "whole tiles, shared out evenly, counted in vmcnt");
+        uint32_t kp[KK], vp[DB];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kp[kk] = __builtin_bit_cast(uint32_t, k_rptr[kk]);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) vp[db] = __builtin_bit_cast(uint32_t, v_rptr[db]);
+        auto landed = [&]() __attribute__((always_inline)) {
+            asm volatile("" : : : "memory");      // (loads and reads stay on their side)
+            TSDPA_WAIT_VMCNT(2 * NLD);
+            if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+            asm volatile("" : : : "memory");
+        };
+        auto ahead_step = [&](int jj, auto par_tag, auto mask_tag) __attribute__((always_inline)) {
+            constexpr int PAR = decltype(par_tag)::value;
+            constexpr bool MASK = decltype(mask_tag)::value;
+            constexpr int KS = PAR ? KSLOT1 : KSLOT0, VS = PAR ? VSLOT1 : VSLOT0;
+            if constexpr (MASK) tree_words_of(jj * TN);
+            landed();
+            const TileSrc vsrc = tile_src(v, v_rsrc, jj + NS);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sacc[0][i] = 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                u32x4 kb[KK / 2];
+                StreamRead<D>::template keys<KS>(kb, kp + half * (KK / 2));
+#pragma unroll
+                for (int i2 = 0; i2 < KK / 2; ++i2) {
+                    const int kk = half * (KK / 2) + i2;
+                    sacc[0] = E::mfma(__builtin_bit_cast(vec8, kb[i2]), qf[kk], sacc[0]);
+#pragma unroll
+                    for (int i = kk * NLD / KK; i < (kk + 1) * NLD / KK; ++i) issue(vsrc, vsrc, lds, lds + (PAR ? VSLOT0 : VSLOT1), NLD + i);
+                    __builtin_amdgcn_sched_barrier(0x786);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+            if constexpr (MASK) tree_bits_of(jj * TN);
+            softmax_tile(jj * TN, mask_tag);
+            landed();
+            const TileSrc ksrc = tile_src(k, k_rsrc, jj + 2 * NS);
+            __builtin_amdgcn_s_setprio(2);
+            auto products = [&](auto ks_tag) __attribute__((always_inline)) {
+                constexpr int ks = decltype(ks_tag)::value;
+                i16x4 vf[DB][2];
+                StreamRead<D>::template values<VS + ks * 16 * G::ROW>(vf, vp);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    i16x8 a = __builtin_shufflevector(vf[db][0], vf[db][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    if constexpr (MASK) take_not_finite(a, db, 0, ks);
+                    oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), pb[0][ks], oacc[db]);
+                    constexpr int HOOKS = 2 * DB;
+                    const int h = ks * DB + db;
+#pragma unroll
+                    for (int i = h * NLD / HOOKS; i < (h + 1) * NLD / HOOKS; ++i) issue(ksrc, ksrc, lds + KS, lds, i);
+                    if constexpr (!MASK) __builtin_amdgcn_sched_barrier(0x786);
+                }
+            };
+            products(P0{});
+            products(P1{});
+            __builtin_amdgcn_s_setprio(0);
+        };
+        auto load_part_of = [&](const T *tensor, const decltype(k_rsrc) &whole, int jj, int slot, int first) __attribute__((always_inline)) {
+            const TileSrc src = tile_src(tensor, whole, jj);
+#pragma unroll
+            for (int i = 0; i < NLD; ++i) issue(src, src, lds + slot, lds + slot, first + i);
+        };
+        load_part_of(k, k_rsrc, s0, KSLOT0, 0);
+        load_part_of(v, v_rsrc, s0, VSLOT0, NLD);
+        load_part_of(k, k_rsrc, s0 + NS, KSLOT1, 0);
+        int jj = s0;
+        for (; jj < fast_end; jj += 2 * NS) {
+            ahead_step(jj, P0{}, std::false_type{});
+            ahead_step(jj + NS, P1{}, std::false_type{});
+        }
+        for (; jj < t1; jj += NS) {
+            if (((jj - s0) / NS) & 1) ahead_step(jj, P1{}, std::true_type{});
+            else                      ahead_step(jj, P0{}, std::true_type{});
+        }
+        if constexpr (NW > 1)
+            if ((t1 - s0 + NS - 1) / NS < (t1 - t0 + NS - 1) / NS) {
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_s_barrier();
+            }
+        TSDPA_WAIT_VMCNT0();                      // (nothing may still be on its way into the LDS)
+    } else {
     load_tiles(s0 + rot, lds + KSLOT0, lds + VSLOT0);
     TSDPA_WAIT_VMCNT0();
     if constexpr (NW > 1) __syncthreads();        // (a wavefront that streams alone waits for nobody)
@@ -865,6 +1044,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // (a stream has the others' number of tiles or one less)
     if constexpr (NS > 1 && NW > 1)
         if ((t1 - s0 + NS - 1) / NS < (t1 - t0 + NS - 1) / NS) __syncthreads();
+    }
     }
 
     // ---- O_i = o_i / l_i (Section 4.1.2), rounded once to the 16-bit output type.  The accumulators

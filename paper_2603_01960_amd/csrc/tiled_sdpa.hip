@@ -322,20 +322,19 @@ int default_splits(int BH, int rows, int Skv, int D, bool fewest = false)
 // (32-row ones at D = 160), and the split count, whichever is the least by a model of the time in us,
 //     start + rounds * (prologue + steps * (q0 + q1 * D / 128)) + (splits > 1: merge + states in MB * byte),
 // steps of 32 keys per stream; a round is as many workgroups as the GPU holds, a last one that is not half full counts as `alone`.  The
-// constants are fits to 90 shapes (1 ... 64 entries, 36 ... 1600 rows per head, 256 ... 32256 keys, lengths from all, half and a tenth
+// constants are fits to 110 shapes (1 ... 64 entries, 36 ... 1600 rows per head, 256 ... 32256 keys, lengths from all, half and a tenth
 // of the capacity on; BF16), each timed in every form at up to 11 split counts.  Mean time over them, the best form and count of each
-// being 1: this 1.04, the rule for blocks of queries without a tree (pick_streams_kv, default_splits) 1.11; us, that rule / this:
-// 8 heads of 256 rows, 8192 keys D = 128 26.9 / 24.6; 128 of 64, 4096 keys D = 64 43 / 33; 256 of 60 rows, 2048 ... 8192 keys D = 128 in
-// pages 159 / 141; 133 of 184, 1408 keys D = 96 39 / 32.  (64 rows in four streams, 64 rows on 64-row tiles and 128 in two streams were
-// the best by 1 % on average, and are not built.  32 rows beyond two workgroups per CU: what they read of the keys is then too much for
-// the L2.)
+// being 1: this 1.04, at most 1.40; of one form at its best count 32 rows 1.16, 64 rows 1.10, 128 rows (from 65 on) 1.19; of one split in
+// the best form 1.87.  us, 32 / 64 / 128 rows at the best counts: 8 heads of 256 rows, 8192 keys D = 128 24.3 / 23.0 / 28.1; 256 heads of 60 rows, 2048
+// ... 8192 keys in pages 159 / 139 / 153.  (64 rows in four streams, 128 in two: the best by 0.3 % on average, not built.  32 rows beyond
+// two workgroups per CU: what they read of the keys is then too much for the L2.)
 struct TreeForm { int rows, streams, splits; };
 TreeForm pick_tree(int heads, int rows, int Skv, int D, int splits, unsigned long long workspace)
 {
     struct Cost { int rows, streams; double start, prologue, q0, q1, alone, merge, byte; };
-    static const Cost costs[] = {{32, 4, 4.6, 3.4, 0.16, 0.61, 0.94, 1.1, 0.77},
-                                 {64, 2, 6.9, 0.2, 0.20, 0.77, 0.83, 1.3, 0.66},
-                                 {128, 1, 8.2, 2.2, 0.03, 0.70, 0.71, 0.9, 0.44}};
+    static const Cost costs[] = {{32, 4, 4.6, 3.6, 0.07, 0.66, 0.87, 0.95, 0.84},
+                                 {64, 2, 6.7, 1.4, 0.21, 0.68, 0.69, 0.92, 0.69},
+                                 {128, 1, 6.7, 2.6, 0.03, 0.74, 0.70, 1.45, 0.44}};
     TreeForm best{64, 2, splits > 0 ? splits : 1};
     double least = -1.0;
     for (const Cost &c : costs) {
