@@ -1,6 +1,6 @@
-// The tensor entry points of the Python package (sdpa, sdpa_kv, sdpa_paged, sdpa_backward, sdpa_tree, sdpa_tree_paged, and those around
-// attention: tree_mask, cache_step, qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward) in native code: argument checks, output and workspace tensors from torch's allocator, the current stream, and one call into the C-ABI of
-// include/tiled_sdpa.h.
+// The tensor entry points of the Python package (sdpa, sdpa_kv, sdpa_paged, sdpa_backward, sdpa_tree, sdpa_tree_paged, and those
+// around attention: tree_mask, cache_step, qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward) in native code: argument
+// checks, output and workspace tensors from torch's allocator, the current stream, and one call into the C-ABI of include/tiled_sdpa.h.
 //
 // Why native: a short call is bound by the host.  One forward call of a small problem (B=1 H=2 S=128 D=64, a kernel of
 // 4.4 us) took 8.7 us of host time through Python attribute reads, data_ptr() calls and ctypes argument conversion, a
@@ -636,6 +636,24 @@ at::Tensor made(const at::Tensor &t, at::IntArrayRef shape, at::ScalarType type,
     return t;
 }
 
+// Memory of a contiguous tensor.  Outputs that overlap what a kernel's other workgroups still read are refused.
+struct Extent {
+    const char *at;
+    int64_t bytes;
+    explicit Extent(const at::Tensor &t) : at((const char *)data(t)), bytes((int64_t)t.nbytes()) {}
+    Extent(const int *p, int64_t count) : at((const char *)p), bytes(p ? count * (int64_t)sizeof(int) : 0) {}
+    bool meets(const Extent &o) const { return bytes > 0 && o.bytes > 0 && at < o.at + o.bytes && o.at < at + bytes; }
+};
+void distinct(std::initializer_list<Extent> outputs, std::initializer_list<Extent> inputs, const char *complaint)
+{
+    for (const Extent *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Extent &i : inputs)
+            if (o->meets(i)) fail(complaint);
+        for (const Extent *other = outputs.begin(); other != o; ++other)
+            if (o->meets(*other)) fail(complaint);
+    }
+}
+
 // tree_mask(parents, out)
 PyObject *call_tree_mask(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -659,6 +677,7 @@ PyObject *call_tree_mask(PyObject *, PyObject *const *args, Py_ssize_t n)
             const Given<2> given(args[1], text);
             mask = made(given.t[0], shape, at::kLong, parents, text);
             depths = made(given.t[1], s, at::kInt, parents, text);
+            distinct({Extent(mask), Extent(depths)}, {Extent(parents)}, "mask, depths and parents must not overlap");
         }
         const Launch on(parents);
         const int st = without_gil(tiled_sdpa_tree_mask, (const int *)data(parents), (long long *)data(mask), (int *)data(depths), (int)B, (int)T, on.stream);
@@ -722,8 +741,10 @@ PyObject *call_cache_step(PyObject *, PyObject *const *args, Py_ssize_t n)
             slots = made(given.t[1], {B, S}, at::kInt, lens, text);
             positions = made(given.t[2], {B, S}, at::kInt, lens, text);
             new_pool = made(given.t[3], {2}, at::kInt, lens, text);
+            distinct({Extent(new_lens), Extent(slots), Extent(positions), Extent(new_pool)},
+                     {Extent(lens), Extent(counts, B), Extent(depths, B * S), Extent(table, B * max_blocks), Extent(free_pages, pool_size), Extent(pool, 2)},
+                     "new_lens, slots, positions and new_pool must be other tensors than each other and what the step reads (kv_lens and pool among it)");
         }
-        if ((B > 0 && data(new_lens) == data(lens)) || data(new_pool) == (const void *)pool) fail("new_lens and new_pool must be other tensors than kv_lens and pool");
         if (B > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
         const Launch on(lens);
         const int st = without_gil(tiled_sdpa_cache_step, (const int *)data(lens), counts, depths, table, free_pages, pool, (int *)data(new_lens), (int *)data(slots),

@@ -187,3 +187,23 @@ def test_cache_step_refusals(lib):
         lib.cache_step(lens, counts, 1, 0)
     with pytest.raises(lib.TiledSdpaError):
         lib.cache_step(lens, counts, -1, 64)
+
+
+def test_outputs_that_overlap_inputs_or_each_other_are_refused(lib):
+    both = i32([0] * 8)
+    parents, mask, depths = i32([[-1, 0]]), torch.zeros(1, 2, 1, dtype=torch.int64, device="cuda"), i32([[0, 0]])
+    for out in ((mask, parents), (mask, mask.view(torch.int32).view(-1)[2:].view(1, 2))):
+        with pytest.raises(ValueError, match="overlap"):
+            lib.tree_mask(parents, out=out)
+    lib.tree_mask(parents, out=(mask, depths))
+    lens, counts, table, free, pool = i32([3, 4]), i32([1, 1]), i32([[0], [1]]), i32([2, 3]), i32([2, 0])
+    good = [i32([0, 0]), i32([[0], [0]]), i32([[0], [0]]), i32([0, 0])]
+    for at, t in ((0, counts), (0, lens), (1, table), (1, both[:2].view(2, 1)), (2, free.view(2, 1)), (3, counts), (3, pool), (3, good[0])):
+        out = list(good)
+        out[at] = t
+        if t.data_ptr() == both.data_ptr():
+            out[2] = both[1:3].view(2, 1)
+        with pytest.raises(ValueError, match="other tensors"):
+            lib.cache_step(lens, counts, 1, 64, pages=(table, free, pool), out=out)
+    lib.cache_step(lens, counts, 1, 64, pages=(table, free, pool), out=good)
+    assert good[0].tolist() == [4, 5]
