@@ -14,6 +14,9 @@
  * The call surface mirrors the functional API of Section 4.2.1,
  * sdpa(q, k, v, causal, scale) -> o; causal = true is TSDPA_FLAG_CAUSAL of tiled_sdpa_fwd_ex.
  *
+ * Beside it: attention over dense and paged caches, of trees of drafted tokens, the backward pass; and what a serving or training step
+ * does around attention: the trees' masks, a cache's pages and slots, norm and rotation of queries and keys.
+ *
  * All pointers are DEVICE pointers owned by the caller.  The library allocates
  * and frees nothing, keeps no state besides its kernel table, never
  * synchronises, and is thread-safe.  Work is enqueued on `stream`.
@@ -377,6 +380,9 @@ unsigned long long tiled_sdpa_bwd_full_workspace_bytes(int B, int H, int Hkv, in
  *   depths  : NULL, or device int32 [B, T]: the number of ancestors: the token's distance from the first position behind the
  *             cached sequence (see tiled_sdpa_cache_step).
  *   T       : 0 ... 1024.
+ * In a batch of trees of several sizes a tree of n < T tokens takes the last n places, behind a chain (token i follows i - 1) of T - n
+ * that its first tokens follow: the chain stands for the last T - n rows of the cached sequence, which all tokens see.
+ * The outputs must not overlap parents.
  */
 int tiled_sdpa_tree_mask(const int *parents, long long *mask, int *depths, int B, int T, void *stream);
 
@@ -401,8 +407,8 @@ int tiled_sdpa_tree_mask(const int *parents, long long *mask, int *depths, int B
  *                  TSDPA_FLAG_CAUSAL are the last positions).
  *   positions    : device int32 [B, S]: the row's position (0 where there is no slot).
  *   new_pool     : device int32 [2]: pages free after the step, and 0; or, of a step that is REFUSED, the pages as they were and
- *                  what is missing: pages (dense: rows) that the pool or the ends of entries lack, -1 if a length, count or pool
- *                  cannot be one (negative, beyond the capacity, more than S).  A refused step changes nothing: new_lens =
+ *                  what is missing: pages (dense: rows) that the pool or the ends of entries lack (of one entry's end at most 65536
+ *                  are counted), -1 if a length, count or pool cannot be one (negative, beyond the capacity, more than S).  A refused step changes nothing: new_lens =
  *                  kv_lens, every slot -1.
  *
  * Pages go in this order: those given up (entry by entry) to those needed (entry by entry), then from the end of the pool; what is
@@ -446,7 +452,8 @@ typedef struct {
  * rotation of each pair (a, b) by its angle,
  *     y = x / sqrt(mean(x^2) + eps) * w,     (y_a cos - y_b sin, y_b cos + y_a sin),
  * and the layout.  FP32 throughout (angles in 64 bits up to whole turns: any position is as exact as the first), one rounding.  The mean
- * of squares is taken in FP32: BF16 values whose squares overflow it (beyond 1e18) have no norm.
+ * of squares is taken in FP32: rows of BF16 values whose squares overflow it (beyond 1e18) have no norm, nor, with eps = 0, rows
+ * whose squares all fall below it (1e-19).
  *
  *   q, k         : tsdpa_rows of [B, S, H, D] and [B, S, Hkv, D].
  *   q_out, k_out : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned: what tiled_sdpa_fwd and its kin read.  Must not
@@ -477,7 +484,7 @@ int tiled_sdpa_qk_norm_rope_cache(const tsdpa_rope *p, const tsdpa_rows *q, cons
  *
  *   dq_out, dk_out     : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned.
  *   q, k               : as for the forward call (without weights they are not looked at).
- *   dq, dk             : tsdpa_rows to be written, of the shapes of q and k; every element is overwritten.
+ *   dq, dk             : tsdpa_rows to be written, of the shapes of q and k; every element is overwritten.  Must not overlap the inputs.
  *   dq_weight, dk_weight : [D] in weight_dtype; not looked at (may be NULL) where there is no weight.
  *   workspace          : device, 16-byte aligned, at least tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(B, S, D) bytes; not looked at
  *                        without weights.  Calls that may overlap on the GPU need distinct ones.

@@ -288,3 +288,22 @@ def test_a_captured_verification_step(lib):
         assert int(after[3][1]) == 0
         mine[4].copy_(after[0])
         mine[5].copy_(after[3])
+
+
+def test_trees_of_several_sizes_in_one_batch(lib):
+    """Smaller trees take the last places behind a chain that stands for cached rows: each entry against its own tree alone."""
+    B, H, Hkv, T, cap, D = 5, 8, 2, 20, 400, 128
+    had, counts = [300, 40, 3, 64, 200], [20, 7, 2, 1, 0]
+    rng = random.Random(5)
+    own = [a_tree(c, rng) for c in counts]
+    parents = [[i - 1 for i in range(T - c)] + [T - c + p for p in tree] for tree, c in zip(own, counts)]      # (a root follows the chain's end, or nothing)
+    mask, depths = lib.tree_mask(i32(parents))
+    grown, slots, positions, _ = lib.cache_step(i32(had), i32(counts), T, cap, depths=depths)
+    for b, c in enumerate(counts):
+        assert positions[b].tolist() == [0] * (T - c) + [had[b] + d for d in ref.ancestors(own[b])[1]]
+        assert slots[b].tolist() == [-1] * (T - c) + [b * cap + had[b] + i for i in range(c)]
+    q, k, v = inputs(B, H, Hkv, T, cap, D, torch.bfloat16, 7)
+    o = lib.sdpa_tree(q, k, v, mask, kv_lens=grown)
+    for b, c in enumerate(counts):
+        if c > 0:
+            check(lib, q[b:b + 1, :, T - c:], k[b:b + 1], v[b:b + 1], [had[b] + c], [ref.ancestors(own[b])[0]], o[b:b + 1, :, T - c:])
