@@ -1053,7 +1053,103 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // XOR-swizzled by row against bank conflicts) and reads it back as whole rows, so that every global
     // store instruction writes complete, contiguous rows (16 B per lane) instead of 8-byte pieces.
     float l_tot = pair_sum(l_run);
-    if constexpr (NS > 1) {
+    constexpr bool SHARED = TREE && NS > 2;
+    if constexpr (SHARED) {
+        // ---- one state from the streams', each of which takes its share of the columns: the other streams' part of them through the LDS, combined,
+        // stored.  (us, one stream for all columns while the others wait, as below -> this: 8 entries of 40 rows and 8 heads, 512 keys D = 128
+        // 11.0 -> 9.8; 2 heads of 240 rows, 5000 keys D = 160 16.7 -> 15.8; 8 heads of 64 rows, 8192 keys D = 128 17.7 -> 17.2.  Of two streams
+        // 256 rows of 8192 keys 21.6 -> 21.8.)
+        constexpr int CH = DB * 4, SHARE = CH / NS;      // chunks of 8 columns (4 in a lane and 4 in lane ^ 32), of a stream
+        constexpr int PART = SHARE * 1024, STATS = NS * (NS - 1) * NW * PART;
+        static_assert(NS == 4 && CH % NS == 0 && STATS + NS * NW * 512 <= NS * G::LDS_BYTES, "[taker][giver among the others][wavefront] parts, then (m, l)");
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const lds_ptr base = (lds_ptr)smem + lane * 16, stats = (lds_ptr)smem + STATS + (wave * 64 + lane) * 8;
+        auto part_of = [&](int taker, int other) __attribute__((always_inline)) { return base + ((taker * (NS - 1) + other) * NW + wave) * PART; };
+        f32x4 own[SHARE];
+        __syncthreads();
+        auto give = [&](auto from_tag) __attribute__((always_inline)) {
+            constexpr int FROM = decltype(from_tag)::value;
+#pragma unroll
+            for (int ch = 0; ch < CH; ++ch) {
+                f32x4 part;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[e] = oacc[ch / 4][(ch % 4) * 4 + e];
+                if (ch / SHARE == FROM) own[ch % SHARE] = part;
+                else *(TSDPA_LDS f32x4 *)(part_of(ch / SHARE, FROM < ch / SHARE ? FROM : FROM - 1) + (ch % SHARE) * 1024) = part;
+            }
+        };
+        if (stream == 0) give(std::integral_constant<int, 0>{});
+        else if (stream == 1) give(std::integral_constant<int, 1>{});
+        else if (stream == 2) give(std::integral_constant<int, 2>{});
+        else give(std::integral_constant<int, 3>{});
+        *(TSDPA_LDS f32x2 *)(stats + stream * (NW * 512)) = f32x2{m_ref, l_tot};
+        __syncthreads();
+        f32x2 ml[NS - 1];
+        float M = m_ref;
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) {
+            ml[i] = *(TSDPA_LDS f32x2 *)(stats + (i < stream ? i : i + 1) * (NW * 512));
+            M = fmaxf(M, ml[i][0]);
+        }
+        // (m = -inf in all streams or in none: a row that no key of the run reaches)
+        const float w_own = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - M);
+        l_tot *= w_own;
+        m_ref = M;
+#pragma unroll
+        for (int i = 0; i < SHARE; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) own[i][e] *= w_own;
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) {
+            const float w = ml[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i][0] - M);
+            l_tot += w * ml[i][1];
+#pragma unroll
+            for (int ch = 0; ch < SHARE; ++ch) {
+                const f32x4 part = *(TSDPA_LDS f32x4 *)(part_of(stream, i) + ch * 1024);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[ch][e] += w * part[e];
+            }
+        }
+        const int ch0 = stream * SHARE;
+        if (splits > 1) {
+            const size_t prow = (size_t)(head * splits + sp) * S + qrow;
+            if (qrow < S) {
+                float *po = ws + prow * D + ch0 * 8 + g * 4;
+#pragma unroll
+                for (int ch = 0; ch < SHARE; ++ch) *(f32x4 *)(po + ch * 8) = own[ch];
+                if (g == 0 && stream == 0) {
+                    float *pml = ws + (size_t)(N / nQ) * S * D + prow * 2;
+                    pml[0] = m_ref;
+                    pml[1] = l_tot;
+                }
+            }
+            return;
+        }
+        const float inv = m_ref == -INFINITY ? 0.f : 1.0f / l_tot;
+        if (lse != nullptr && g == 0 && stream == 0 && qrow < S)
+            lse[(size_t)head * S + qrow] = l_tot > 0.f ? (m_ref + __builtin_amdgcn_logf(l_tot)) * 0.69314718055994530942f : -INFINITY;
+        // rows to the LDS and from there to memory, as below
+        __syncthreads();
+        constexpr int OCPR = G::OROW / 16, CMASK = OCPR - 1, ORPI = 64 / OCPR;
+        const lds_ptr ow = (lds_ptr)smem + wave * (32 * G::OROW);
+#pragma unroll
+        for (int ch = 0; ch < SHARE; ++ch) {
+            vec4 out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = (T)(own[ch][e] * inv);
+            *(TSDPA_LDS vec4 *)(ow + l32 * G::OROW + (((ch0 + ch) ^ (l32 & CMASK)) << 4) + g * 8) = out;
+        }
+        __syncthreads();
+        const int qrow0 = qt * TM + wave * 32;
+#pragma unroll
+        for (int i = 0; i < 32 / ORPI / NS; ++i) {
+            const int r = (stream * (32 / ORPI / NS) + i) * ORPI + lane / OCPR, cc = lane % OCPR;
+            const u32x4 val = lds_read128(ow + r * G::OROW + ((cc ^ (r & CMASK)) << 4));
+            if (qrow0 + r < S && cc < GCPR) *(u32x4 *)(o + head_off + (size_t)(qrow0 + r) * D + cc * 8) = val;
+        }
+        return;
+    }
+    if constexpr (NS > 1 && !SHARED) {
         // ---- one state from the streams': o, m, l of all but the first go through the LDS, lane by lane
         constexpr int STATE = 32 * D * 4 + 512;   // bytes per wavefront: [o chunk][lane] x 16, then [lane] x (m, l)
         typedef float f32x2 __attribute__((ext_vector_type(2)));
