@@ -324,8 +324,8 @@ int default_splits(int BH, int rows, int Skv, int D, bool fewest = false)
 // steps of 32 keys per stream; a round is as many workgroups as the GPU holds, a last one that is not half full counts as `alone`.  The
 // constants are fits to 110 shapes (1 ... 64 entries, 36 ... 1600 rows per head, 256 ... 32256 keys, lengths from all, half and a tenth
 // of the capacity on; BF16), each timed in every form at up to 11 split counts.  Mean time over them, the best form and count of each
-// being 1: this 1.04, at most 1.40; of one form at its best count 32 rows 1.16, 64 rows 1.10, 128 rows (from 65 on) 1.19; of one split in
-// the best form 1.87.  us, 32 / 64 / 128 rows at the best counts: 8 heads of 256 rows, 8192 keys D = 128 24.3 / 23.0 / 28.1; 256 heads of 60 rows, 2048
+// being 1: this 1.03, at most 1.38; of one form at its best count 32 rows 1.12, 64 rows 1.14, 128 rows (from 65 on) 1.23; of one split in
+// the best form 1.86.  us, 32 / 64 / 128 rows at the best counts: 8 heads of 256 rows, 8192 keys D = 128 24.3 / 23.0 / 28.1; 256 heads of 60 rows, 2048
 // ... 8192 keys in pages 159 / 139 / 153.  (64 rows in four streams, 128 in two: the best by 0.3 % on average, not built.  32 rows beyond
 // two workgroups per CU: what they read of the keys is then too much for the L2.)
 struct TreeForm { int rows, streams, splits; };
