@@ -2,7 +2,8 @@
 // positions of the tokens that a step appends to a cache.  See include/tiled_sdpa.h for the contract of the entry points.
 //
 // Both are a few kilobytes of work and bound by latency: one launch each, no atomics, no workspace, nothing that depends on
-// which workgroup runs first.
+// which workgroup runs first.  Kernel / whole call, us: masks of 1 tree of 15 tokens 1.8 / 4.8, of 64 trees of 255 3.7 / 4.8; steps
+// of 1 entry and token 2.8 / 4.9, of 256 entries of up to 60 tokens 4.1 / 5.0 (an empty kernel's call: 3.7 to 4.5).
 #include "tiled_sdpa.h"
 
 #include <cstdint>
