@@ -92,6 +92,7 @@ __device__ __forceinline__ StepEntry step_entry(const StepArgs &a, int b)
         // (next <= 2^31 - 1 + S, held in 64 bits; the sum over the entries in 32: it is a number of pages to wait for, not an index)
         const long long over = a.table ? (next - most + a.block_rows - 1) / a.block_rows : next - most;
         e.over = (int)(over < (1 << 16) ? over : 1 << 16);
+        e.next = (int)most;                        // (what is missing is counted up to the end from the pool, from there on as past it)
     } else if (e.sound) {
         e.next = (int)next;
     }

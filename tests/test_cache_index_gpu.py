@@ -207,3 +207,16 @@ def test_outputs_that_overlap_inputs_or_each_other_are_refused(lib):
             lib.cache_step(lens, counts, 1, 64, pages=(table, free, pool), out=out)
     lib.cache_step(lens, counts, 1, 64, pages=(table, free, pool), out=good)
     assert good[0].tolist() == [4, 5]
+
+
+def test_what_a_refused_step_lacks(lib):
+    """Of an entry that would pass its end the pages up to the end are missing from the pool, those behind it from its row."""
+    for lens, counts, R, M, free_now in (([0, 0], [5, 1], 1, 3, 2), ([60, 64], [400, 100], 64, 4, 1), ([0, 100, 7], [10, -100, 300], 64, 2, 0), ([3], [6], 1, 8, 3)):
+        p = Pool(lib, len(lens), M, R, lens, extra=free_now, seed=4)
+        have = min(p.have, free_now)
+        table, free = p.gpu[1].tolist(), p.gpu[2].tolist()
+        S = max(counts)
+        want = ref.step(lens, counts, S, R, table, free, have)
+        assert want[3][1] > 0
+        got = lib.cache_step(i32(lens), i32(counts), S, R, pages=(p.gpu[1], p.gpu[2], i32([have, 0])))
+        assert [x.tolist() for x in got] == [want[0], want[1], want[2], want[3]]
