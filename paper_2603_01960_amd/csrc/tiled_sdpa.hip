@@ -21,7 +21,7 @@ static __device__ __align__(256) unsigned char scratch[TSDPA_STATIC_SCRATCH_BYTE
 
 namespace {
 
-constexpr int kVersion = 300;  // 0.3.0
+constexpr int kVersion = 400;  // 0.4.0
 
 constexpr int kMaxDevices = 64;
 void *g_scratch_ptr[kMaxDevices];      // per device: address of that device's copy of `scratch`, once looked up
