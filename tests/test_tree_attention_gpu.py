@@ -307,3 +307,27 @@ def test_trees_of_several_sizes_in_one_batch(lib):
     for b, c in enumerate(counts):
         if c > 0:
             check(lib, q[b:b + 1, :, T - c:], k[b:b + 1], v[b:b + 1], [had[b] + c], [ref.ancestors(own[b])[0]], o[b:b + 1, :, T - c:])
+
+
+def test_caches_past_2_to_the_31(lib):
+    """Entries and pages on both sides of 2^31 elements, dense and paged, in every form."""
+    B, Hkv, cap, D, R = 3, 2, 4_000_000, 128, 128
+    lens = [300, 0, 257]
+    cache = [torch.empty(B, Hkv, cap, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    pages = [x.view(B * cap // R, Hkv, R, D) for x in cache]
+    last = pages[0].shape[0] - 1
+    table = i32([[0, last, 5], [7, 8, 9], [last - 1, 40000, 70000]])
+    for T, H in ((4, 4), (15, 4), (40, 4), (90, 4)):
+        q, k, v = inputs(B, H, Hkv, T, max(lens), D, torch.bfloat16, T)
+        sees = [ref.ancestors(a_tree(T, random.Random(b)))[0] for b in range(B)]
+        mask = torch.stack([ref.words_of(s, T) for s in sees]).cuda()
+        for x, y in zip(cache, (k, v)):
+            for b, n in enumerate(lens):
+                x[b, :, :n] = y[b, :, :n]
+        check(lib, q, k, v, lens, sees, lib.sdpa_tree(q, *cache, mask, kv_lens=i32(lens)))
+        for x, y in zip(pages, (k, v)):
+            for b, n in enumerate(lens):
+                for i in range(-(-n // R)):
+                    part = y[b, :, i * R:min(n, i * R + R)]
+                    x[int(table[b, i]), :, :part.shape[1]] = part
+        check(lib, q, k, v, lens, sees, lib.sdpa_tree_paged(q, *pages, i32(lens), table, mask))
