@@ -194,9 +194,15 @@ template <int D, bool INTER> struct RopeLane {
 template <typename T, int D, bool INTER> struct RopeTable {
     static constexpr int EACH = (D / 2 + 63) / 64;       // pairs of a lane
     double step[EACH];                             // turns per position
-    long long axis[EACH];                          // where its axis's positions begin
+    float freq[EACH];
+    int which[EACH];                               // its axis
+    long long axis[EACH];                          // where that one's positions begin
     int column[EACH][2];
     float *mine;
+    // Requests what the lane needs of the arguments' arrays.  Nothing here waits for a load, nor does request: their latencies, and in the
+    // forward kernel those of the first positions and rows, pass at the same time.  (One after another: B=4 S=512 H=32+8 D=128 BF16 into a cache
+    // 10.8 us instead of 9.9, B=4 S=2048 H=16+4 D=160 FP16 backward 37.7 / 37.4.  The backward's first rows requested before the
+    // others have arrived: 39.9.)
     __device__ __forceinline__ RopeTable(const RopeArgs &a, int lane, float *wave_sh) : mine(wave_sh + lane)
     {
 #pragma unroll
@@ -205,12 +211,32 @@ template <typename T, int D, bool INTER> struct RopeTable {
             const int c0 = RopeLane<D, INTER>::columns(a.rot, j, 0), c1 = RopeLane<D, INTER>::columns(a.rot, j, 1);
             const int pair = !INTER ? c0 + i : i < 4 ? c0 / 2 + i : c1 / 2 + i - 4;
             const bool turns = j < a.rot / 16;
-            step[e] = turns ? (double)a.inv_freq[pair] * 0.15915494309189533577 : 0.0;
-            int x = turns && a.axes != nullptr ? a.axes[pair] : 0;
-            x = x < 0 ? 0 : x < a.n_axes ? x : a.n_axes - 1;
-            axis[e] = x * a.pos_axis;
+            freq[e] = 0.f;
+            if (turns) freq[e] = a.inv_freq[pair];
+            which[e] = 0;
+            if (a.axes != nullptr && turns) which[e] = a.axes[pair];
 #pragma unroll
             for (int p = 0; p < 2; ++p) column[e][p] = RopeLane<D, INTER>::column(c0, c1, p, i);
+        }
+    }
+    // Where the positions are; the frequencies.
+    __device__ __forceinline__ void locate(const RopeArgs &a)
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            axis[e] = 0;
+            if (a.axes == nullptr) continue;
+            asm volatile("" : "+v"(which[e]));
+            axis[e] = (which[e] < 0 ? 0 : which[e] < a.n_axes ? which[e] : a.n_axes - 1) * a.pos_axis;
+        }
+    }
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            asm volatile("" : "+v"(freq[e]));          // (not where it is loaded)
+            step[e] = (double)freq[e] * 0.15915494309189533577;
+            asm volatile("" : "+v"(step[e]));          // (nor in the loop, which would wait for its own loads too)
         }
     }
     // whether the lane has an e-th pair
@@ -242,13 +268,31 @@ template <typename T, int D, bool INTER> struct RopeTable {
         }
         __builtin_amdgcn_wave_barrier();
     }
-    // the weights of its pairs' columns (1 without a norm)
-    __device__ __forceinline__ void weights(const void *at, int weight32, float (&w)[EACH][2]) const
+    // The weights of its pairs' columns: the words that hold them (16-bit ones two by two, whatever the type one load), and the values (1
+    // without a norm).
+    __device__ __forceinline__ void request(const void *at, int weight32, uint32_t (&words)[EACH][2]) const
     {
 #pragma unroll
         for (int e = 0; e < EACH; ++e)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) w[e][p] = at == nullptr ? 1.f : weight32 ? ((const float *)at)[column[e][p]] : (float)((const T *)at)[column[e][p]];
+            for (int p = 0; p < 2; ++p) words[e][p] = 0;
+        if (at == nullptr) return;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) words[e][p] = ((const uint32_t *)at)[weight32 ? column[e][p] : column[e][p] >> 1];
+    }
+    __device__ __forceinline__ void weights(const void *at, int weight32, uint32_t (&words)[EACH][2], float (&w)[EACH][2]) const
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                asm volatile("" : "+v"(words[e][p]));
+                const float own = (float)__builtin_bit_cast(T, (uint16_t)(words[e][p] >> (column[e][p] & 1) * 16));
+                w[e][p] = at == nullptr ? 1.f : weight32 ? __builtin_bit_cast(float, words[e][p]) : own;
+                asm volatile("" : "+v"(w[e][p]));
+            }
     }
 };
 __device__ __forceinline__ void rope_table_read(float (&x)[8], const float *at)
@@ -298,10 +342,6 @@ template <typename T, int D, bool CACHE, bool INTER, bool STREAM> __global__ voi
     if (wave >= items) return;
     const RopeLane<D, INTER> me(a.rot, lane);
     float *const table = table_sh[threadIdx.x >> 6];
-    const Table pairs(a, lane, table);
-    float weights[2][Table::EACH][2];
-    pairs.weights(a.weight[0], a.weight32, weights[0]);
-    pairs.weights(a.weight[1], a.weight32, weights[1]);
 
     struct Item { int which, b, s, token, first, last; };      // (first and last head)
     auto item_at = [&](int i) __attribute__((always_inline)) {
@@ -328,8 +368,17 @@ template <typename T, int D, bool CACHE, bool INTER, bool STREAM> __global__ voi
     int next_item = wave + a.waves, h0 = cur.first;
     bool fresh = true;
     Rows one, two;
+    Table pairs(a, lane, table);
+    uint32_t words[2][Table::EACH][2];
+    float weights[2][Table::EACH][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) pairs.request(a.weight[i], a.weight32, words[i]);
+    pairs.locate(a);
     pairs.positions(a, cur.b, cur.s, one.position);
     load(cur, h0, one.raw);
+    pairs.finish();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) pairs.weights(a.weight[i], a.weight32, words[i], weights[i]);
     // works on `now` and requests the next row group into `then`; false after the last
     auto turn = [&](Rows &now, Rows &then) __attribute__((always_inline)) {
         Item next = cur;
@@ -415,21 +464,6 @@ template <typename T, int D, bool INTER, bool STREAM> __global__ void __launch_b
     const long long dy_head = (long long)a.S * D;
     const RopeLane<D, INTER> me(a.rot, lane);
     float *const table = table_sh[wave_in];
-    const Table pairs(a, lane, table);
-    float w[Table::EACH][2];
-    pairs.weights(weight, a.weight32, w);
-    if (wave_in == 0)
-#pragma unroll
-        for (int e = 0; e < Table::EACH; ++e)
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-                if (pairs.has(e)) weight_sh[p][lane + e * 64] = w[e][p];
-    __syncthreads();
-    float wx[8], wy[8], dwx[8], dwy[8];
-    rope_table_read(wx, weight_sh[0] + me.first);
-    rope_table_read(wy, weight_sh[1] + me.first);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dwx[i] = dwy[i] = 0.f;
     const int items = a.B * a.S * spans;
 
     struct Item { int b, s, first, last; };
@@ -454,6 +488,25 @@ template <typename T, int D, bool INTER, bool STREAM> __global__ void __launch_b
     int next_item = wave + groups * 4, h0 = 0;
     bool fresh = true;
     Rows one, two;
+    Table pairs(a, lane, table);
+    uint32_t words[Table::EACH][2];
+    float w[Table::EACH][2];
+    pairs.request(weight, a.weight32, words);
+    pairs.locate(a);
+    pairs.finish();
+    pairs.weights(weight, a.weight32, words, w);
+    if (wave_in == 0)
+#pragma unroll
+        for (int e = 0; e < Table::EACH; ++e)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                if (pairs.has(e)) weight_sh[p][lane + e * 64] = w[e][p];
+    __syncthreads();
+    float wx[8], wy[8], dwx[8], dwy[8];
+    rope_table_read(wx, weight_sh[0] + me.first);
+    rope_table_read(wy, weight_sh[1] + me.first);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dwx[i] = dwy[i] = 0.f;
     auto turn = [&](Rows &now, Rows &then) __attribute__((always_inline)) {
         Item next = cur;
         int next_h0 = h0 + G::ROWS;
