@@ -17,8 +17,8 @@
 //     in 64 bits up to whole turns (a position of 2^31 has no fraction left in 32), then sine and cosine of the rest;
 //   * the next row group's loads are on their way while one is worked on.
 // Kernels, us and TB/s of what they have to read and write (a copy of 1 GiB: 5.2, of 64 MiB 8.0): forward B=2 S=8192 H=32+8 D=128 BF16 62, 5.4;
-// B=64 S=197 H=12+12 D=64 FP16 15, 5.1; into a cache B=4 S=512 H=32+8 D=128 BF16 11, 4.4, one token of it 3.7; backward of the first 88, 5.7
-// (and 4.5 for the weights' sums), B=4 S=2048 H=16+4 D=160 FP16 32, 4.9.
+// B=64 S=197 H=12+12 D=64 FP16 15, 5.1; into a cache B=4 S=512 H=32+8 D=128 BF16 10, 4.9, one token of it 3.0; backward of the first 88, 5.8
+// (and 4.6 for the weights' sums), B=4 S=2048 H=16+4 D=160 FP16 32, 5.0.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -69,9 +69,10 @@ int launch_rope_bwd_f16(int D, const RopeArgs &a);
 int launch_rope_bwd_bf16(int D, const RopeArgs &a);
 
 // Wavefronts per SIMD that the kernels are built for, and launches of no more: they are persistent.  One row group at a time and one
-// on its way needs few registers.  (us, forward at 4 / 5 / 6 wavefronts: B=2 S=8192 H=32+8 D=128 BF16 64.2 / 63.5 / 63.5, B=4 S=512 of it
-// into a cache 11.2 / 10.8 / 10.8; backward at 2 / 3 / 4: 93.0 / 98.1 / 99.4, B=4 S=2048 H=16+4 D=160 FP16 37.7 / 38.2 / 43.4: more rows of
-// partial sums, and no registers to spare.  Two row groups at a time: forward 65.1, backward 98.8 and 40.6.)
+// on its way needs few registers.  (us, forward at 4 / 5 / 6 wavefronts: B=2 S=8192 H=32+8 D=128 BF16 64.1 / 63.7 / 63.5, B=64 S=197
+// H=12+12 D=64 FP16 16.4 / 15.8 / 16.2, B=4 S=512 of the first into a cache 9.9 at each; backward at 2 / 3 / 4: 92.4 / 97.7 / 96.8, B=4 S=2048
+// H=16+4 D=160 FP16 37.5 / 37.9 / 44.5: more rows of partial sums, and no registers to spare.  Two row groups at a time, at an earlier step:
+// forward 63.5 -> 65.1, backward 93.0 -> 98.8.)
 constexpr int kRopeWaves = 5 * 1024, kRopeBwdMost = 2 * 256;   // wavefronts; workgroups, each of which leaves a row of partial sums
 
 #if defined(__HIP_DEVICE_COMPILE__)
