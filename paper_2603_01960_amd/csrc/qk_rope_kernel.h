@@ -135,6 +135,7 @@ template <typename T, bool INTER> struct RopePairs {
 template <int D, bool INTER> struct RopeLane {
     int row, col[2];                               // row within the wavefront's; first columns of the two pieces
     bool active;                                   // the lane has a row
+    bool turns;                                    // its columns are rotated: all of them or none
     int first;                                     // its first pair, of the D / 2 that the lanes of a row have
     int other[4];                                  // D = 96, 160: lanes that row_sum takes (times 4)
     __device__ __forceinline__ RopeLane(int rot, int lane)
@@ -143,6 +144,7 @@ template <int D, bool INTER> struct RopeLane {
         row = lane / G::LANES;
         const int j = lane % G::LANES;
         active = row < G::ROWS;
+        turns = j < rot / 16;
         first = j * 8;
         constexpr int H = G::LANES / 2;
 #pragma unroll
@@ -427,8 +429,10 @@ template <typename T, int D, bool CACHE, bool INTER, bool STREAM> __global__ voi
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float x0 = x[i], y0 = y[i];
-                x[i] = r * __builtin_fmaf(x0, cx[i], -(y0 * sy[i]));
-                y[i] = r * __builtin_fmaf(y0, cy[i], x0 * sx[i]);
+                // (a sine of 0 would do for finite values only: columns that are not rotated have nothing of each other's)
+                const float from_y = me.turns ? y0 * sy[i] : 0.f, from_x = me.turns ? x0 * sx[i] : 0.f;
+                x[i] = r * __builtin_fmaf(x0, cx[i], -from_y);
+                y[i] = r * __builtin_fmaf(y0, cy[i], from_x);
             }
             P::write(now.raw, x, y);
         }
@@ -529,9 +533,9 @@ template <typename T, int D, bool INTER, bool STREAM> __global__ void __launch_b
         P::read(g, h, now.draw);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {                  // rotated back
-            const float g0 = g[i];
-            g[i] = __builtin_fmaf(g0, c[i], h[i] * sn[i]);
-            h[i] = __builtin_fmaf(h[i], c[i], -(g0 * sn[i]));
+            const float g0 = g[i], from_h = me.turns ? h[i] * sn[i] : 0.f, from_g = me.turns ? g0 * sn[i] : 0.f;
+            g[i] = __builtin_fmaf(g0, c[i], from_h);
+            h[i] = __builtin_fmaf(h[i], c[i], -from_g);
         }
         if (norm) {
             float x[8], y[8], dot = 0.f;
