@@ -456,8 +456,8 @@ typedef struct {
  * whose squares all fall below it (1e-19).
  *
  *   q, k         : tsdpa_rows of [B, S, H, D] and [B, S, Hkv, D].
- *   q_out, k_out : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned: what tiled_sdpa_fwd and its kin read.  Must not
- *                  overlap the inputs.
+ *   q_out, k_out : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned: what tiled_sdpa_fwd and its kin read.  Must overlap
+ *                  neither each other nor the inputs.
  *
  * Validation order, of all three calls: dtypes, D, shape (rot, n_axes, the cache's among it), empty problem, null pointers, alignment,
  * strides, eps, workspace, launch.
@@ -472,7 +472,8 @@ int tiled_sdpa_qk_norm_rope(const tsdpa_rope *p, const tsdpa_rows *q, const tsdp
  *                      token whose slot is negative or past the last page's is not written.  Tokens with the same slot: one of them
  *                      is, row by row and which one is not said.
  *   k_cache, v_cache : [pages, Hkv, block_rows, D] (of a dense cache [B, Hkv, Skv, D]: pages = B, block_rows = Skv); pages *
- *                      block_rows fits an int.  Other rows are left as they are.
+ *                      block_rows fits an int.  Other rows are left as they are.  q_out and the caches must overlap neither each
+ *                      other nor the inputs (rows that another token's part of the call still reads, among them).
  */
 int tiled_sdpa_qk_norm_rope_cache(const tsdpa_rope *p, const tsdpa_rows *q, const tsdpa_rows *k, const tsdpa_rows *v, const int *slots,
                                   void *q_out, void *k_cache, void *v_cache, int pages, int block_rows, void *stream);
@@ -484,7 +485,8 @@ int tiled_sdpa_qk_norm_rope_cache(const tsdpa_rope *p, const tsdpa_rows *q, cons
  *
  *   dq_out, dk_out     : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned.
  *   q, k               : as for the forward call (without weights they are not looked at).
- *   dq, dk             : tsdpa_rows to be written, of the shapes of q and k; every element is overwritten.  Must not overlap the inputs.
+ *   dq, dk             : tsdpa_rows to be written, of the shapes of q and k; every element is overwritten.  Must overlap neither each
+ *                        other (views of one packed tensor that share no element do not) nor the inputs that are looked at.
  *   dq_weight, dk_weight : [D] in weight_dtype; not looked at (may be NULL) where there is no weight.
  *   workspace          : device, 16-byte aligned, at least tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(B, S, D) bytes; not looked at
  *                        without weights.  Calls that may overlap on the GPU need distinct ones.

@@ -390,7 +390,8 @@ def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, *, axes=None, ep
     ``q_weight``, ``k_weight`` [D] (float32 or the dtype of q; None: no norm of that tensor).  ``inv_freq`` float32 [rot / 2]: the angle of
     pair i is position * inv_freq[i]; columns past rot (a multiple of 16) are not rotated; pairs are columns (i, i + rot / 2), or
     neighbours if ``interleaved``.  ``positions`` int32 [S] or [B, S]; with several axes (time, height, width) [A, S] or [A, B, S], and
-    ``axes`` int32 [rot / 2] names each pair's.  See tiled_sdpa_qk_norm_rope."""
+    ``axes`` int32 [rot / 2] names each pair's.  ``out=(q_out, k_out)`` must overlap neither each other nor what the call reads.  See
+    tiled_sdpa_qk_norm_rope."""
     return _checked(_calls().qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, out))
 
 
@@ -398,14 +399,15 @@ def qk_norm_rope_cache(q, k, v, q_weight, k_weight, positions, inv_freq, k_cache
                        interleaved: bool = False, out=None):
     """:func:`qk_norm_rope` for a serving step: returns q for attention, and writes k (normed, rotated) and v [B, S, Hkv, D] (as it is) to
     the rows ``slots`` (int32 [B, S], of :func:`cache_step`; negative: nowhere) of the cache [pages, Hkv, block_rows, D], or of a dense one
-    [B, Hkv, Skv, D].  See tiled_sdpa_qk_norm_rope_cache."""
+    [B, Hkv, Skv, D].  The result and the caches must overlap neither each other nor what the call reads.  See tiled_sdpa_qk_norm_rope_cache."""
     return _checked(_calls().qk_norm_rope_cache(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, v, k_cache, v_cache, slots, out))
 
 
 def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_freq, *, axes=None, eps: float = 1e-6,
                           interleaved: bool = False, workspace=None, grads=None):
     """(dq, dk, dq_weight, dk_weight) of :func:`qk_norm_rope`, given the gradients [B, H, S, D] and [B, Hkv, S, D] of its results and its
-    arguments.  ``grads=(dq, dk)`` lets the caller own these (views into one packed tensor, for example); the weights' gradients are
+    arguments.  ``grads=(dq, dk)`` lets the caller own these (views into one packed tensor, for example, that share no element with each
+    other, nor with what the call reads); the weights' gradients are
     in the weights' dtype, None where there is no weight.  See tiled_sdpa_qk_norm_rope_bwd."""
     return _checked(_calls().qk_norm_rope_backward(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, dq_out, dk_out, workspace, grads))
 

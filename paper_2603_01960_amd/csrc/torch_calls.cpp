@@ -21,6 +21,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include "rows_overlap.h"
 #include "tiled_sdpa.h"
 
 namespace {
@@ -636,13 +637,33 @@ at::Tensor made(const at::Tensor &t, at::IntArrayRef shape, at::ScalarType type,
     return t;
 }
 
-// Memory of a contiguous tensor.  Outputs that overlap what a kernel's other workgroups still read are refused.
+// Memory of a tensor: contiguous, or rows of a strided one ([B, S, heads, D]).  Outputs that overlap what a kernel's other workgroups
+// still read are refused; most calls' tensors are told apart by where they begin and end.
 struct Extent {
-    const char *at;
-    int64_t bytes;
-    explicit Extent(const at::Tensor &t) : at((const char *)data(t)), bytes((int64_t)t.nbytes()) {}
-    Extent(const int *p, int64_t count) : at((const char *)p), bytes(p ? count * (int64_t)sizeof(int) : 0) {}
-    bool meets(const Extent &o) const { return bytes > 0 && o.bytes > 0 && at < o.at + o.bytes && o.at < at + bytes; }
+    int64_t at = 0, end = 0;
+    const at::Tensor *rows = nullptr;              // strided
+    Extent() = default;
+    explicit Extent(const at::Tensor &t) : at((int64_t)(uintptr_t)data(t)), end(at + (int64_t)t.nbytes())
+    {
+        if (t.dim() != 4 || end == at || t.is_contiguous()) return;
+        rows = &t;
+        end = at + (int64_t)t.element_size() * (t.stride(0) * (t.size(0) - 1) + t.stride(1) * (t.size(1) - 1) + t.stride(2) * (t.size(2) - 1) + t.size(3));
+    }
+    Extent(const void *p, int64_t bytes) : at((int64_t)(uintptr_t)p), end(p ? at + bytes : at) {}
+    Extent(const int *p, int64_t count) : Extent((const void *)p, count * (int64_t)sizeof(int)) {}
+    tsdpa::RowSet set() const
+    {
+        if (!rows) return tsdpa::RowSet{at, end - at};
+        const int64_t size = (int64_t)rows->element_size();
+        tsdpa::RowSet r{at, rows->size(3) * size, 3};
+        for (int i = 0; i < 3; ++i) r.dim[i] = {rows->stride(i) * size, rows->size(i)};
+        return r;
+    }
+    bool meets(const Extent &o) const
+    {
+        if (at >= o.end || o.at >= end || at == end || o.at == o.end) return false;
+        return (!rows && !o.rows) || tsdpa::RowsOverlap()(set(), o.set());
+    }
 };
 void distinct(std::initializer_list<Extent> outputs, std::initializer_list<Extent> inputs, const char *complaint)
 {
@@ -770,6 +791,7 @@ struct Rope {
     tsdpa_rope p{};
     at::Tensor q, k;
     at::Tensor weight[2];
+    int64_t n_positions = 0;
     explicit Rope(PyObject *const *args)
     {
         q = rows_tensor(args[0], "q");
@@ -817,6 +839,7 @@ struct Rope {
                 fail(text);
             if (several && (x.size(0) < 1 || x.size(0) > std::numeric_limits<int>::max())) fail(text);
             p.positions = (const int *)data(x);
+            n_positions = x.numel();
             p.pos_batch = dims == 2 ? (long long)s[1] : 0;
             p.pos_axis = dims == 2 ? (long long)(s[0] * s[1]) : (long long)s[1];
             p.n_axes = several ? (int)x.size(0) : 1;
@@ -826,6 +849,16 @@ struct Rope {
         if (eps == -1.0 && PyErr_Occurred()) throw PyFail{};
         p.eps = (float)eps;
         p.flags = as_bool(args[8]) ? (unsigned)TSDPA_FLAG_INTERLEAVED : 0u;
+    }
+    // Refuses outputs that overlap each other or what the kernel reads (`rows` and the arguments).
+    void apart(std::initializer_list<Extent> outputs, std::initializer_list<Extent> rows, const char *complaint) const
+    {
+        distinct(outputs, rows, complaint);
+        const int64_t weight_bytes = (int64_t)p.D * (p.weight_dtype == TSDPA_F32 ? 4 : 2), pairs = p.rot / 2;
+        for (const Extent &i : {Extent(p.q_weight, weight_bytes), Extent(p.k_weight, weight_bytes), Extent(p.positions, n_positions),
+                                Extent((const void *)p.inv_freq, pairs * (int64_t)sizeof(float)), Extent(p.axes, pairs)})
+            for (const Extent &o : outputs)
+                if (o.meets(i)) fail(complaint);
     }
     // [B, heads, S, D], as attention reads them
     at::Tensor heads_out(const at::Tensor &given, const at::Tensor &x, const char *complaint) const
@@ -843,6 +876,7 @@ PyObject *call_qk_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
         static const char text[] = "out must be (q_out, k_out): contiguous [B, H, S, D] and [B, Hkv, S, D] like q and k";
         const Given<2> given(args[9], text);
         const at::Tensor q_out = r.heads_out(given.t[0], r.q, text), k_out = r.heads_out(given.t[1], r.k, text);
+        if (args[9] != Py_None) r.apart({Extent(q_out), Extent(k_out)}, {Extent(r.q), Extent(r.k)}, "q_out and k_out must overlap neither each other nor what the call reads");
         const tsdpa_rows q = rows_of(r.q), k = rows_of(r.k);
         const Launch on(r.q);
         const int st = without_gil(tiled_sdpa_qk_norm_rope, &r.p, &q, &k, data(q_out), data(k_out), on.stream);
@@ -867,6 +901,9 @@ PyObject *call_qk_norm_rope_cache(PyObject *, PyObject *const *args, Py_ssize_t 
         static const char text[] = "out must be contiguous [B, H, S, D] like q";
         if (args[13] != Py_None && !THPVariable_Check(args[13])) fail(text);
         const at::Tensor q_out = r.heads_out(args[13] == Py_None ? at::Tensor() : THPVariable_Unpack(args[13]), r.q, text);
+        r.apart({Extent(kc), Extent(vc), args[13] == Py_None ? Extent() : Extent(q_out)},      // (a new tensor overlaps nothing)
+                {Extent(r.q), Extent(r.k), Extent(v), Extent(slots, (int64_t)r.p.B * r.p.S)},
+                "the result, k_cache and v_cache must overlap neither each other nor what the call reads");
         const tsdpa_rows q = rows_of(r.q), k = rows_of(r.k), vr = rows_of(v);
         const Launch on(r.q);
         const int st = without_gil(tiled_sdpa_qk_norm_rope_cache, &r.p, &q, &k, &vr, slots, data(q_out), data(kc), data(vc), (int)c[0], (int)c[2], on.stream);
@@ -901,6 +938,9 @@ PyObject *call_qk_norm_rope_backward(PyObject *, PyObject *const *args, Py_ssize
                 if (!same_sizes(t, like) || t.scalar_type() != like.scalar_type() || t.device() != like.device() || (t.size(3) > 1 && t.stride(3) != 1)) fail(text);
                 dx[i] = t;
             }
+            // (of q and k the norm's rows are read, no others)
+            const auto read = [&](int i, const at::Tensor &x) { return r.weight[i].defined() ? Extent(x) : Extent(); };
+            r.apart({Extent(dx[0]), Extent(dx[1])}, {Extent(dq_out), Extent(dk_out), read(0, r.q), read(1, r.k)}, "dq and dk must overlap neither each other nor what the call reads");
         }
         for (int i = 0; i < 2; ++i)
             if (r.weight[i].defined()) dw[i] = empty(r.weight[i].sizes(), r.weight[i].scalar_type(), r.q);
