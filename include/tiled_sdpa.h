@@ -392,8 +392,11 @@ int tiled_sdpa_tree_mask(const int *parents, long long *mask, int *depths, int B
  *
  *   kv_lens      : device int32 [B]: rows of each entry now.  An entry holds exactly ceil(rows / block_rows) pages, the first of
  *                  its row of block_table.
- *   counts       : device int32 [B]: rows to append (0 ... S), or to drop (negative: rejected drafts; -kv_lens[b] for a request
- *                  that is done).
+ *   counts       : device int32 [B]: rows to append (0 ... S), or to drop (negative; -kv_lens[b] for a request that is done).  What is
+ *                  dropped are an entry's LAST rows, whichever tokens they hold: of drafts in a chain the rejected ones.  The accepted
+ *                  tokens of a tree that branches are a path through it, in general not the first of its rows: the caller moves
+ *                  their rows of K and V to the front of the tree's first (row i of the tree to slot i of those that this call
+ *                  returned; a token's position, that of its depth, is then its row's), or siblings' rows stay in their place.
  *   depths       : NULL, or device int32 [B, S] (tiled_sdpa_tree_mask): token i of an entry has position
  *                  new_lens[b] - S + depths[b][i] instead of the one of its row.
  *   block_table  : device int32 [B, max_blocks], in and out: as for tiled_sdpa_fwd_paged.  NULL = a dense cache [B, Hkv, block_rows, D]

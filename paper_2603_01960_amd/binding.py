@@ -370,8 +370,11 @@ def tree_mask(parents, *, out=None):
 
 def cache_step(kv_lens, counts, S: int, block_rows: int, *, pages=None, depths=None, out=None):
     """(new_lens, slots, positions, new_pool) of a serving step that appends ``counts[b]`` (0 ... S) rows to entry b of a cache, or drops
-    that many (negative: rejected drafts, finished requests).  slots and positions are int32 [B, S], an entry's new tokens at the end
-    of its row, -1 (and 0) before them: what :func:`qk_norm_rope_cache` takes.
+    that many (negative: finished requests, rejected drafts).  What is dropped are the entry's last rows: of a tree that branches the
+    accepted tokens, a path through it, have to be moved to the front of the tree's rows first, in K and V of every layer (of trees of S
+    tokens each, with ``path`` int64 [B, S], the accepted tokens in order and i itself from there on: ``src = slots.gather(1, path)``, and
+    ``cache[slots // block_rows, :, slots % block_rows] = cache[src // block_rows, :, src % block_rows]``).  slots and positions are int32
+    [B, S], an entry's new tokens at the end of its row, -1 (and 0) before them: what :func:`qk_norm_rope_cache` takes.
 
     ``pages = (block_table, free_pages, pool)`` of a paged cache: int32 [B, max_blocks] and [pool_size], changed in place, and the
     int32 [2] that the last step returned as new_pool (at first: the number of pages in free_pages, 0).  Without it the cache is
