@@ -687,16 +687,17 @@ template <typename T> int launch_decode(int D, const LaunchArgs &a)
     }
 }
 
-template <typename T, int D, int NQ> int launch_tree_decode_rows(const LaunchArgs &a)
+template <typename T, int D, int NQ, bool HALVES> int launch_tree_decode_rows(const LaunchArgs &a)
 {
     if (decode_waves(a.BH, a.splits, a.Skv) == 8)
-        return a.block_table ? launch_decode_one<T, D, NQ, 8, true, false, true>(a) : launch_decode_one<T, D, NQ, 8, false, false, true>(a);
-    return a.block_table ? launch_decode_one<T, D, NQ, 4, true, false, true>(a) : launch_decode_one<T, D, NQ, 4, false, false, true>(a);
+        return a.block_table ? launch_decode_one<T, D, NQ, 8, true, HALVES, true>(a) : launch_decode_one<T, D, NQ, 8, false, HALVES, true>(a);
+    return a.block_table ? launch_decode_one<T, D, NQ, 4, true, HALVES, true>(a) : launch_decode_one<T, D, NQ, 4, false, HALVES, true>(a);
 }
 
 template <typename T, int D> int launch_tree_decode_dim(const LaunchArgs &a)
 {
-    return a.S > 16 ? launch_tree_decode_rows<T, D, 2>(a) : launch_tree_decode_rows<T, D, 1>(a);
+    if (a.S > 16) return launch_tree_decode_rows<T, D, 2, false>(a);
+    return a.halves ? launch_tree_decode_rows<T, D, 1, true>(a) : launch_tree_decode_rows<T, D, 1, false>(a);
 }
 
 template <typename T> int launch_tree_decode(int D, const LaunchArgs &a)

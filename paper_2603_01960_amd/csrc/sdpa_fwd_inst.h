@@ -21,7 +21,7 @@ constexpr int kLdsPerCU = 160 * 1024;
 // halves and move them back and forth (or to scratch) inside the loop.
 template <int D, int NW, int TN> constexpr int waves_per_simd() { return (TN == 32 && D <= 128) ? 3 : 2; }
 
-template <typename T, int D, int NW, int TN, int KV = 0, int NS = 1>     // KV: 0 square, 1 dense cache, 2 paged cache, 3 and 4 these with halved weights, 5 and 6 with trees; NS streams
+template <typename T, int D, int NW, int TN, int KV = 0, int NS = 1>     // KV: 0 square, 1 dense cache, 2 paged cache, 3 and 4 these with halved weights, 5 and 6 with trees, 7 and 8 with both; NS streams
 int launch_one(const LaunchArgs &a)
 {
     constexpr int WPS = NS > 1 ? 2 : waves_per_simd<D, NW, TN>();

@@ -318,7 +318,7 @@ template <> struct StreamRead<160> {
 // as two 16-bit halves, for the few query rows of a decoding step (pick_halves).  5, 6: dense and paged, the queries being a tree of
 // drafted tokens: the last Sp keys are the tokens' own, and which of them a query sees stands in its row of `tree`, tree_words
 // 32-bit words, bit j for key Skv - Sp + j.  Keys before them are seen by all, so that only the last tiles take the masked path; there a
-// lane shifts the bits of a block of 32 keys out of two words of its row.
+// lane shifts the bits of a block of 32 keys out of two words of its row.  7, 8: these two with weights in halves.
 // TILE: rows T_N of a K/V tile, plus 1000 * (NS - 1).  NS > 1: NS streams of NW wavefronts each work on
 // the same query rows; stream s takes the tiles s, s + NS, ... into LDS slots of its own, and the streams' states (o, m,
 // l of Eqs. 2-4) are combined through the LDS at the end, in their order.  For launches of few workgroups: the chain of tiles
@@ -335,7 +335,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                 int batches, Divisor by_batches, const uint32_t *__restrict__ tree, long long tree_batch, int tree_words)
 {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass only needs the launch stub; the body uses device-only types
-    constexpr bool KV = KVM != 0, TREE = KVM >= 5, PAGED = KVM == 2 || KVM == 4 || KVM == 6, HALVES = KVM == 3 || KVM == 4;
+    constexpr bool KV = KVM != 0, TREE = KVM >= 5, PAGED = KVM != 0 && KVM % 2 == 0, HALVES = KVM == 3 || KVM == 4 || KVM >= 7;
     constexpr int TN = TILE % 1000, NS = 1 + TILE / 1000;
     using E = Elem<T>;
     using vec8 = typename E::vec8;
@@ -928,6 +928,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                     i16x8 a = __builtin_shufflevector(vf[db][0], vf[db][1], 0, 1, 2, 3, 4, 5, 6, 7);
                     if constexpr (MASK) take_not_finite(a, db, 0, ks);
                     oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), pb[0][ks], oacc[db]);
+                    if constexpr (HALVES) oacc[db] = E::mfma(__builtin_bit_cast(vec8, a), ph[0][ks], oacc[db]);
                     constexpr int HOOKS = 2 * DB;
                     const int h = ks * DB + db;
 #pragma unroll

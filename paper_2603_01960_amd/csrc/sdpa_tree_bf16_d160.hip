@@ -3,5 +3,8 @@
 
 namespace tsdpa {
 int launch_tree_bf16_d160_tn32(int tile_m, const LaunchArgs &a);
-int launch_tree_bf16_d160(int tile_m, const LaunchArgs &a) { return launch_tree<__bf16, 160>(tile_m, a, launch_tree_bf16_d160_tn32); }
+int launch_tree_bf16_d160(int tile_m, const LaunchArgs &a)
+{
+    return launch_tree<__bf16, 160>(tile_m, a, launch_tree_bf16_d160_tn32, nullptr);
+}
 }  // namespace tsdpa

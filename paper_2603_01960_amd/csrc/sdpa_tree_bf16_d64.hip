@@ -3,5 +3,9 @@
 
 namespace tsdpa {
 int launch_tree_bf16_d64_tn64(int tile_m, const LaunchArgs &a);
-int launch_tree_bf16_d64(int tile_m, const LaunchArgs &a) { return launch_tree<__bf16, 64>(tile_m, a, launch_tree_bf16_d64_tn64); }
+int launch_tree_bf16_d64_halves(int tile_m, const LaunchArgs &a);
+int launch_tree_bf16_d64(int tile_m, const LaunchArgs &a)
+{
+    return launch_tree<__bf16, 64>(tile_m, a, launch_tree_bf16_d64_tn64, launch_tree_bf16_d64_halves);
+}
 }  // namespace tsdpa

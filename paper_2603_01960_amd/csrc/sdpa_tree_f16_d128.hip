@@ -3,5 +3,9 @@
 
 namespace tsdpa {
 int launch_tree_f16_d128_tn64(int tile_m, const LaunchArgs &a);
-int launch_tree_f16_d128(int tile_m, const LaunchArgs &a) { return launch_tree<_Float16, 128>(tile_m, a, launch_tree_f16_d128_tn64); }
+int launch_tree_f16_d128_halves(int tile_m, const LaunchArgs &a);
+int launch_tree_f16_d128(int tile_m, const LaunchArgs &a)
+{
+    return launch_tree<_Float16, 128>(tile_m, a, launch_tree_f16_d128_tn64, launch_tree_f16_d128_halves);
+}
 }  // namespace tsdpa

@@ -1,0 +1,6 @@
+// Trees of drafted tokens: element type f16, head dim 96, 32 rows in four streams with weights in halves.
+#include "sdpa_tree_inst.h"
+
+namespace tsdpa {
+int launch_tree_f16_d96_halves(int tile_m, const LaunchArgs &a) { return launch_tree_halved<_Float16, 96>(tile_m, a); }
+}  // namespace tsdpa

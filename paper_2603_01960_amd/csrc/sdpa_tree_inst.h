@@ -14,6 +14,15 @@ template <typename T, int D> int launch_tree_plain(int tile_m, const LaunchArgs 
     return a.block_table ? launch_one<T, D, 4, TN, 6>(a) : launch_one<T, D, 4, TN, 5>(a);
 }
 
+using LaunchTree = int (*)(int tile_m, const LaunchArgs &a);
+
+// 32 rows with weights in halves (pick_halves): in translation units of their own (sdpa_tree_*_halves.hip), up to D = 128
+template <typename T, int D> int launch_tree_halved(int tile_m, const LaunchArgs &a)
+{
+    if (tile_m != 32 || a.streams != 4) return (int)hipErrorInvalidValue;
+    return a.block_table ? launch_one<T, D, 1, 32, 8, 4>(a) : launch_one<T, D, 1, 32, 7, 4>(a);
+}
+
 template <typename T, int D, int KV> int launch_tree_streams(int tile_m, const LaunchArgs &a)
 {
     switch (tile_m * 10 + a.streams) {
@@ -23,11 +32,10 @@ template <typename T, int D, int KV> int launch_tree_streams(int tile_m, const L
     return (int)hipErrorInvalidValue;
 }
 
-using LaunchTree = int (*)(int tile_m, const LaunchArgs &a);
-
-template <typename T, int D> int launch_tree(int tile_m, const LaunchArgs &a, LaunchTree plain)
+template <typename T, int D> int launch_tree(int tile_m, const LaunchArgs &a, LaunchTree plain, LaunchTree halved)
 {
     if (a.streams <= 1) return plain(tile_m, a);
+    if (a.halves) return halved ? halved(tile_m, a) : (int)hipErrorInvalidValue;
     return a.block_table ? launch_tree_streams<T, D, 6>(tile_m, a) : launch_tree_streams<T, D, 5>(tile_m, a);
 }
 

@@ -287,7 +287,10 @@ int pick_streams_kv(long long heads, int rows, int Skv, int D, int *tm)
 // the place of the decoding kernel's runs of a tile or two per wavefront, the error was 5 to 18 % larger, and is smaller this way
 // (BF16, 16 heads, 2 rows, 744 keys, D = 96 in six runs 1.96e-3, in one 2.32e-3, this way 1.81e-3).  The calls take 0 to
 // 4 % longer for it (us: 7 heads, 2 rows, 365 keys D = 64 in several runs 6.7, in one 4.6, this way 4.7; 68 heads, 26 rows, 1607 keys
-// in the decoding kernel 16.3, in streams 14.7, this way 15.5).
+// in the decoding kernel 16.3, in streams 14.7, this way 15.5).  Trees of drafted tokens likewise, so that a chain given as a tree is as
+// exact as under the causal mask: errors of 1.40 times the result's own rounding (BF16, 16 heads, 2 rows, 744 keys, D = 96) are below
+// 1.15 (us, whole weights / this way / causal: that call 7.7 / 7.8; in streams 72 heads of 20 rows, 512 keys D = 128 9.2 / 9.9 / 9.3,
+// 112 of 32, 385 keys D = 96 7.8 / 8.4 / 8.6, 72 of 24, 900 keys D = 64 7.9 / 9.1 / 9.0, 66 of 20, 3000 keys D = 128 27.7 / 28.7 / 26.1).
 bool pick_halves(int BH, int rows, int Skv, int D, int splits, int streams)
 {
     if (Skv <= 256) return false;                 // (one run of a tile or two at all times)
@@ -842,7 +845,7 @@ static int fwd_kv_impl(const void *q, const void *k, const void *v, void *o, flo
         }
     }
     const bool decode = heuristic_tile && rows <= kDecodeRows && a.streams <= 1;
-    a.halves = !tree.mask && (decode || a.streams > 1) && pick_halves(a.BH, rows, Skv, D, splits, a.streams) ? 1 : 0;
+    a.halves = (decode || a.streams > 1) && pick_halves(a.BH, rows, Skv, D, splits, a.streams) ? 1 : 0;
     // The decoding kernel combines the runs itself while they are few: a mark (8 bytes) per run must fit a head's part of o,
     // and past 32 states per head, eight rows, or four columns for each thread, the one workgroup that does it is slower than the
     // merge kernel's many (time with the marks / with two kernels, over 300 shapes: one row 0.95 at 2 runs, 0.97 at 8, 1.04 at 20;
