@@ -1092,7 +1092,8 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
             ml[i] = *(TSDPA_LDS f32x2 *)(stats + (i < stream ? i : i + 1) * (NW * 512));
             M = fmaxf(M, ml[i][0]);
         }
-        // (m = -inf in all streams or in none: a row that no key of the run reaches)
+        // (m = -inf: no key of the stream's tiles reaches the row, in a tree in some streams perhaps and in others not.  In all of them, a
+        // row that no key of the run reaches, M is -inf too and m - M no number: hence the case of its own)
         const float w_own = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - M);
         l_tot *= w_own;
         m_ref = M;
@@ -1179,7 +1180,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
                 ml[s] = *(TSDPA_LDS f32x2 *)(at + (s - 1) * (NW * STATE) - lane * 8 + 32 * D * 4);
                 M = fmaxf(M, ml[s][0]);
             }
-            // (m = -inf in all streams or in none: a row that no key of the run reaches)
+            // (m = -inf: in all streams, M among it, of a row that no key of the run reaches, see above; in a tree also in some of them)
             float w[NS];
             l_tot = 0.f;
 #pragma unroll
