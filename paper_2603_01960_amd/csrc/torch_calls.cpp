@@ -722,11 +722,12 @@ PyObject *call_cache_step(PyObject *, PyObject *const *args, Py_ssize_t n)
         int *table = nullptr, *free_pages = nullptr;
         const int *pool = nullptr;
         int64_t max_blocks = 0, pool_size = 0;
+        at::Tensor pages[3];                       // (a sequence that nobody else holds may be all that keeps them)
         if (args[4] != Py_None) {
             static const char text[] = "pages must be (block_table, free_pages, pool): contiguous int32 [B, max_blocks], [pool_size] and [2] on the device of kv_lens";
             each_of(args[4], 3, text, [&](Py_ssize_t i, PyObject *x) {
                 if (!THPVariable_Check(x)) fail(text);
-                const at::Tensor &t = THPVariable_Unpack(x);
+                const at::Tensor &t = pages[i] = THPVariable_Unpack(x);
                 if (t.scalar_type() != at::kInt || t.device() != device || !t.is_contiguous() || t.dim() != (i == 0 ? 2 : 1)) fail(text);
                 if (i == 0) {
                     if (t.size(0) != B) fail(text);
