@@ -456,7 +456,8 @@ typedef struct {
  *     y = x / sqrt(mean(x^2) + eps) * w,     (y_a cos - y_b sin, y_b cos + y_a sin),
  * and the layout.  FP32 throughout (angles in 64 bits up to whole turns: any position is as exact as the first), one rounding.  The mean
  * of squares is taken in FP32: rows of BF16 values whose squares overflow it (beyond 1e18) have no norm, nor, with eps = 0, rows
- * whose squares all fall below it (1e-19).
+ * whose squares all fall below it (1e-19); an eps below 1.2e-38 (FP32's smallest normal number) counts as 0.  Columns from rot on
+ * are only normed and weighted: what another column holds, infinities and NaN included, reaches them through the row's mean alone.
  *
  *   q, k         : tsdpa_rows of [B, S, H, D] and [B, S, Hkv, D].
  *   q_out, k_out : [B, H, S, D] and [B, Hkv, S, D], contiguous, 16-byte aligned: what tiled_sdpa_fwd and its kin read.  Must overlap

@@ -364,7 +364,8 @@ def sdpa_tree_paged(q, k_pages, v_pages, kv_lens, block_table, mask, scale=None,
 def tree_mask(parents, *, out=None):
     """(mask, depths) of trees of drafted tokens: ``parents`` int32 [B, T] (or [T]) names the earlier token of the tree that each token
     follows, any other value the cached sequence.  mask int64 [B, T, ceil(T / 64)]: bit j of token i's words is set iff j is i or one of its
-    ancestors (what :func:`sdpa_tree` reads); depths int32 [B, T]: how many ancestors (what :func:`cache_step` takes).  T <= 1024."""
+    ancestors (what :func:`sdpa_tree` reads); depths int32 [B, T]: how many ancestors (what :func:`cache_step` takes).  T <= 1024.
+    Without ``out`` the two share one allocation: either keeps (and torch.save stores) both."""
     return _checked(_calls().tree_mask(parents, out))
 
 
@@ -381,7 +382,8 @@ def cache_step(kv_lens, counts, S: int, block_rows: int, *, pages=None, depths=N
     dense, [B, Hkv, block_rows, D].  new_pool[1] != 0 says that the step was refused (pages or rows missing, -1: numbers that cannot
     be) and changed nothing.  ``depths`` (of :func:`tree_mask`): the tokens of a tree have the position of their depth.
 
-    Nothing is read back by the host.  new_lens and new_pool must not be kv_lens and pool.  See tiled_sdpa_cache_step."""
+    Nothing is read back by the host.  new_lens and new_pool must not be kv_lens and pool.  Without ``out`` the four results share one
+    allocation: any of them keeps (and torch.save stores) all.  See tiled_sdpa_cache_step."""
     return _checked(_calls().cache_step(kv_lens, counts, S, block_rows, pages, depths, out))
 
 
