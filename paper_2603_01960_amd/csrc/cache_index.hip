@@ -3,7 +3,10 @@
 //
 // Both are a few kilobytes of work and bound by latency: one launch each, no atomics, no workspace, nothing that depends on
 // which workgroup runs first.  Kernel / whole call, us: masks of 1 tree of 15 tokens 1.8 / 4.8, of 64 trees of 255 3.7 / 4.8; steps
-// of 1 entry and token 2.8 / 4.9, of 256 entries of up to 60 tokens 4.1 / 5.0 (an empty kernel's call: 3.7 to 4.5).
+// of 1 entry and token 2.8 / 4.5 to 5.3, of 256 entries of up to 60 tokens 4.1 / 4.6 to 5.3 (an empty kernel's call: 3.7 to 4.5).
+// A step's sums are every workgroup's own, so that its time grows with the square of the entries: 16 tokens each, all appended /
+// 64 tokens at most, a quarter of the entries giving a page up to the others, a call in us: 32 entries 3.8 / 7.3, 256 3.9 / 7.9, 1024
+// 6.5 / 12, 4096 25 / 66, 8192 102 / 374.  (The pages handed over cost a sum over the threads one by one, and a search per page.)
 #include "tiled_sdpa.h"
 
 #include <cstdint>

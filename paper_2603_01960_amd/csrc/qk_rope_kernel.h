@@ -16,9 +16,10 @@
 //   * a wavefront stays with one token and goes through its heads, so that the angles are computed once for all of them:
 //     in 64 bits up to whole turns (a position of 2^31 has no fraction left in 32), then sine and cosine of the rest;
 //   * the next row group's loads are on their way while one is worked on.
-// Kernels, us and TB/s of what they have to read and write (a copy of 1 GiB: 5.2, of 64 MiB 8.0): forward B=2 S=8192 H=32+8 D=128 BF16 62, 5.4;
-// B=64 S=197 H=12+12 D=64 FP16 15, 5.1; into a cache B=4 S=512 H=32+8 D=128 BF16 10, 4.9, one token of it 3.0; backward of the first 88, 5.8
-// (and 4.6 for the weights' sums), B=4 S=2048 H=16+4 D=160 FP16 32, 5.0.
+// Kernels, us and TB/s of what they have to read and write, on three sets of tensors in turn (in brackets a copy of as many bytes, likewise):
+// forward B=2 S=8192 H=32+8 D=128 BF16 64, 5.3 (5.3); B=64 S=197 H=12+12 D=64 FP16 15, 5.0 (6.7); into a cache B=4 S=512 H=32+8 D=128 BF16
+// 10, 4.9 (6.3), one token of it 3.2; backward of the first 90, 5.6 (5.3), and 4.6 for the weights' sums, B=4 S=2048 H=16+4 D=160 FP16 35, 4.5
+// (5.1).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

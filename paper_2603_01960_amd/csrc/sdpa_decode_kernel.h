@@ -152,7 +152,7 @@ template <> struct DecodeRead<160> {
 // see pick_halves (an instantiation of its own: the code alone costs the shortest calls 0.3 us).  TREE: the queries are a tree of drafted
 // tokens (see the forward kernel's); of at most 32 rows the tree has at most 32 tokens, and a row's bits are one word, which a tile
 // shifts to where its keys lie.  (us, tree / causal mask, BF16, 32 query heads over 8, D = 128: 32 entries of 4 tokens, 4096 keys 92.3 / 92.2,
-// 5.8 TB/s; of 8 tokens 98.5 / 95.9; 1 entry of 4 tokens, 8192 keys 14.2 / 14.0.)
+// 5.8 TB/s; of 8 tokens 99.5 / 95.0; 1 entry of 4 tokens, 8192 keys 14.2 / 14.0.)
 template <typename T, int D, int NQ, int NW, bool PAGED, bool HALVES, bool TREE = false>
 __global__ void __launch_bounds__(NW * 64, 2)
 sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v,
