@@ -14,8 +14,9 @@
  * The call surface mirrors the functional API of Section 4.2.1,
  * sdpa(q, k, v, causal, scale) -> o; causal = true is TSDPA_FLAG_CAUSAL of tiled_sdpa_fwd_ex.
  *
- * Beside it: attention over dense and paged caches, of trees of drafted tokens, the backward pass; and what a serving or training step
- * does around attention: the trees' masks, a cache's pages and slots, norm and rotation of queries and keys.
+ * Beside it: attention over dense and paged caches, of 16 or 8 bits, of trees of drafted tokens, the backward pass; and what a serving or
+ * training step does around attention: the trees' masks, a cache's pages and slots, norm and rotation of queries and keys, writing to and
+ * reading from a cache of 8 bits.
  *
  * All pointers are DEVICE pointers owned by the caller.  The library allocates
  * and frees nothing, keeps no state besides its kernel table, never
@@ -500,6 +501,81 @@ int tiled_sdpa_qk_norm_rope_bwd(const tsdpa_rope *p, const void *dq_out, const v
                                 const tsdpa_rows *dq, const tsdpa_rows *dk, void *dq_weight, void *dk_weight,
                                 void *workspace, unsigned long long workspace_bytes, void *stream);
 unsigned long long tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(int B, int S, int D);
+
+/*
+ * ---- A cache of 8 bits: half the bytes of a 16-bit one to read in a decoding step, and to hold.
+ *
+ * A value is code * 2^E.  Codes are E4M3 (sign, four bits of exponent, three of mantissa; largest 448; 0x7f and 0xff are NaN, there is no
+ * infinity); 32 consecutive rows (0 ... 31, 32 ... 63, ... of an entry) of a head of K share one E, and of V another, kept as the byte
+ * E + 127, -62 <= E <= 62 (other bytes count as the nearest of these).  A power of two, because the codes are floating point themselves: a
+ * finer scale would gain the top of their range at most, and products with this one are exact.  What is stored is within 2^-4 of a value,
+ * or within 2^-10 * 2^E if it is smaller than that, and E is the least with which the largest magnitude of the 32 rows (so far) is at
+ * most 448 * 2^E: the values of a head's 32 rows keep their four significant bits down to 2^-14 of the largest one's magnitude or less.
+ */
+typedef struct {
+    void *k, *v;                 /* device, codes [pages, Hkv, block_rows, D], 16-byte aligned */
+    unsigned char *k_scales, *v_scales;   /* device, E + 127, [pages, Hkv, ceil(block_rows / 32)] */
+    const int *block_table;      /* NULL: a dense cache, pages = B, entry b's rows in page b; else device int32 [B, max_blocks], as for
+                                    tiled_sdpa_fwd_paged: block_rows is then 64, 128, 256, ... */
+    int pages, Hkv, block_rows;
+    int D;                       /* 64, 96, 128 or 160 */
+    int max_blocks;
+} tsdpa_cache8;
+
+/*
+ * Keys and values of a step's tokens into the cache.
+ *
+ *   k, v      : tsdpa_rows of [B, S, Hkv, D], of type dtype (TSDPA_F16 or TSDPA_BF16).
+ *   kv_lens   : device int32 [B]: rows of each entry before the step.
+ *   new_lens  : device int32 [B]: rows after it (tiled_sdpa_cache_step): token i of entry b is row new_lens[b] - S + i, and is written if that is
+ *               kv_lens[b] or more (entries with fewer than S new tokens have them at the end), and below the capacity (block_rows, or
+ *               max_blocks * block_rows).  new_lens[b] <= kv_lens[b], as of a refused step or a drop: nothing is written for the entry.
+ *
+ * Why lengths and not slots: the tokens that share a scale have to be known together.  Of each block of 32 rows that gets a token, E becomes the
+ * least that its new rows need, or, if rows of the block lie below kv_lens[b], what it was if that is more.  Where it grows, these rows
+ * keep their values: their codes become code * 2^(old E - new E), rounded (exact but for codes that leave the normal range, below 2^-6).
+ * (E of a block falls only when its rows are written from the first on, new: dropped rows leave it as it is.)  Values go to the nearest
+ * code, of two equally near ones to that with the even mantissa; magnitudes beyond 448 * 2^62 to the largest, NaN and infinities to NaN,
+ * and neither counts for E.  Rows from new_lens[b] on are left as they are, byte for byte; so is what other entries hold, as long as no
+ * page is in two entries.  A page number that is none (below 0 or from `pages` on) is not written to.  The cache must not overlap the inputs.
+ *
+ * Validation order, of all calls of this section: null structs, dtype, D, shape, empty problem, null pointers, alignment, strides, scale,
+ * splits, workspace, launch.
+ */
+int tiled_sdpa_cache8_write(const tsdpa_cache8 *c, const tsdpa_rows *k, const tsdpa_rows *v, const int *kv_lens, const int *new_lens,
+                            int B, int S, int dtype, void *stream);
+
+/*
+ * Rows of the cache, back in 16 bits: what the calls over a 16-bit cache take, or tokens that are to be written to other rows (the accepted
+ * path of a tree: read it, then write it behind the rows from before the tree).
+ *
+ *   slots        : device int32 [B, n] (as of tiled_sdpa_cache_step): page * block_rows + row in the page.  A slot that is negative or past
+ *                  the last page's gives zeros.
+ *   k_out, v_out : [B, Hkv, n, D], of type dtype, 16-byte aligned; must overlap neither each other nor the cache.  code * 2^E is exact in
+ *                  both types but for what lies outside of FP16's range (below 2^-14, from 65520 on: rounded).
+ *   c            : block_table and max_blocks are not looked at; block_rows may be any number; pages * block_rows fits an int.
+ */
+int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out, void *v_out, int B, int n, int dtype, void *stream);
+
+/*
+ * Attention over the cache: tiled_sdpa_fwd_kvcache (c->block_table NULL) or tiled_sdpa_fwd_paged on the values that the codes stand for.
+ *
+ *   q, o         : [B, H, Sq, D], of type dtype, contiguous, 16-byte aligned; H % Hkv == 0, query head h reads head h / (H / Hkv).
+ *   lse          : NULL or FP32 [B, H, Sq].
+ *   kv_lens      : device int32 [B], rows of each entry, clamped to [0, capacity]; of a dense cache NULL = all of them hold block_rows.
+ *   flags        : TSDPA_FLAG_CAUSAL (the queries are the last Sq positions: needs a capacity of Sq or more) or 0.
+ *   splits, workspace : as for tiled_sdpa_fwd_kv; 0 = tiled_sdpa_cache8_default_splits of the capacity, or fewer, as many as the workspace
+ *                  has room for.  tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, n) bytes hold n.
+ *
+ * Scores and sums are FP32.  K is multiplied as 16-bit numbers of q's type, which its codes are; the weights are rounded to FP16 for the
+ * product with V, each times its scale, against the greatest such product of the row, so that what contributes most keeps 11 bits.
+ * A row that no key reaches gets O = 0 and LSE = -infinity.  Keys that a row does not see do not reach it, NaN among their values included.
+ * Page numbers that are none count as the nearest one that is.
+ */
+int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *lse, const int *kv_lens, int B, int H, int Sq, float scale,
+                          int dtype, unsigned flags, int splits, void *workspace, unsigned long long workspace_bytes, void *stream);
+
+int tiled_sdpa_cache8_default_splits(int B, int H, int Hkv, int Sq, int Skv, int D, int dtype, unsigned flags, int *splits);
 
 /*
  * Measurement aid, not part of the attention path: enqueue a register-resident stream of

@@ -9,4 +9,5 @@ from .binding import (  # noqa: F401
     probe_mfma, probe_hbm_read, tune_tile, sdpa, sdpa_kv, sdpa_paged, status_string, tiled_sdpa_fwd, tiled_sdpa_fwd_ex, tiled_sdpa_fwd_kv,
     tiled_sdpa_fwd_gqa, tiled_sdpa_fwd_kvcache, tiled_sdpa_fwd_kvcache_static, tiled_sdpa_fwd_paged, version,
     sdpa_tree, sdpa_tree_paged, tree_mask, cache_step, qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward,
+    cache8_write, cache8_read, sdpa_kv8, sdpa_paged8, cache8_default_splits,
 )

@@ -3,8 +3,8 @@
 Every step of the forward pass runs in the HIP kernels behind the C-ABI declared
 in include/tiled_sdpa.h.  PyTorch supplies device memory and the current stream.
 The tensor functions (sdpa, sdpa_kv, sdpa_paged, sdpa_backward, sdpa_tree, sdpa_tree_paged; tree_mask, cache_step,
-qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward around them) go through native
-code (csrc/torch_calls.cpp), the C-ABI itself is exposed through ctypes.
+qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward around them; cache8_write, cache8_read, sdpa_kv8, sdpa_paged8 of
+8-bit caches) go through native code (csrc/torch_calls.cpp), the C-ABI itself is exposed through ctypes.
 There is no CPU fallback: if the library is missing, loading raises.
 """
 from __future__ import annotations
@@ -48,6 +48,10 @@ EXPORTS = (
     "tiled_sdpa_qk_norm_rope_cache",
     "tiled_sdpa_qk_norm_rope_bwd",
     "tiled_sdpa_qk_norm_rope_bwd_workspace_bytes",
+    "tiled_sdpa_cache8_write",
+    "tiled_sdpa_cache8_read",
+    "tiled_sdpa_fwd_cache8",
+    "tiled_sdpa_cache8_default_splits",
     "tiled_sdpa_kv_default_splits",
     "tiled_sdpa_kv_tile_splits",
     "tiled_sdpa_kv_workspace_bytes",
@@ -76,6 +80,13 @@ class Rope(ctypes.Structure):
                 ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("pos_batch", ctypes.c_longlong), ("pos_axis", ctypes.c_longlong), ("inv_freq", ctypes.c_void_p), ("axes", ctypes.c_void_p),
                 ("n_axes", ctypes.c_int)]
+
+
+class Cache8(ctypes.Structure):
+    """tsdpa_cache8: an 8-bit cache, dense or paged."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("block_rows", ctypes.c_int),
+                ("D", ctypes.c_int), ("max_blocks", ctypes.c_int)]
 
 
 def library_path() -> Path:
@@ -146,6 +157,15 @@ def load_library():
     lib.tiled_sdpa_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(Rope), vp, vp, rows, rows, rows, rows, vp, vp, vp, ctypes.c_ulonglong, vp]
     lib.tiled_sdpa_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_ulonglong
     lib.tiled_sdpa_qk_norm_rope_bwd_workspace_bytes.argtypes = [ci, ci, ci]
+    cache8 = ctypes.POINTER(Cache8)
+    lib.tiled_sdpa_cache8_write.restype = ci
+    lib.tiled_sdpa_cache8_write.argtypes = [cache8, rows, rows, vp, vp, ci, ci, ci, vp]
+    lib.tiled_sdpa_cache8_read.restype = ci
+    lib.tiled_sdpa_cache8_read.argtypes = [cache8, vp, vp, vp, ci, ci, ci, vp]
+    lib.tiled_sdpa_fwd_cache8.restype = ci
+    lib.tiled_sdpa_fwd_cache8.argtypes = [cache8] + [vp] * 4 + [ci] * 3 + [cf, ci, ctypes.c_uint, ci, vp, ctypes.c_ulonglong, vp]
+    lib.tiled_sdpa_cache8_default_splits.restype = ci
+    lib.tiled_sdpa_cache8_default_splits.argtypes = [ci] * 7 + [ctypes.c_uint, ctypes.POINTER(ci)]
     lib.tiled_sdpa_probe_hbm_read.restype = ci
     lib.tiled_sdpa_probe_hbm_read.argtypes = [vp, ctypes.c_ulonglong, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.tiled_sdpa_probe_mfma.restype = ci
@@ -415,6 +435,56 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, i
     other, nor with what the call reads); the weights' gradients are
     in the weights' dtype, None where there is no weight.  See tiled_sdpa_qk_norm_rope_bwd."""
     return _checked(_calls().qk_norm_rope_backward(q, k, q_weight, k_weight, positions, inv_freq, axes, eps, interleaved, dq_out, dk_out, workspace, grads))
+
+
+SCALE_ROWS = 32       # rows of an 8-bit cache that share a scale
+
+
+def cache8_write(k, v, k_cache, v_cache, k_scales, v_scales, kv_lens, new_lens, *, block_table=None):
+    """Keys and values of a step's tokens, k, v [B, S, Hkv, D] (float16 or bfloat16; views of a projection, or of :func:`qk_norm_rope`'s k as
+    ``k.transpose(1, 2)``: strides in multiples of 8 elements), into an 8-bit cache: ``k_cache``, ``v_cache`` float8_e4m3fn
+    [B, Hkv, Skv, D], or [pages, Hkv, block_rows, D] with ``block_table`` int32 [B, max_blocks]; ``k_scales``, ``v_scales`` uint8 (or
+    float8_e8m0fnu) [pages, Hkv, ceil(block_rows / 32)], the exponent of a power of two for each head's 32 rows, plus 127.
+
+    ``kv_lens``, ``new_lens`` int32 [B]: an entry's rows before and after the step (of :func:`cache_step`); token i of entry b is row
+    new_lens[b] - S + i if that is kv_lens[b] or more.  The scale of a block of 32 rows grows as its rows need; the rows that it has
+    already then keep their values.  See tiled_sdpa_cache8_write."""
+    _checked(_calls().cache8_write(k_cache, v_cache, k_scales, v_scales, k, v, kv_lens, new_lens, block_table))
+
+
+def cache8_read(k_cache, v_cache, k_scales, v_scales, slots, dtype, *, out=None):
+    """(k, v) [B, Hkv, n, D] in ``dtype`` (torch.float16 or torch.bfloat16): the rows ``slots`` (int32 [B, n], page * block_rows + row, as of
+    :func:`cache_step`; rows of zeros where negative) of an 8-bit cache.  ``out=(k, v)`` must overlap neither each other nor the
+    cache.  See tiled_sdpa_cache8_read."""
+    import torch
+
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("dtype must be float16 or bfloat16")
+    return _checked(_calls().cache8_read(k_cache, v_cache, k_scales, v_scales, slots, dtype == torch.bfloat16, out))
+
+
+def sdpa_kv8(q, k_cache, v_cache, k_scales, v_scales, causal: bool = False, scale=None, *, kv_lens=None, splits: int = 0,
+             return_lse: bool = False, out=None, workspace=None):
+    """:func:`sdpa_kv` over an 8-bit cache (see :func:`cache8_write`): q [B, H, Sq, D], ``k_cache``, ``v_cache`` [B, Hkv, Skv, D], H a multiple
+    of Hkv.  What a row does not see does not reach it, NaN included.  See tiled_sdpa_fwd_cache8."""
+    return _checked(_calls().sdpa_cache8(k_cache, v_cache, k_scales, v_scales, q, kv_lens, None, causal, scale, splits, return_lse, out, workspace))
+
+
+def sdpa_paged8(q, k_pages, v_pages, k_scales, v_scales, kv_lens, block_table, causal: bool = False, scale=None, *, splits: int = 0,
+                return_lse: bool = False, out=None, workspace=None):
+    """:func:`sdpa_paged` over an 8-bit cache: ``k_pages``, ``v_pages`` [P, Hkv, block_rows, D], ``block_table`` int32 [B, max_blocks]; otherwise
+    as :func:`sdpa_kv8`."""
+    if block_table is None:
+        raise ValueError("block_table must be a contiguous int32 tensor [B, max_blocks] on the device of the cache")
+    return _checked(_calls().sdpa_cache8(k_pages, v_pages, k_scales, v_scales, q, kv_lens, block_table, causal, scale, splits, return_lse, out, workspace))
+
+
+def cache8_default_splits(B: int, H: int, Hkv: int, Sq: int, Skv: int, D: int, dtype: int, flags: int = 0) -> int:
+    n = ctypes.c_int(0)
+    st = load_library().tiled_sdpa_cache8_default_splits(B, H, Hkv, Sq, Skv, D, dtype, flags, ctypes.byref(n))
+    if st != 0:
+        raise TiledSdpaError(st, status_string(st))
+    return n.value
 
 
 def bwd_workspace_bytes(B: int, H: int, S: int) -> int:

@@ -1,0 +1,446 @@
+// The 8-bit cache: writing a step's tokens to it, reading rows back, and the C-ABI of these and of attention over it (kernels of the
+// latter in sdpa_cache8_decode_kernel.h).  See include/tiled_sdpa.h.
+#include "tiled_sdpa.h"
+
+#include <cmath>
+#include <cstdint>
+#include <limits>
+
+#include "cache8_args.h"
+
+namespace tsdpa {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ int quotient(int n, const Divisor &d) { return (int)(__umulhi(2u * (unsigned)n, d.mul) >> d.shift); }
+
+// 2^e, -126 <= e <= 127
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (e + 127) << 23); }
+
+template <typename T> struct Half;
+template <> struct Half<_Float16> {
+    static constexpr uint32_t INF = 0x7c00u;
+    static __device__ __forceinline__ float value(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (unsigned short)bits); }
+};
+template <> struct Half<__bf16> {
+    static constexpr uint32_t INF = 0x7f80u;
+    static __device__ __forceinline__ float value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+};
+
+// The maximum over a wavefront's lanes, of numbers that are not negative: within rows of 16 lanes, then across them.
+__device__ __forceinline__ int lanes_max(int x)
+{
+#define TSDPA_MAX_STEP(ctrl, rows) { const int y = __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false); x = x > y ? x : y; }
+    TSDPA_MAX_STEP(0x111, 0xf) TSDPA_MAX_STEP(0x112, 0xf) TSDPA_MAX_STEP(0x114, 0xf) TSDPA_MAX_STEP(0x118, 0xf)      // row_shr
+    TSDPA_MAX_STEP(0x142, 0xa) TSDPA_MAX_STEP(0x143, 0xc)                                                          // row_bcast
+#undef TSDPA_MAX_STEP
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The least exponent E with which `largest` (not negative) is at most the largest code, 448 = 1.75 * 2^8, times 2^E.
+__device__ __forceinline__ int exponent_for(float largest)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, largest);
+    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return e < -kScaleMost ? -kScaleMost : (e < kScaleMost ? e : kScaleMost);
+}
+
+// One wavefront: the new rows of one block of 32 rows of one head of K or V, a block being what shares a scale.  It holds them in registers
+// between their largest magnitude and their codes, so that they are read once; the block's older rows are read only if the scale grows.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+cache8_write_kernel(Cache8Args c, Cache8Rows xk, Cache8Rows xv, const int *__restrict__ kv_lens, const int *__restrict__ new_lens, int S, int capacity,
+                    int windows, Divisor by_heads, Divisor by_windows, int units)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int CPR = D / 8, N = 32 * CPR / 64;  // 16-byte chunks of a row of x, and of the block per lane
+    const int lane = threadIdx.x & 63;
+    const int u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (u >= units) return;
+    int rest = quotient(u, by_heads);
+    const int h = u - rest * c.heads, tensor = rest & 1;
+    rest >>= 1;
+    const int b = quotient(rest, by_windows), w = rest - b * windows;
+    const int now = kv_lens[b] > 0 ? kv_lens[b] : 0, next = new_lens[b] < capacity ? new_lens[b] : capacity;
+    if (new_lens[b] <= 0) return;
+    const int before = new_lens[b] - S;            // row of token 0
+    const int lo = now > before ? now : before;
+    if (lo >= next) return;
+    const int row0 = (lo / kScaleRows + w) * kScaleRows;
+    if (row0 >= next) return;
+    const int first = lo > row0 ? lo : row0, end = next - row0 < kScaleRows ? next : row0 + kScaleRows;
+    const int held = (now < first ? now : first) - row0;         // rows of the block that the entry has already (if > 0)
+    int page = b, row = row0;
+    if (c.block_table != nullptr) {
+        const int shift = __builtin_ctz(c.block_rows);
+        page = c.block_table[(size_t)b * c.max_blocks + (row0 >> shift)];
+        if ((unsigned)page >= (unsigned)c.pages) return;          // (no memory of the cache's)
+        row = row0 & (c.block_rows - 1);
+    }
+    const size_t head = (size_t)page * c.heads + h;
+    unsigned char *codes = (unsigned char *)(tensor ? c.data[1] : c.data[0]) + (head * c.block_rows + row) * D;
+    unsigned char *scale = (tensor ? c.scales[1] : c.scales[0]) + head * c.blocks + row / kScaleRows;
+    const Cache8Rows x = tensor ? xv : xk;
+    const T *from = (const T *)x.data + b * x.batch + h * x.head;
+
+    u32x4 in[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int p = j * 64 + lane, r = row0 + p / CPR;
+        in[j] = u32x4{0u, 0u, 0u, 0u};
+        if (r >= first && r < end) in[j] = *(const u32x4 *)(from + (long long)(r - before) * x.row + p % CPR * 8);
+    }
+    const int was = held > 0 ? (int)*scale : 0;
+    u16x2 most = {0, 0};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t size = in[j][i] & 0x7fff7fffu;
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, size));
+        }
+    int largest = lanes_max(most[0] > most[1] ? most[0] : most[1]);
+    const bool finite = largest < (int)Half<T>::INF;
+    if (!finite) {                                // the largest of those that are
+        int own = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int size = (int)(in[j][i >> 1] >> (i & 1) * 16 & 0x7fffu);
+                own = size < (int)Half<T>::INF && size > own ? size : own;
+            }
+        largest = lanes_max(own);
+    }
+    int e = exponent_for(Half<T>::value((uint32_t)largest));
+    int old = was - kScaleBias;
+    old = old < -kScaleMost ? -kScaleMost : (old < kScaleMost ? old : kScaleMost);
+    if (held > 0 && old > e) e = old;
+    if (held > 0 && e > old) {
+        // the rows that are there already keep their values: code * 2^(old - e), rounded (exact but below the normal codes)
+        const float down = power_of_two(old - e);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            const int p = j * 64 + lane;
+            if (p / (D / 16) >= held) continue;
+            u32x4 *at = (u32x4 *)(codes + p * 16);
+            u32x4 y = *at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false), z = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
+                int out = __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * down, a[1] * down, 0, false);
+                y[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[0] * down, z[1] * down, out, true);
+            }
+            *at = y;
+        }
+    }
+    // new rows: x * 2^-e, at most 448 unless e is the largest exponent there is, to the nearest code, of two the even one
+    const float up = power_of_two(-e);
+    const bool plain = finite && e < kScaleMost;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int p = j * 64 + lane, r = row0 + p / CPR;
+        if (r < first || r >= end) continue;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = Half<T>::value(in[j][i >> 1] >> (i & 1) * 16 & 0xffffu) * up;
+        if (!plain) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool number = (in[j][i >> 1] >> (i & 1) * 16 & 0x7fffu) < Half<T>::INF;
+                const float cut = fminf(fmaxf(y[i], -448.f), 448.f);
+                y[i] = number ? cut : __builtin_nanf("");
+            }
+        }
+        u32x2 out;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int pair = __builtin_amdgcn_cvt_pk_fp8_f32(y[i * 4], y[i * 4 + 1], 0, false);
+            out[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[i * 4 + 2], y[i * 4 + 3], pair, true);
+        }
+        *(u32x2 *)(codes + p * 8) = out;
+    }
+    if (lane == 0) *scale = (unsigned char)(e + kScaleBias);
+#endif
+}
+
+// One thread: eight columns of one token, in HEADS heads of K and V.
+template <typename T, int D, int HEADS>
+__global__ void __launch_bounds__(256)
+cache8_read_kernel(Cache8Args c, const int *__restrict__ slots, T *__restrict__ k_out, T *__restrict__ v_out, int n, int tokens, Divisor by_n, Divisor by_rows)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef T vec8 __attribute__((ext_vector_type(8)));
+    constexpr int CPR = D / 8;
+    const int x = blockIdx.x * 256 + threadIdx.x;
+    const int token = x / CPR, col = x % CPR * 8;
+    if (token >= tokens) return;
+    const int slot = slots[token];
+    const int b = quotient(token, by_n), i = token - b * n;
+    const bool inside = slot >= 0 && slot < c.pages * c.block_rows;
+    const int page = inside ? quotient(slot, by_rows) : 0, row = inside ? slot - page * c.block_rows : 0;
+    const int h0 = blockIdx.y * HEADS;
+    u32x2 raw[HEADS][2];
+    int e[HEADS][2];
+#pragma unroll
+    for (int j = 0; j < HEADS; ++j) {
+        const int h = h0 + j < c.heads ? h0 + j : c.heads - 1;
+        const size_t head = (size_t)page * c.heads + h;
+#pragma unroll
+        for (int tensor = 0; tensor < 2; ++tensor) {
+            raw[j][tensor] = u32x2{0u, 0u};
+            e[j][tensor] = kScaleBias;
+            if (inside) {
+                raw[j][tensor] = *(const u32x2 *)((const unsigned char *)c.data[tensor] + (head * c.block_rows + row) * D + col);
+                e[j][tensor] = c.scales[tensor][head * c.blocks + row / kScaleRows];
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < HEADS; ++j) {
+        if (h0 + j >= c.heads) break;
+#pragma unroll
+        for (int tensor = 0; tensor < 2; ++tensor) {
+            int x8 = e[j][tensor];
+            x8 = x8 < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x8 < kScaleBias + kScaleMost ? x8 : kScaleBias + kScaleMost);
+            const float scale = __builtin_bit_cast(float, x8 << 23);
+            vec8 out;
+#pragma unroll
+            for (int i4 = 0; i4 < 2; ++i4) {
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(raw[j][tensor][i4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(raw[j][tensor][i4], true);
+                out[i4 * 4] = (T)(lo[0] * scale);
+                out[i4 * 4 + 1] = (T)(lo[1] * scale);
+                out[i4 * 4 + 2] = (T)(hi[0] * scale);
+                out[i4 * 4 + 3] = (T)(hi[1] * scale);
+            }
+            *(vec8 *)((tensor ? v_out : k_out) + (((size_t)b * c.heads + h0 + j) * n + i) * D + col) = out;
+        }
+    }
+#endif
+}
+
+template <typename T, int D> int launch_write(const Cache8Write &x)
+{
+    const long long units = (long long)x.B * x.windows * x.c.heads * 2;
+    hipLaunchKernelGGL((cache8_write_kernel<T, D>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, x.stream, x.c, x.x[0], x.x[1], x.kv_lens, x.new_lens, x.S,
+                       x.capacity, x.windows, divisor((uint32_t)x.c.heads), divisor((uint32_t)x.windows), (int)units);
+    return (int)hipGetLastError();
+}
+
+template <typename T, int D, int HEADS> int launch_read_heads(const Cache8Read &x)
+{
+    const int tokens = x.B * x.n;
+    hipLaunchKernelGGL((cache8_read_kernel<T, D, HEADS>), dim3((unsigned)(((long long)tokens * (D / 8) + 255) / 256), (unsigned)((x.c.heads + HEADS - 1) / HEADS)),
+                       dim3(256), 0, x.stream, x.c, x.slots, (T *)x.out[0], (T *)x.out[1], x.n, tokens, divisor((uint32_t)x.n), divisor((uint32_t)x.c.block_rows));
+    return (int)hipGetLastError();
+}
+
+template <typename T, int D> int launch_read(const Cache8Read &x) { return launch_read_heads<T, D, 1>(x); }
+
+template <typename T> int launch_write_dim(int D, const Cache8Write &x)
+{
+    switch (D) {
+        case 64: return launch_write<T, 64>(x);
+        case 96: return launch_write<T, 96>(x);
+        case 128: return launch_write<T, 128>(x);
+        default: return launch_write<T, 160>(x);
+    }
+}
+
+template <typename T> int launch_read_dim(int D, const Cache8Read &x)
+{
+    switch (D) {
+        case 64: return launch_read<T, 64>(x);
+        case 96: return launch_read<T, 96>(x);
+        case 128: return launch_read<T, 128>(x);
+        default: return launch_read<T, 160>(x);
+    }
+}
+
+}  // namespace tsdpa
+
+namespace {
+
+constexpr int64_t kMost = std::numeric_limits<int>::max();
+
+bool misaligned(const void *at, uintptr_t bytes) { return ((uintptr_t)at & (bytes - 1)) != 0; }
+
+// The cache's own numbers; capacity: rows that an entry can have.
+int check_cache(const tsdpa_cache8 &c, int B, bool tables, int *capacity)
+{
+    if (c.D != 64 && c.D != 96 && c.D != 128 && c.D != 160) return TSDPA_ERR_UNSUPPORTED_D;
+    if (B < 0 || c.pages < 0 || c.Hkv < 0 || c.block_rows < 0 || c.max_blocks < 0) return TSDPA_ERR_BAD_SHAPE;
+    if ((int64_t)c.pages * c.block_rows > kMost) return TSDPA_ERR_BAD_SHAPE;
+    *capacity = c.block_rows;
+    if (!tables) return TSDPA_OK;
+    if (c.block_table) {
+        // pages of 64 << n rows, so that no tile straddles two
+        if (c.block_rows < 64 || (c.block_rows & (c.block_rows - 1)) != 0 || (int64_t)c.max_blocks * c.block_rows > kMost) return TSDPA_ERR_BAD_SHAPE;
+        *capacity = c.max_blocks * c.block_rows;
+    } else if (c.pages != B) {
+        return TSDPA_ERR_BAD_SHAPE;
+    }
+    return TSDPA_OK;
+}
+
+bool bad_strides(const tsdpa_rows &r, int B, int S, int heads)
+{
+    const struct { long long stride; int size; } d[3] = {{r.batch, B}, {r.row, S}, {r.head, heads}};
+    for (const auto &x : d)
+        if (x.size > 1 && (x.stride < 0 || (x.stride & 7) != 0)) return true;      // (one row has no stride)
+    return false;
+}
+
+tsdpa::Cache8Args args_of(const tsdpa_cache8 &c)
+{
+    return tsdpa::Cache8Args{{c.k, c.v}, {c.k_scales, c.v_scales}, c.block_table, c.pages, c.Hkv, c.block_rows, tsdpa::scale_blocks(c.block_rows), c.max_blocks};
+}
+
+bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !c.v_scales; }
+
+// Splits along the key axis: two workgroups per CU in all, of two tiles or more.
+int pick_splits(int64_t tiles, int Skv)
+{
+    int64_t want = (512 + tiles - 1) / tiles;
+    const int64_t most = Skv / 128 > 1 ? Skv / 128 : 1;
+    if (want > most) want = most;
+    return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
+}
+
+int default_splits(int heads, int rows, int Skv)
+{
+    return pick_splits((int64_t)heads * ((rows + 15) / 16), Skv);
+}
+
+int check_attention(int B, int H, int Hkv, int Sq, int Skv, int D, int dtype, unsigned flags)
+{
+    if (dtype != TSDPA_F16 && dtype != TSDPA_BF16) return TSDPA_ERR_BAD_DTYPE;
+    if (D != 64 && D != 96 && D != 128 && D != 160) return TSDPA_ERR_UNSUPPORTED_D;
+    if (B < 0 || H < 0 || Hkv < 0 || Sq < 0 || Skv < 0) return TSDPA_ERR_BAD_SHAPE;
+    const int64_t bh = (int64_t)B * H;
+    // B * H * ceil(Sq / 16) * splits workgroups must fit an int
+    if (bh > kMost || (bh > 0 && Sq > 0 && ((int64_t)Sq + 15) / 16 > kMost / TSDPA_MAX_SPLITS / bh)) return TSDPA_ERR_BAD_SHAPE;
+    // a head is addressed through 32 bits, with room for a "fetch nothing" offset above it
+    if (((int64_t)Skv + 1024) * D >= ((int64_t)1 << 30)) return TSDPA_ERR_BAD_SHAPE;
+    if (bh > 0 && Sq > 0 && Skv == 0) return TSDPA_ERR_BAD_SHAPE;
+    if ((flags & TSDPA_FLAG_CAUSAL) && Skv < Sq) return TSDPA_ERR_BAD_SHAPE;
+    if (H > 0 && (Hkv == 0 || H % Hkv != 0)) return TSDPA_ERR_BAD_SHAPE;
+    if (H > 0 && (int64_t)(H / Hkv) * Sq > kMost) return TSDPA_ERR_BAD_SHAPE;
+    return TSDPA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tiled_sdpa_cache8_write(const tsdpa_cache8 *c, const tsdpa_rows *k, const tsdpa_rows *v, const int *kv_lens, const int *new_lens, int B, int S, int dtype,
+                            void *stream)
+{
+    if (!c || !k || !v) return TSDPA_ERR_NULL_PTR;
+    if (dtype != TSDPA_F16 && dtype != TSDPA_BF16) return TSDPA_ERR_BAD_DTYPE;
+    int capacity;
+    const int st = check_cache(*c, B, true, &capacity);
+    if (st != TSDPA_OK) return st;
+    if (S < 0) return TSDPA_ERR_BAD_SHAPE;
+    // (S tokens of an entry touch a block more than they fill if they begin inside one; none past the capacity)
+    const int64_t most = S < capacity ? S : capacity, windows = most <= 1 ? most : (most + 2 * (tsdpa::kScaleRows - 1)) / tsdpa::kScaleRows;
+    const int64_t per_entry = windows * c->Hkv;
+    if (B > 0 && per_entry > (kMost - 3) / 2 / B) return TSDPA_ERR_BAD_SHAPE;
+    if (B * per_entry == 0 || c->pages == 0) return TSDPA_OK;
+    if (incomplete(*c) || !k->data || !v->data || !kv_lens || !new_lens) return TSDPA_ERR_NULL_PTR;
+    if (misaligned(c->k, 16) || misaligned(c->v, 16) || misaligned(k->data, 16) || misaligned(v->data, 16) || misaligned(kv_lens, 4) || misaligned(new_lens, 4) ||
+        misaligned(c->block_table, 4))
+        return TSDPA_ERR_MISALIGNED;
+    if (bad_strides(*k, B, S, c->Hkv) || bad_strides(*v, B, S, c->Hkv)) return TSDPA_ERR_BAD_STRIDE;
+    tsdpa::Cache8Write x{args_of(*c), {{k->data, k->batch, k->row, k->head}, {v->data, v->batch, v->row, v->head}}, kv_lens, new_lens, B, S, capacity, (int)windows,
+                         (hipStream_t)stream};
+    const int err = dtype == TSDPA_F16 ? tsdpa::launch_write_dim<_Float16>(c->D, x) : tsdpa::launch_write_dim<__bf16>(c->D, x);
+    return err == 0 ? TSDPA_OK : TSDPA_ERR_LAUNCH;
+}
+
+int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out, void *v_out, int B, int n, int dtype, void *stream)
+{
+    if (!c) return TSDPA_ERR_NULL_PTR;
+    if (dtype != TSDPA_F16 && dtype != TSDPA_BF16) return TSDPA_ERR_BAD_DTYPE;
+    int capacity;
+    const int st = check_cache(*c, B, false, &capacity);
+    if (st != TSDPA_OK) return st;
+    if (n < 0 || (int64_t)B * n > kMost / (c->D / 8) - 256 || c->Hkv > 65535) return TSDPA_ERR_BAD_SHAPE;
+    if ((int64_t)B * n == 0 || c->Hkv == 0) return TSDPA_OK;
+    // (a cache without rows has no memory: every slot lies past its end)
+    if (!slots || !k_out || !v_out || (capacity > 0 && c->pages > 0 && incomplete(*c))) return TSDPA_ERR_NULL_PTR;
+    if (misaligned(c->k, 16) || misaligned(c->v, 16) || misaligned(k_out, 16) || misaligned(v_out, 16) || misaligned(slots, 4)) return TSDPA_ERR_MISALIGNED;
+    tsdpa::Cache8Read x{args_of(*c), slots, {k_out, v_out}, B, n, (hipStream_t)stream};
+    if (x.c.block_rows < 1) x.c.pages = 0, x.c.block_rows = 1;
+    const int err = dtype == TSDPA_F16 ? tsdpa::launch_read_dim<_Float16>(c->D, x) : tsdpa::launch_read_dim<__bf16>(c->D, x);
+    return err == 0 ? TSDPA_OK : TSDPA_ERR_LAUNCH;
+}
+
+int tiled_sdpa_cache8_default_splits(int B, int H, int Hkv, int Sq, int Skv, int D, int dtype, unsigned flags, int *splits)
+{
+    if (!splits) return TSDPA_ERR_NULL_PTR;
+    const int st = check_attention(B, H, Hkv, Sq, Skv, D, dtype, flags);
+    if (st != TSDPA_OK) return st;
+    *splits = (int64_t)B * H * Sq == 0 ? 1 : default_splits(B * Hkv, H / Hkv * Sq, Skv);
+    return TSDPA_OK;
+}
+
+int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *lse, const int *kv_lens, int B, int H, int Sq, float scale, int dtype,
+                          unsigned flags, int splits, void *workspace, unsigned long long workspace_bytes, void *stream)
+{
+    if (!c) return TSDPA_ERR_NULL_PTR;
+    if (dtype != TSDPA_F16 && dtype != TSDPA_BF16) return TSDPA_ERR_BAD_DTYPE;
+    int capacity;
+    int st = check_cache(*c, B, true, &capacity);
+    if (st == TSDPA_OK) st = check_attention(B, H, c->Hkv, Sq, capacity, c->D, dtype, flags);
+    if (st != TSDPA_OK) return st;
+    if ((int64_t)B * H * Sq == 0) return TSDPA_OK;
+    if (!q || !o || incomplete(*c) || (c->block_table && !kv_lens)) return TSDPA_ERR_NULL_PTR;
+    if (c->pages == 0) return TSDPA_ERR_BAD_SHAPE;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(c->k, 16) || misaligned(c->v, 16) || misaligned(lse, 4) || misaligned(kv_lens, 4) ||
+        misaligned(c->block_table, 4))
+        return TSDPA_ERR_MISALIGNED;
+    if (std::isnan(scale)) scale = 1.0f / std::sqrt((float)c->D);
+    if (std::isinf(scale)) return TSDPA_ERR_BAD_SCALE;
+    if (splits < 0 || splits > TSDPA_MAX_SPLITS) return TSDPA_ERR_BAD_SPLITS;
+    const int rows = H / c->Hkv * Sq, heads = B * c->Hkv;
+    if (splits == 0) {
+        splits = default_splits(heads, rows, capacity);
+        // (with less memory than that takes: as many as fit)
+        const unsigned long long each = tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, 2) / 2, given = workspace ? workspace_bytes / each : 0;
+        if ((unsigned long long)splits > given) splits = given > 1 ? (int)given : 1;
+    }
+    if (splits > 1 && (!workspace || misaligned(workspace, 16) || workspace_bytes < tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, splits)))
+        return TSDPA_ERR_WORKSPACE;
+    tsdpa::Cache8Attend x{args_of(*c), {}};
+    tsdpa::LaunchArgs &a = x.a;
+    a.q = q;
+    a.o = o;
+    a.lse = lse;
+    a.BH = heads;
+    a.S = rows;
+    a.rows_per_head = Sq;
+    a.kv_lens = kv_lens;
+    a.heads_per_batch = c->Hkv;
+    a.batches = B;
+    a.c = std::fabs(scale) * 1.44269504088896340736f;
+    a.qsign = std::signbit(scale) && scale != 0.0f ? 0x80008000u : 0u;
+    a.causal = (flags & TSDPA_FLAG_CAUSAL) ? 1 : 0;
+    a.kv = 1;
+    a.Skv = capacity;
+    a.splits = splits;
+    a.ws = (float *)workspace;
+    a.stream = (hipStream_t)stream;
+    const int err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_decode_f16(c->D, x) : tsdpa::launch_cache8_decode_bf16(c->D, x);
+    if (err != 0) return TSDPA_ERR_LAUNCH;
+    if (splits > 1) {
+        tsdpa::merge_states(a, c->D, dtype, (int64_t)heads * rows <= 2048);
+        if (hipGetLastError() != hipSuccess) return TSDPA_ERR_LAUNCH;
+    }
+    return TSDPA_OK;
+}
+
+}  // extern "C"

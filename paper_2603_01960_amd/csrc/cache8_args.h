@@ -1,0 +1,56 @@
+// The 8-bit cache: what host code and kernels share.  See include/tiled_sdpa.h for the format.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "sdpa_fwd_launch.h"
+
+namespace tsdpa {
+
+constexpr int kScaleRows = 32;                    // rows of a head that share a scale
+// Exponents of scales: what is multiplied and summed with two of them stays far from the ends of FP32.  The weight of a key that matters,
+// 2^0 ... 2^-24 of the row's, times 2^(difference of two exponents, 124 at most) is a normal FP32 number.
+constexpr int kScaleMost = 62, kScaleBias = 127;
+
+inline int scale_blocks(int rows) { return rows / kScaleRows + (rows % kScaleRows != 0); }
+
+struct Cache8Args {
+    void *data[2];                                // K, V
+    unsigned char *scales[2];
+    const int *block_table;                       // NULL: dense
+    int pages, heads, block_rows, blocks;         // blocks: scales per head and page
+    int max_blocks;
+};
+
+struct Cache8Rows { const void *data; long long batch, row, head; };
+
+struct Cache8Write {
+    Cache8Args c;
+    Cache8Rows x[2];
+    const int *kv_lens, *new_lens;
+    int B, S, capacity;
+    int windows;                                  // blocks of 32 rows that an entry's S tokens can touch
+    hipStream_t stream;
+};
+
+struct Cache8Read {
+    Cache8Args c;
+    const int *slots;
+    void *out[2];
+    int B, n;
+    hipStream_t stream;
+};
+
+struct Cache8Attend {
+    Cache8Args c;
+    LaunchArgs a;                                 // q, o, lse, BH, S, rows_per_head, kv_lens, heads_per_batch, batches, c, qsign, causal, Skv, splits, ws, ticket, stream
+};
+
+int launch_cache8_decode_f16(int D, const Cache8Attend &x);
+int launch_cache8_decode_bf16(int D, const Cache8Attend &x);
+
+// In tiled_sdpa.hip: the states of a.splits runs combined, and a number that no other call has.
+void merge_states(const LaunchArgs &a, int D, int dtype, bool wide);
+unsigned long long new_ticket();
+
+}  // namespace tsdpa

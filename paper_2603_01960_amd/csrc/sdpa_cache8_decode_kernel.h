@@ -1,0 +1,610 @@
+// Attention of few query rows (16 or 32 per workgroup, the grouped query heads' rows together) over an 8-bit cache.
+//
+// The values of a cache are code * 2^E, E4M3 codes, one E for each head and 32 rows of K, one of V.  With c = scale * log2(e)
+//     s_j = <q, codes of key j>,   p_j = 2^(s_j * (c * 2^EK) + EV - m),   o = sum_j p_j * codes of value j,   l = sum_j p_j * 2^-EV,
+// and O = o / l: the scales cost nothing per value.  EK folds into the factor of the score, EV into the exponent, so that m is the greatest
+// score PLUS exponent seen: the weights that enter the products are sized by what they contribute, and the products, whose weights and
+// values are both FP16 here whatever the type of q (every code is an FP16 number), keep 11 bits of the largest contributions.  l takes
+// the exponent out again, in FP32.
+//
+// Such a call is bound by reading the cache once.  As in sdpa_decode_kernel.h each wavefront streams tiles of its own through LDS slots
+// of its own, with no barrier in the loop: one slot for K and one for V, each refilled as soon as it has been read into registers.  A
+// tile is 64 keys, as many bytes as 32 keys of 16 bits, so that as many are in flight.
+#pragma once
+#include "cache8_args.h"
+#include "sdpa_fwd_kernel.h"
+
+namespace tsdpa {
+
+constexpr int kTile8 = 64;                        // keys per tile
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+// Eight codes as eight 16-bit numbers (exact).
+template <typename T> struct Codes;
+template <> struct Codes<_Float16> {
+    static __device__ __forceinline__ f16x8 wide(uint32_t lo, uint32_t hi)
+    {
+        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+};
+template <> struct Codes<__bf16> {
+    static __device__ __forceinline__ bf16x8 wide(uint32_t lo, uint32_t hi)
+    {
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+};
+
+// LDS layout of a tile: 64 rows of D bytes, unpadded; 16-byte chunks are permuted within each row (chunk c at c ^ swizzle(row)).
+//   K: 16 lanes read one chunk of 16 consecutive rows.
+//   V: the transposing read has 32 lanes fetch one chunk of 16 rows, 4 at a time: 0 ... 7 and 16 ... 23, or those plus 8.
+// Both land on 16 different 16-byte slots of the 64 banks.  Rows of 96 and 160 bytes start on 8 different even slots, eight rows in turn: there
+// the lowest bit of the chunk tells the two eights apart.
+template <int D> struct Geom8 {
+    static constexpr int ROW = D, CPR = D / 16;
+    static constexpr int TILE = kTile8 * ROW;
+    static constexpr int UNITS = TILE / 1024;     // direct-to-LDS load instructions per tile
+    static constexpr int P = UNITS / 2;           // ... per 32 rows, after which the lanes' offsets repeat
+    static __host__ __device__ constexpr int kx(int r) { return D == 128 ? (r >> 1) & 7 : D == 64 ? (r >> 2) & 3 : (r >> 3) & 1; }
+    static __host__ __device__ constexpr int vx(int r)
+    {
+        return D == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : D == 64 ? ((r >> 2) & 1) | ((r >> 4) & 1) << 1 : (r >> 4) & 1;
+    }
+    static constexpr int KC = D / 64;             // 16-byte pieces of K per lane and row block; D % 64 = 32: and one of 8
+    static constexpr bool TAIL = D % 64 != 0;
+    static constexpr int NKP = (D == 128 ? 2 : 1) + (TAIL ? 1 : 0);       // pointers of K's reads (the tail's is the last)
+    static constexpr int NVP = D == 128 ? 8 : D == 64 ? 4 : 2;            // ... of V's: one per 16 columns, or per parity of these
+};
+
+// The reads of one tile and the wait for them, in one block of inline assembly each (see DecodeRead in sdpa_decode_kernel.h for why).
+//   keys:   x[b][h] = 16 bytes at row block b (16 rows), y[b] = 8 bytes of the tail
+//   values: x[db][kb] = transposing read of 16 columns, 32 rows
+#define TSDPA_RD_K(i, a, off) "ds_read_b128 %" #i ", %" #a " offset:" #off "\n\t"
+#define TSDPA_RD_K8(i, a, off) "ds_read_b64 %" #i ", %" #a " offset:" #off "\n\t"
+#define TSDPA_RD_V(i, a, off) "ds_read_b64_tr_b8 %" #i ", %" #a " offset:" #off "\n\t"
+#define TSDPA_RD_WAIT "s_waitcnt lgkmcnt(0)"
+template <int D> struct Read8;
+template <> struct Read8<64> {
+    static __device__ __forceinline__ void keys(u32x4 (&x)[4][1], u32x2 (&)[4], const uint32_t (&p)[1])
+    {
+        asm volatile(TSDPA_RD_K(0, 4, 0) TSDPA_RD_K(1, 4, 1024) TSDPA_RD_K(2, 4, 2048) TSDPA_RD_K(3, 4, 3072) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[1][0]), "=&v"(x[2][0]), "=&v"(x[3][0])
+                     : "v"(p[0])
+                     : "memory");
+    }
+    static __device__ __forceinline__ void values(u32x2 (&x)[4][2], const uint32_t (&p)[4])
+    {
+        asm volatile(TSDPA_RD_V(0, 8, 0) TSDPA_RD_V(1, 8, 2048) TSDPA_RD_V(2, 9, 0) TSDPA_RD_V(3, 9, 2048)
+                     TSDPA_RD_V(4, 10, 0) TSDPA_RD_V(5, 10, 2048) TSDPA_RD_V(6, 11, 0) TSDPA_RD_V(7, 11, 2048) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+                       "=&v"(x[3][0]), "=&v"(x[3][1])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3])
+                     : "memory");
+    }
+};
+template <> struct Read8<96> {
+    static __device__ __forceinline__ void keys(u32x4 (&x)[4][1], u32x2 (&y)[4], const uint32_t (&p)[2])
+    {
+        asm volatile(TSDPA_RD_K(0, 8, 0) TSDPA_RD_K(1, 8, 1536) TSDPA_RD_K(2, 8, 3072) TSDPA_RD_K(3, 8, 4608)
+                     TSDPA_RD_K8(4, 9, 0) TSDPA_RD_K8(5, 9, 1536) TSDPA_RD_K8(6, 9, 3072) TSDPA_RD_K8(7, 9, 4608) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[1][0]), "=&v"(x[2][0]), "=&v"(x[3][0]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+                     : "v"(p[0]), "v"(p[1])
+                     : "memory");
+    }
+    static __device__ __forceinline__ void values(u32x2 (&x)[6][2], const uint32_t (&p)[2])
+    {
+        asm volatile(TSDPA_RD_V(0, 12, 0) TSDPA_RD_V(1, 12, 3072) TSDPA_RD_V(2, 13, 0) TSDPA_RD_V(3, 13, 3072)
+                     TSDPA_RD_V(4, 12, 32) TSDPA_RD_V(5, 12, 3104) TSDPA_RD_V(6, 13, 32) TSDPA_RD_V(7, 13, 3104)
+                     TSDPA_RD_V(8, 12, 64) TSDPA_RD_V(9, 12, 3136) TSDPA_RD_V(10, 13, 64) TSDPA_RD_V(11, 13, 3136) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+                       "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1]), "=&v"(x[5][0]), "=&v"(x[5][1])
+                     : "v"(p[0]), "v"(p[1])
+                     : "memory");
+    }
+};
+template <> struct Read8<128> {
+    static __device__ __forceinline__ void keys(u32x4 (&x)[4][2], u32x2 (&)[4], const uint32_t (&p)[2])
+    {
+        asm volatile(TSDPA_RD_K(0, 8, 0) TSDPA_RD_K(1, 9, 0) TSDPA_RD_K(2, 8, 2048) TSDPA_RD_K(3, 9, 2048)
+                     TSDPA_RD_K(4, 8, 4096) TSDPA_RD_K(5, 9, 4096) TSDPA_RD_K(6, 8, 6144) TSDPA_RD_K(7, 9, 6144) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+                       "=&v"(x[3][0]), "=&v"(x[3][1])
+                     : "v"(p[0]), "v"(p[1])
+                     : "memory");
+    }
+    static __device__ __forceinline__ void values(u32x2 (&x)[8][2], const uint32_t (&p)[8])
+    {
+        asm volatile(TSDPA_RD_V(0, 16, 0) TSDPA_RD_V(1, 16, 4096) TSDPA_RD_V(2, 17, 0) TSDPA_RD_V(3, 17, 4096)
+                     TSDPA_RD_V(4, 18, 0) TSDPA_RD_V(5, 18, 4096) TSDPA_RD_V(6, 19, 0) TSDPA_RD_V(7, 19, 4096)
+                     TSDPA_RD_V(8, 20, 0) TSDPA_RD_V(9, 20, 4096) TSDPA_RD_V(10, 21, 0) TSDPA_RD_V(11, 21, 4096)
+                     TSDPA_RD_V(12, 22, 0) TSDPA_RD_V(13, 22, 4096) TSDPA_RD_V(14, 23, 0) TSDPA_RD_V(15, 23, 4096) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+                       "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1]), "=&v"(x[5][0]), "=&v"(x[5][1]),
+                       "=&v"(x[6][0]), "=&v"(x[6][1]), "=&v"(x[7][0]), "=&v"(x[7][1])
+                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7])
+                     : "memory");
+    }
+};
+template <> struct Read8<160> {
+    static __device__ __forceinline__ void keys(u32x4 (&x)[4][2], u32x2 (&y)[4], const uint32_t (&p)[2])
+    {
+        asm volatile(TSDPA_RD_K(0, 12, 0) TSDPA_RD_K(1, 12, 64) TSDPA_RD_K(2, 12, 2560) TSDPA_RD_K(3, 12, 2624)
+                     TSDPA_RD_K(4, 12, 5120) TSDPA_RD_K(5, 12, 5184) TSDPA_RD_K(6, 12, 7680) TSDPA_RD_K(7, 12, 7744)
+                     TSDPA_RD_K8(8, 13, 0) TSDPA_RD_K8(9, 13, 2560) TSDPA_RD_K8(10, 13, 5120) TSDPA_RD_K8(11, 13, 7680) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+                       "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+                     : "v"(p[0]), "v"(p[1])
+                     : "memory");
+    }
+    static __device__ __forceinline__ void values(u32x2 (&x)[10][2], const uint32_t (&p)[2])
+    {
+        asm volatile(TSDPA_RD_V(0, 20, 0) TSDPA_RD_V(1, 20, 5120) TSDPA_RD_V(2, 21, 0) TSDPA_RD_V(3, 21, 5120)
+                     TSDPA_RD_V(4, 20, 32) TSDPA_RD_V(5, 20, 5152) TSDPA_RD_V(6, 21, 32) TSDPA_RD_V(7, 21, 5152)
+                     TSDPA_RD_V(8, 20, 64) TSDPA_RD_V(9, 20, 5184) TSDPA_RD_V(10, 21, 64) TSDPA_RD_V(11, 21, 5184)
+                     TSDPA_RD_V(12, 20, 96) TSDPA_RD_V(13, 20, 5216) TSDPA_RD_V(14, 21, 96) TSDPA_RD_V(15, 21, 5216)
+                     TSDPA_RD_V(16, 20, 128) TSDPA_RD_V(17, 20, 5248) TSDPA_RD_V(18, 21, 128) TSDPA_RD_V(19, 21, 5248) TSDPA_RD_WAIT
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+                       "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1]), "=&v"(x[5][0]), "=&v"(x[5][1]),
+                       "=&v"(x[6][0]), "=&v"(x[6][1]), "=&v"(x[7][0]), "=&v"(x[7][1]), "=&v"(x[8][0]), "=&v"(x[8][1]),
+                       "=&v"(x[9][0]), "=&v"(x[9][1])
+                     : "v"(p[0]), "v"(p[1])
+                     : "memory");
+    }
+};
+#undef TSDPA_RD_K
+#undef TSDPA_RD_K8
+#undef TSDPA_RD_V
+#undef TSDPA_RD_WAIT
+
+// Values that are NaN, in keys that only some rows see (the causal mask): the product with a weight of 0 would be NaN for the others.
+// Eight codes: 1 (FP16) where one is NaN, and the codes without those.
+struct Nan8 {
+    static __device__ __forceinline__ uint32_t marks(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+    static __device__ __forceinline__ uint32_t whole(uint32_t m) { return (m >> 7) * 0xffu; }
+    static __device__ __forceinline__ f16x8 ones(u32x2 x)
+    {
+        const uint32_t a = whole(marks(x[0])) & 0x38383838u, b = whole(marks(x[1])) & 0x38383838u;      // (0x38: the code of 1)
+        return Codes<_Float16>::wide(a, b);
+    }
+    static __device__ __forceinline__ u32x2 without(u32x2 x) { return u32x2{x[0] & ~whole(marks(x[0])), x[1] & ~whole(marks(x[1]))}; }
+};
+
+// A workgroup: NW wavefronts, one (run of keys, 16 * NQ query rows of a key/value head).  a.S query rows per head, of which rows_per_head
+// (the query positions) belong to each query head.
+template <typename T, int D, int NQ, int NW, bool PAGED>
+__global__ void __launch_bounds__(NW * 64, 2)
+sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__restrict__ lse, Cache8Args cache, int S, int heads, int row_tiles, float c,
+                          uint32_t qsign, int causal, int Skv_cap, int splits, float *__restrict__ ws, int rows_per_head, const int *__restrict__ kv_lens, int batches)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    using vec8 = typename Elem<T>::vec8;
+    using vec4 = typename Elem<T>::vec4;
+    using G = Geom8<D>;
+    constexpr int KS = D / 32, DB = D / 16, NU = G::UNITS, TM = NQ * 16;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const lds_ptr lds = (lds_ptr)smem;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t = lane >> 4, l16 = lane & 15;
+
+    // (runs in the order of sdpa_decode_kernel.h; a head's tiles of query rows next to each other)
+    const int unit = blockIdx.x / row_tiles, r0 = (blockIdx.x - unit * row_tiles) * TM;
+    const int sp = unit / heads;
+    int head = unit - sp * heads + (int)((long long)sp * heads / splits);
+    if (head >= heads) head -= heads;
+    const int hpb = cache.heads, b = head / hpb, h = head - b * hpb;
+    auto clamped = [&](int x) __attribute__((always_inline)) { return x < 0 ? 0 : (x < Skv_cap ? x : Skv_cap); };
+    int len = Skv_cap, longest = len;             // keys of this entry, and (runs are a share of these) of the longest one
+    if (kv_lens != nullptr) {
+        len = longest = clamped(kv_lens[b]);
+        if (splits > 1 && batches > 1 && batches <= 64) {
+            longest = clamped(lane < batches ? kv_lens[lane] : 0);
+#pragma unroll
+            for (int w = 1; w < 64; w <<= 1) {
+                const int y = __shfl_xor(longest, w, 64);
+                longest = longest > y ? longest : y;
+            }
+        }
+        len = __builtin_amdgcn_readfirstlane(len);
+        longest = __builtin_amdgcn_readfirstlane(longest);
+    }
+    // this workgroup's run of tiles: [t0, t0 + n)
+    const int nT = (len + kTile8 - 1) / kTile8;
+    int run = ((longest + kTile8 - 1) / kTile8 + splits - 1) / splits;
+    if (run < 2) run = 2;
+    const int t0 = sp * run;
+    int n = nT - t0 < run ? nT - t0 : run;
+    if (n < 0) n = 0;
+    const size_t states = (size_t)heads * splits * S * D;
+    if (n == 0 && splits > 1) {                   // the state of no keys (o is not looked at then)
+        if (tid < TM && r0 + tid < S) {
+            float *ml = ws + states + ((size_t)(head * splits + sp) * S + r0 + tid) * 2;
+            ml[0] = -INFINITY;
+            ml[1] = 0.f;
+        }
+        return;
+    }
+
+    // ---- tiles: HBM -> LDS.  Wavefront w takes the tiles w, w + NW, ... of the run, entered at a tile that depends on the workgroup (heads of
+    // a dense cache lie a power of two apart: in step they would keep hitting the same memory channels).
+    const lds_ptr kslot = lds + wave * 2 * G::TILE, vslot = kslot + G::TILE;
+    const unsigned char *kbase = (const unsigned char *)cache.data[0], *vbase = (const unsigned char *)cache.data[1];
+    const size_t head_off = (size_t)head * (size_t)Skv_cap * D;
+    const auto k_rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(kbase + (PAGED ? 0 : head_off)), (short)0, len * G::ROW, 0x00020000);
+    const auto v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(vbase + (PAGED ? 0 : head_off)), (short)0, len * G::ROW, 0x00020000);
+    const int *pages = PAGED ? cache.block_table + (size_t)b * cache.max_blocks : nullptr;
+    int kgoff[G::P], vgoff[G::P];
+#pragma unroll
+    for (int u = 0; u < G::P; ++u) {
+        const int p = u * 64 + lane, r = p / G::CPR, cp = p % G::CPR;
+        kgoff[u] = r * G::ROW + ((cp ^ G::kx(r)) << 4);
+        vgoff[u] = r * G::ROW + ((cp ^ G::vx(r)) << 4);
+    }
+    const int shift = PAGED ? __builtin_ctz(cache.block_rows) : 0;
+    // (a page that does not exist is none of the cache's memory: the nearest that does is read in its place)
+    auto page_of = [&](int tile) __attribute__((always_inline)) {
+        const int page = __builtin_amdgcn_readfirstlane(pages[(tile * kTile8) >> shift]);
+        return page < 0 ? 0 : (page < cache.pages ? page : cache.pages - 1);
+    };
+    struct Src { decltype(k_rsrc) kr, vr; int soff; };
+    auto src_of = [&](int tile, bool valid, int page) __attribute__((always_inline)) {
+        if constexpr (!PAGED) return Src{k_rsrc, v_rsrc, valid ? tile * G::TILE : nT * G::TILE};
+        else {
+            const int row0 = tile * kTile8;
+            int rows = valid ? len - row0 : 0;
+            rows = rows < kTile8 ? rows : kTile8;
+            const unsigned long long first = (((unsigned long long)page * hpb + h) << shift) + (row0 & ((1 << shift) - 1));
+            const unsigned long long byte0 = first * (unsigned long long)G::ROW;
+            const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)byte0), hi = __builtin_amdgcn_readfirstlane((unsigned)(byte0 >> 32));
+            const unsigned long long at = ((unsigned long long)hi << 32) | lo;
+            const int bytes = __builtin_amdgcn_readfirstlane(rows * G::ROW);
+            return Src{__builtin_amdgcn_make_buffer_rsrc((void *)(kbase + at), (short)0, bytes, 0x00020000),
+                       __builtin_amdgcn_make_buffer_rsrc((void *)(vbase + at), (short)0, bytes, 0x00020000), 0};
+        }
+    };
+    auto load_k = [&](const Src &s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(s.kr, (TSDPA_LDS void *)(kslot + u * 1024), 16, kgoff[u % G::P], s.soff + u / G::P * (32 * G::ROW), 0, 0);
+    };
+    auto load_v = [&](const Src &s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(s.vr, (TSDPA_LDS void *)(vslot + u * 1024), 16, vgoff[u % G::P], s.soff + u / G::P * (32 * G::ROW), 0, 0);
+    };
+    // the four exponents of a tile: lane 0 and 1 of every four K's, 2 and 3 V's (of a block past the end the last one's)
+    const unsigned char *scales = (lane & 2) ? cache.scales[1] : cache.scales[0];
+    auto load_scale = [&](int tile, int page) __attribute__((always_inline)) {
+        int block = 2 * tile + (lane & 1);
+        size_t first;
+        if constexpr (PAGED) {
+            block &= cache.blocks - 1;
+            first = ((size_t)page * hpb + h) * (size_t)cache.blocks;
+        } else {
+            block = block < cache.blocks ? block : cache.blocks - 1;
+            first = (size_t)head * (size_t)cache.blocks;
+        }
+        return (int)scales[first + block];
+    };
+    const int mine = (n - wave + NW - 1) / NW;       // tiles of this wavefront (n - wave > -NW)
+    const int rot = n > NW ? (int)((((unsigned)blockIdx.x * 2654435761u) >> 12) % (unsigned)n) : 0;
+    int cur = wave + rot;                         // within the run
+    if (cur >= n) cur -= n;
+    auto advance = [&](int x) __attribute__((always_inline)) { x += NW; return x >= n ? x - n : x; };
+
+    // ---- Q rows as MFMA B-operands.  The order of the products over D is free: lane t of a row takes bytes t * 16 ... of each 64 columns of K,
+    // of the last 32 (D = 96, 160) t * 8 ..., and Q's columns are those.
+    vec8 qf[NQ][KS];
+    int klim[NQ], klim_least = 0x7fffffff;        // key j contributes to this lane's row iff j <= klim
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        const int row = r0 + nq * 16 + l16 < S ? r0 + nq * 16 + l16 : S - 1;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int col = (G::TAIL && ks == KS - 1) ? ks * 32 + t * 8 : (ks >> 1) * 64 + t * 16 + (ks & 1) * 8;
+            u32x4 raw = *(const u32x4 *)(q + ((size_t)head * S + row) * D + col);
+            raw ^= qsign;
+            qf[nq][ks] = __builtin_bit_cast(vec8, raw);
+        }
+        klim[nq] = causal ? row % rows_per_head + len - rows_per_head : len - 1;
+    }
+    if (causal) {                                 // (wave-uniform: every tile that ends behind it takes the masked path)
+        klim_least = len - rows_per_head;
+    } else {
+        klim_least = len - 1;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    int page_next = 0, scale_next = 0;
+    if (mine > 0) {
+        if constexpr (PAGED) page_next = page_of(t0 + cur);
+        const Src s = src_of(t0 + cur, true, page_next);
+        load_k(s);
+        scale_next = load_scale(t0 + cur, page_next);
+        load_v(s);
+        if constexpr (PAGED) page_next = page_of(mine > 1 ? t0 + advance(cur) : t0);
+    }
+
+    f32x4 oacc[NQ][DB];
+    float m_ref[NQ], l_run[NQ];                   // the lazy reference of sdpa_fwd_kernel.h, this lane's share of the normaliser
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        m_ref[nq] = klim[nq] >= t0 * kTile8 ? kNoWeight : -INFINITY;
+        l_run[nq] = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[nq][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr float kLazyLimit = 256.f;
+
+    // ---- pointers of the reads
+    uint32_t kptr[G::NKP], vptr[G::NVP];
+    {
+        const uint32_t row = __builtin_bit_cast(uint32_t, kslot) + l16 * G::ROW;
+        kptr[0] = row + ((t ^ G::kx(l16)) << 4);
+        if constexpr (D == 128) kptr[1] = row + (((4 + t) ^ G::kx(l16)) << 4);
+        if constexpr (G::TAIL) kptr[G::NKP - 1] = row + (((4 * G::KC + (t >> 1)) ^ G::kx(l16)) << 4) + (t & 1) * 8;
+        const int r = l16 >> 1, v_row = t * 4 + (r & 3) + (r >> 2) * 16;
+#pragma unroll
+        for (int i = 0; i < G::NVP; ++i)
+            vptr[i] = __builtin_bit_cast(uint32_t, vslot) + v_row * G::ROW + ((i ^ G::vx(v_row)) << 4) + (l16 & 1) * 8;
+    }
+
+    f16x8 pb[NQ][2];
+    float ck[2], ev[2], ew[2];                    // of the tile's two blocks: c * 2^EK, EV, 2^-EV
+    // weights of one tile: their sum (what the lazy limit looks at) and their part of l
+    struct Sums { float p, l; };
+    auto exponentials = [&](const f32x4 (&s)[4], int nq, int key0, auto mask_tag) __attribute__((always_inline)) {
+        float sum[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const float off = ev[kb] - m_ref[nq];
+            sum[kb] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb * 2 + (x >> 2)][x & 3], ck[kb], off));
+                if (decltype(mask_tag)::value && key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim[nq]) p = 0.f;
+                sum[kb] += p;
+                pb[nq][kb][x] = (_Float16)p;
+            }
+        }
+        return Sums{sum[0] + sum[1], sum[0] * ew[0] + sum[1] * ew[1]};
+    };
+    auto softmax = [&](f32x4 (&s)[4], int nq, int key0, auto mask_tag) __attribute__((always_inline)) {
+        Sums ps = exponentials(s, nq, key0, mask_tag);
+        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit)) != 0) {            // also inf (first score) and NaN
+            // Eq. 2 for all rows of the wavefront: the tile's maximum, new reference and the rescale of Eqs. 3-4
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+                if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim[nq]) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
+            float m_tile = fmaxf(mx[0] * ck[0] + ev[0], mx[1] * ck[1] + ev[1]);
+            m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 16, 64));
+            m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
+            const bool grow = m_tile > m_ref[nq];      // (a row without finite scores so far: -inf or NaN, left alone)
+            const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref[nq] - m_tile) : 1.f;
+            m_ref[nq] = grow ? m_tile : m_ref[nq];
+            l_run[nq] *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) oacc[nq][db][e] *= alpha;
+            ps = exponentials(s, nq, key0, mask_tag);
+        }
+        l_run[nq] += ps.l;
+    };
+
+    for (int i = 0; i < mine; ++i) {
+        const int next = advance(cur);
+        const bool more = i + 1 < mine;
+        const Src s = src_of(t0 + next, more, page_next);
+        const int page_of_next = page_next;
+        if constexpr (PAGED) page_next = page_of(i + 2 < mine ? t0 + advance(next) : t0);
+        // In flight, in this order: the tile's K, its exponents, its V.  (K has landed when at most V's loads are outstanding, V when at most
+        // the next K's are.  A load of the exponents that the compiler moves makes these waits longer, never shorter.)
+        u32x4 kf[4][G::KC];
+        u32x2 kt[4];
+        TSDPA_WAIT_VMCNT(NU);
+        Read8<D>::keys(kf, kt, kptr);
+        const int scale_now = scale_next;
+        load_k(s);
+        {
+            int x = scale_now;
+            x = x < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x < kScaleBias + kScaleMost ? x : kScaleBias + kScaleMost);
+            const float power = __builtin_bit_cast(float, x << 23) * c, e = (float)(x - kScaleBias), inverse = __builtin_bit_cast(float, (2 * kScaleBias - x) << 23);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                ck[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, power), kb));
+                ev[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), 2 + kb));
+                ew[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), 2 + kb));
+            }
+        }
+        f32x4 sacc[NQ][4];
+#pragma unroll
+        for (int blk = 0; blk < 4; ++blk) {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) sacc[nq][blk] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                vec8 a;
+                if constexpr (G::TAIL) {
+                    if (ks == KS - 1) a = Codes<T>::wide(kt[blk][0], kt[blk][1]);
+                    else a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
+                } else {
+                    a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
+                }
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) sacc[nq][blk] = Elem16<T>::mfma(a, qf[nq][ks], sacc[nq][blk]);
+            }
+            __builtin_amdgcn_sched_barrier(0);    // (or all blocks are converted first, and spill)
+        }
+        const int key0 = (t0 + cur) * kTile8 + t * 4;
+        const bool masked = (t0 + cur) * kTile8 + kTile8 - 1 > klim_least;
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            if (masked) softmax(sacc[nq], nq, key0, std::true_type{});
+            else softmax(sacc[nq], nq, key0, std::false_type{});
+        }
+        u32x2 vf[DB][2];
+        TSDPA_WAIT_VMCNT(NU);
+        Read8<D>::values(vf, vptr);
+        scale_next = load_scale(more ? t0 + next : t0 + cur, page_of_next);
+        load_v(s);
+        bool nan = false;
+        if (masked && causal) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) any |= Nan8::marks(vf[db][kb][0]) | Nan8::marks(vf[db][kb][1]);
+            nan = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+        }
+        if (nan) {
+            // a row gets NaN if it sees one
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                f16x8 seen[NQ];
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) seen[nq][x] = key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim[nq] ? (_Float16)0.f : (_Float16)1.f;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const f16x8 ones = Nan8::ones(vf[db][kb]);
+                    const u32x2 rest = Nan8::without(vf[db][kb]);
+                    const f16x8 a = Codes<_Float16>::wide(rest[0], rest[1]);
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        const f32x4 count = Elem16<_Float16>::mfma(ones, seen[nq], f32x4{0.f, 0.f, 0.f, 0.f});
+                        oacc[nq][db] = Elem16<_Float16>::mfma(a, pb[nq][kb], oacc[nq][db]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) oacc[nq][db][e] += count[e] > 0.f ? __builtin_nanf("") : 0.f;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const f16x8 a = Codes<_Float16>::wide(vf[db][kb][0], vf[db][kb][1]);
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) oacc[nq][db] = Elem16<_Float16>::mfma(a, pb[nq][kb], oacc[nq][db]);
+                    if ((db & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+        cur = next;
+    }
+
+    // ---- the wavefronts' states, over the LDS (no load may still be on its way into it)
+    TSDPA_WAIT_VMCNT0();
+    __syncthreads();
+    typedef TSDPA_LDS float *lds_f;
+    const lds_f mem = (lds_f)lds;
+    float wgt[NQ], M[NQ], L[NQ];                  // this wavefront's weight 2^(m - M); the workgroup's m and l
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        float l = l_run[nq];
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (t == 0) {
+            mem[((wave * NQ + nq) * 16 + l16) * 2] = m_ref[nq];
+            mem[((wave * NQ + nq) * 16 + l16) * 2 + 1] = l;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        M[nq] = -INFINITY;
+        L[nq] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M[nq] = fmaxf(M[nq], mem[((w * NQ + nq) * 16 + l16) * 2]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float m = mem[((w * NQ + nq) * 16 + l16) * 2];
+            L[nq] += (m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M[nq])) * mem[((w * NQ + nq) * 16 + l16) * 2 + 1];
+        }
+        wgt[nq] = m_ref[nq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[nq] - M[nq]);
+        // one split: the division by the normaliser on the way (no key at all: O = 0)
+        if (splits == 1) wgt[nq] *= M[nq] == -INFINITY ? 0.f : 1.f / L[nq];
+    }
+    __syncthreads();
+    // [wave][row][D] floats
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+        if (r0 + nq * 16 + l16 < S)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                f32x4 part;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[e] = oacc[nq][db][e] * wgt[nq];
+                *(TSDPA_LDS f32x4 *)(lds + ((wave * TM + nq * 16 + l16) * D + db * 16 + t * 4) * 4) = part;
+            }
+    __syncthreads();
+    if (wave == 0 && t == 0)
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int row = r0 + nq * 16 + l16;
+            if (row >= S) continue;
+            if (splits > 1) {
+                float *ml = ws + states + ((size_t)(head * splits + sp) * S + row) * 2;
+                ml[0] = M[nq];
+                ml[1] = L[nq];
+            } else if (lse != nullptr) {
+                lse[(size_t)head * S + row] = L[nq] != 0.f ? (M[nq] + __builtin_amdgcn_logf(L[nq])) * 0.69314718055994530942f : -INFINITY;
+            }
+        }
+    const int rows = S - r0 < TM ? S - r0 : TM;
+    for (int x = tid; x < rows * (D / 4); x += NW * 64) {
+        f32x4 sum = *(TSDPA_LDS f32x4 *)(lds + x * 16);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) sum += *(TSDPA_LDS f32x4 *)(lds + w * (TM * D * 4) + x * 16);
+        if (splits > 1) {
+            *(f32x4 *)(ws + ((size_t)(head * splits + sp) * S + r0) * D + (size_t)x * 4) = sum;
+        } else {
+            vec4 out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = (T)sum[e];
+            *(vec4 *)(o + ((size_t)head * S + r0) * D + (size_t)x * 4) = out;
+        }
+    }
+#endif
+}
+
+template <typename T, int D, int NQ, int NW, bool PAGED> int launch_cache8_decode_one(const Cache8Attend &x)
+{
+    auto kern = sdpa_cache8_decode_kernel<T, D, NQ, NW, PAGED>;
+    constexpr int lds_bytes = NW * 2 * Geom8<D>::TILE;
+    static_assert(NW * NQ * 16 * D * 4 <= lds_bytes, "the states of all wavefronts must fit");
+    static std::once_flag once;
+    static hipError_t attr_err = hipSuccess;
+    std::call_once(once, [&] { attr_err = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes); });
+    if (attr_err != hipSuccess) return (int)attr_err;
+    const LaunchArgs &a = x.a;
+    const int row_tiles = (a.S + NQ * 16 - 1) / (NQ * 16);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((long long)a.BH * a.splits * row_tiles)), dim3(NW * 64), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c,
+                       a.S, a.BH, row_tiles, a.c, a.qsign, a.causal, a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.batches);
+    return (int)hipGetLastError();
+}
+
+template <typename T, int D> int launch_cache8_decode_dim(const Cache8Attend &x)
+{
+    return x.c.block_table ? launch_cache8_decode_one<T, D, 1, 4, true>(x) : launch_cache8_decode_one<T, D, 1, 4, false>(x);
+}
+
+template <typename T> int launch_cache8_decode(int D, const Cache8Attend &x)
+{
+    switch (D) {
+        case 64: return launch_cache8_decode_dim<T, 64>(x);
+        case 96: return launch_cache8_decode_dim<T, 96>(x);
+        case 128: return launch_cache8_decode_dim<T, 128>(x);
+        default: return launch_cache8_decode_dim<T, 160>(x);
+    }
+}
+
+}  // namespace tsdpa

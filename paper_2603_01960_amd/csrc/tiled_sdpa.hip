@@ -10,6 +10,7 @@
 #include <mutex>
 #include <random>
 
+#include "cache8_args.h"
 #include "sdpa_bwd_pick.h"
 #include "sdpa_fwd_launch.h"
 #include "sdpa_merge_kernel.h"
@@ -440,6 +441,14 @@ template <typename T> static void launch_merge(const tsdpa::LaunchArgs &a, void 
     hipLaunchKernelGGL(kernel, dim3((rows + block.y - 1) / block.y), block, 0, a.stream,
                        (const float *)a.ws, (T *)o, a.lse, rows, (unsigned)a.S, D, a.splits);
 }
+
+void tsdpa::merge_states(const LaunchArgs &a, int D, int dtype, bool wide)
+{
+    if (dtype == TSDPA_F16) launch_merge<_Float16>(a, a.o, wide, D);
+    else launch_merge<__bf16>(a, a.o, wide, D);
+}
+
+unsigned long long tsdpa::new_ticket() { return call_ticket(); }
 
 extern "C" {
 

@@ -1,6 +1,6 @@
 // The tensor entry points of the Python package (sdpa, sdpa_kv, sdpa_paged, sdpa_backward, sdpa_tree, sdpa_tree_paged, and those
-// around attention: tree_mask, cache_step, qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward) in native code: argument
-// checks, output and workspace tensors from torch's allocator, the current stream, and one call into the C-ABI of include/tiled_sdpa.h.
+// around attention: tree_mask, cache_step, qk_norm_rope, qk_norm_rope_cache, qk_norm_rope_backward; cache8_write, cache8_read, sdpa_cache8
+// of 8-bit caches) in native code: argument checks, output and workspace tensors from torch's allocator, the current stream, and one call into the C-ABI of include/tiled_sdpa.h.
 //
 // Why native: a short call is bound by the host.  One forward call of a small problem (B=1 H=2 S=128 D=64, a kernel of
 // 4.4 us) took 8.7 us of host time through Python attribute reads, data_ptr() calls and ctypes argument conversion, a
@@ -955,6 +955,162 @@ PyObject *call_qk_norm_rope_backward(PyObject *, PyObject *const *args, Py_ssize
     });
 }
 
+// ---- caches of 8 bits
+
+// The cache of the arguments that begin at args[0] (k_cache, v_cache, k_scales, v_scales).
+struct Cache8 {
+    tsdpa_cache8 c{};
+    at::Tensor codes[2], scales[2];
+    explicit Cache8(PyObject *const *args)
+    {
+        static const char *names[2] = {"k_cache", "v_cache"};
+        for (int i = 0; i < 2; ++i) {
+            codes[i] = device_tensor(args[i], names[i]);
+            if (codes[i].dim() != 4 || !codes[i].is_contiguous() || codes[i].scalar_type() != at::kFloat8_e4m3fn)
+                fail_named(names[i], "must be contiguous float8_e4m3fn [pages, Hkv, block_rows, D]");
+        }
+        const at::IntArrayRef s = codes[0].sizes();
+        if (!same_sizes(codes[0], codes[1]) || codes[1].device() != codes[0].device()) fail("k_cache and v_cache must have identical shape and device");
+        for (int i = 0; i < 4; ++i)
+            if (s[i] > std::numeric_limits<int>::max()) fail("k_cache and v_cache are too large");
+        const int64_t blocks[3] = {s[0], s[1], (s[2] + 31) / 32};
+        for (int i = 0; i < 2; ++i) {
+            static const char text[] = "k_scales and v_scales must be contiguous uint8 or float8_e8m0fnu [pages, Hkv, ceil(block_rows / 32)] on the device of the cache";
+            if (!THPVariable_Check(args[2 + i])) fail(text);
+            const at::Tensor &t = scales[i] = THPVariable_Unpack(args[2 + i]);
+            if ((t.scalar_type() != at::kByte && t.scalar_type() != at::kFloat8_e8m0fnu) || !t.is_contiguous() || t.device() != codes[0].device() ||
+                t.sizes() != at::IntArrayRef(blocks, 3))
+                fail(text);
+        }
+        c.k = data(codes[0]);
+        c.v = data(codes[1]);
+        c.k_scales = (unsigned char *)data(scales[0]);
+        c.v_scales = (unsigned char *)data(scales[1]);
+        c.pages = (int)s[0];
+        c.Hkv = (int)s[1];
+        c.block_rows = (int)s[2];
+        c.D = (int)s[3];
+    }
+    // block_table [B, max_blocks], or None
+    void pages_of(PyObject *obj, int64_t B)
+    {
+        if (obj == Py_None) return;
+        static const char text[] = "block_table must be a contiguous int32 tensor [B, max_blocks] on the device of the cache";
+        if (!THPVariable_Check(obj)) fail(text);
+        const at::Tensor &t = THPVariable_Unpack(obj);
+        if (t.dim() != 2 || t.size(1) > std::numeric_limits<int>::max()) fail(text);
+        c.block_table = int_data(obj, {B, t.size(1)}, codes[0].device(), text);
+        c.max_blocks = (int)t.size(1);
+        // (an empty table has no address: any that is not looked at says that there is one)
+        if (!c.block_table) c.block_table = (const int *)alignof(int);
+    }
+    void same_device(const at::Tensor &t, const char *name) const
+    {
+        if (t.device() != codes[0].device()) fail_named(name, "must be on the device of the cache");
+    }
+};
+
+int as_dimension(int64_t x)
+{
+    if (x > std::numeric_limits<int>::max()) fail("a dimension is too large");
+    return (int)x;
+}
+
+// cache8_write(k_cache, v_cache, k_scales, v_scales, k, v, kv_lens, new_lens, block_table)
+PyObject *call_cache8_write(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 9);
+        Cache8 cache(args);
+        const at::Tensor &k = rows_tensor(args[4], "k"), &v = rows_tensor(args[5], "v");
+        const int dtype = element_type(k);
+        const at::IntArrayRef s = k.sizes();
+        if (!same_sizes(k, v) || v.scalar_type() != k.scalar_type() || s[2] != cache.c.Hkv || s[3] != cache.c.D)
+            fail("k and v must be [B, S, Hkv, D] of one dtype, with Hkv and D of the cache");
+        cache.same_device(k, "k");
+        cache.same_device(v, "v");
+        const int B = as_dimension(s[0]), S = as_dimension(s[1]);
+        static const char text[] = "kv_lens and new_lens must be contiguous int32 tensors [B] on the device of the cache";
+        const int *lens = int_data(args[6], s.slice(0, 1), k.device(), text), *new_lens = int_data(args[7], s.slice(0, 1), k.device(), text);
+        cache.pages_of(args[8], s[0]);
+        const int64_t entries = cache.c.max_blocks;
+        distinct({Extent(cache.codes[0]), Extent(cache.codes[1]), Extent(cache.scales[0]), Extent(cache.scales[1])},
+                 {Extent(k), Extent(v), Extent(lens, s[0]), Extent(new_lens, s[0]), Extent(entries ? cache.c.block_table : nullptr, s[0] * entries)},
+                 "the tensors of the cache must overlap neither each other nor what the call reads");
+        const tsdpa_rows kr = rows_of(k), vr = rows_of(v);
+        const Launch on(k);
+        const int st = without_gil(tiled_sdpa_cache8_write, (const tsdpa_cache8 *)&cache.c, &kr, &vr, lens, new_lens, B, S, dtype, on.stream);
+        if (st != TSDPA_OK) return PyLong_FromLong(st);
+        Py_RETURN_NONE;
+    });
+}
+
+// cache8_read(k_cache, v_cache, k_scales, v_scales, slots, bf16, out)
+PyObject *call_cache8_read(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 7);
+        const Cache8 cache(args);
+        const at::Tensor &slots = device_tensor(args[4], "slots");
+        if (slots.scalar_type() != at::kInt || slots.dim() != 2 || !slots.is_contiguous()) fail("slots must be contiguous int32 [B, n]");
+        cache.same_device(slots, "slots");
+        const bool bf16 = as_bool(args[5]);
+        const at::IntArrayRef s = slots.sizes();
+        const int64_t shape[4] = {s[0], cache.c.Hkv, s[1], cache.c.D};
+        const int B = as_dimension(s[0]), rows = as_dimension(s[1]);
+        static const char text[] = "out must be (k, v): contiguous [B, Hkv, n, D] of the dtype asked for, on the device of the cache";
+        const Given<2> given(args[6], text);
+        const at::ScalarType type = bf16 ? at::kBFloat16 : at::kHalf;
+        const at::Tensor k = made(given.t[0], shape, type, slots, text), v = made(given.t[1], shape, type, slots, text);
+        if (args[6] != Py_None)
+            distinct({Extent(k), Extent(v)}, {Extent(cache.codes[0]), Extent(cache.codes[1]), Extent(cache.scales[0]), Extent(cache.scales[1]), Extent(slots)},
+                     "k and v must overlap neither each other nor what the call reads");
+        const Launch on(slots);
+        const int st = without_gil(tiled_sdpa_cache8_read, &cache.c, (const int *)data(slots), data(k), data(v), B, rows, bf16 ? TSDPA_BF16 : TSDPA_F16, on.stream);
+        return tuple_of(st, {&k, &v});
+    });
+}
+
+// sdpa_cache8(k_cache, v_cache, k_scales, v_scales, q, kv_lens, block_table, causal, scale, splits, return_lse, out, workspace): dense (block_table
+// None, kv_lens may be) or paged
+PyObject *call_sdpa_cache8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 13);
+        Cache8 cache(args);
+        const at::Tensor &q = heads_tensor(args[4], "q");
+        cache.same_device(q, "q");
+        const int dtype = element_type(q);
+        const at::IntArrayRef s = q.sizes();
+        const bool paged = args[6] != Py_None;
+        if (s[3] != cache.c.D || (!paged && s[0] != cache.c.pages)) fail("q must be [B, H, Sq, D] with D (and without pages B) of the cache");
+        if (cache.c.Hkv == 0 || s[1] % cache.c.Hkv != 0) fail("the number of query heads must be a multiple of the number of key/value heads");
+        const int B = as_dimension(s[0]), H = as_dimension(s[1]), Sq = as_dimension(s[2]);
+        const int *lens = nullptr;
+        if (paged || args[5] != Py_None) lens = int_data(args[5], s.slice(0, 1), q.device(), "kv_lens must be a contiguous int32 tensor [B] on the device of q");
+        cache.pages_of(args[6], s[0]);
+        const unsigned flags = as_bool(args[7]) ? (unsigned)TSDPA_FLAG_CAUSAL : 0u;
+        const float scale = as_scale(args[8]);
+        int splits = as_int(args[9]);
+        const bool with_lse = as_bool(args[10]);
+        const int64_t capacity = paged ? (int64_t)cache.c.max_blocks * cache.c.block_rows : cache.c.block_rows;
+        if (capacity > std::numeric_limits<int>::max()) return PyLong_FromLong(TSDPA_ERR_BAD_SHAPE);
+        at::Tensor out = output(args[11], q, "out must match q in shape, dtype, device and be contiguous"), lse;
+        if (with_lse) lse = empty(s.slice(0, 3), at::kFloat, q);
+        const bool heuristic = splits == 0;
+        if (heuristic) {
+            const int st = tiled_sdpa_cache8_default_splits(B, H, cache.c.Hkv, Sq, (int)capacity, cache.c.D, dtype, flags, &splits);
+            if (st != TSDPA_OK) return PyLong_FromLong(st);
+        }
+        const Workspace ws(args[12], tiled_sdpa_kv_workspace_bytes(B, H, Sq, cache.c.D, splits), q);
+        if (heuristic && args[12] != Py_None) splits = 0;      // (what fits the caller's buffer: the library decides)
+        const Launch on(q);
+        const int st = without_gil(tiled_sdpa_fwd_cache8, (const tsdpa_cache8 *)&cache.c, (const void *)data(q), data(out), with_lse ? (float *)data(lse) : nullptr,
+                                   lens, B, H, Sq, scale, dtype, flags, splits, ws.ptr, ws.bytes, on.stream);
+        return result(st, args[11], out, with_lse, Py_None, lse);
+    });
+}
+
 PyMethodDef methods[] = {
     {"sdpa", (PyCFunction)(void (*)(void))call_sdpa, METH_FASTCALL, nullptr},
     {"sdpa_kv", (PyCFunction)(void (*)(void))call_sdpa_kv, METH_FASTCALL, nullptr},
@@ -966,6 +1122,9 @@ PyMethodDef methods[] = {
     {"qk_norm_rope", (PyCFunction)(void (*)(void))call_qk_norm_rope, METH_FASTCALL, nullptr},
     {"qk_norm_rope_cache", (PyCFunction)(void (*)(void))call_qk_norm_rope_cache, METH_FASTCALL, nullptr},
     {"qk_norm_rope_backward", (PyCFunction)(void (*)(void))call_qk_norm_rope_backward, METH_FASTCALL, nullptr},
+    {"cache8_write", (PyCFunction)(void (*)(void))call_cache8_write, METH_FASTCALL, nullptr},
+    {"cache8_read", (PyCFunction)(void (*)(void))call_cache8_read, METH_FASTCALL, nullptr},
+    {"sdpa_cache8", (PyCFunction)(void (*)(void))call_sdpa_cache8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
