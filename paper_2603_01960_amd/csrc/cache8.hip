@@ -301,18 +301,18 @@ tsdpa::Cache8Args args_of(const tsdpa_cache8 &c)
 
 bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !c.v_scales; }
 
-// Splits along the key axis: two workgroups per CU in all, of two tiles or more.
-int pick_splits(int64_t tiles, int Skv)
+// Most query rows per key/value head that the decoding kernel takes.
+constexpr int kDecodeRows = 32;
+
+// Splits along the key axis.  Decoding: two workgroups per CU in all, of two tiles or more.
+int default_splits(int heads, int rows, int Skv, int D)
 {
+    if (rows > kDecodeRows) return tsdpa::row_tile_splits(heads, rows, Skv, D);
+    const int64_t tiles = (int64_t)heads * ((rows + 15) / 16);
     int64_t want = (512 + tiles - 1) / tiles;
     const int64_t most = Skv / 128 > 1 ? Skv / 128 : 1;
     if (want > most) want = most;
     return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
-}
-
-int default_splits(int heads, int rows, int Skv)
-{
-    return pick_splits((int64_t)heads * ((rows + 15) / 16), Skv);
 }
 
 int check_attention(int B, int H, int Hkv, int Sq, int Skv, int D, int dtype, unsigned flags)
@@ -384,7 +384,7 @@ int tiled_sdpa_cache8_default_splits(int B, int H, int Hkv, int Sq, int Skv, int
     if (!splits) return TSDPA_ERR_NULL_PTR;
     const int st = check_attention(B, H, Hkv, Sq, Skv, D, dtype, flags);
     if (st != TSDPA_OK) return st;
-    *splits = (int64_t)B * H * Sq == 0 ? 1 : default_splits(B * Hkv, H / Hkv * Sq, Skv);
+    *splits = (int64_t)B * H * Sq == 0 ? 1 : default_splits(B * Hkv, H / Hkv * Sq, Skv, D);
     return TSDPA_OK;
 }
 
@@ -408,7 +408,7 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     if (splits < 0 || splits > TSDPA_MAX_SPLITS) return TSDPA_ERR_BAD_SPLITS;
     const int rows = H / c->Hkv * Sq, heads = B * c->Hkv;
     if (splits == 0) {
-        splits = default_splits(heads, rows, capacity);
+        splits = default_splits(heads, rows, capacity, c->D);
         // (with less memory than that takes: as many as fit)
         const unsigned long long each = tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, 2) / 2, given = workspace ? workspace_bytes / each : 0;
         if ((unsigned long long)splits > given) splits = given > 1 ? (int)given : 1;
@@ -434,10 +434,12 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     a.splits = splits;
     a.ws = (float *)workspace;
     a.stream = (hipStream_t)stream;
-    const int err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_decode_f16(c->D, x) : tsdpa::launch_cache8_decode_bf16(c->D, x);
+    int err;
+    if (rows > kDecodeRows) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_chunk_f16(c->D, x) : tsdpa::launch_cache8_chunk_bf16(c->D, x);
+    else err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_decode_f16(c->D, x) : tsdpa::launch_cache8_decode_bf16(c->D, x);
     if (err != 0) return TSDPA_ERR_LAUNCH;
     if (splits > 1) {
-        tsdpa::merge_states(a, c->D, dtype, (int64_t)heads * rows <= 2048);
+        tsdpa::merge_states(a, c->D, dtype, (int64_t)heads * rows <= 2048 && (splits > 8 || rows <= kDecodeRows));
         if (hipGetLastError() != hipSuccess) return TSDPA_ERR_LAUNCH;
     }
     return TSDPA_OK;

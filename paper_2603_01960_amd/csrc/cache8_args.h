@@ -48,8 +48,11 @@ struct Cache8Attend {
 
 int launch_cache8_decode_f16(int D, const Cache8Attend &x);
 int launch_cache8_decode_bf16(int D, const Cache8Attend &x);
+int launch_cache8_chunk_f16(int D, const Cache8Attend &x);
+int launch_cache8_chunk_bf16(int D, const Cache8Attend &x);
 
-// In tiled_sdpa.hip: the states of a.splits runs combined, and a number that no other call has.
+// In tiled_sdpa.hip: splits of tiles of 128 query rows; the states of a.splits runs combined; a number that no other call has.
+int row_tile_splits(int heads, int rows, int Skv, int D);
 void merge_states(const LaunchArgs &a, int D, int dtype, bool wide);
 unsigned long long new_ticket();
 

@@ -11,35 +11,9 @@
 // of its own, with no barrier in the loop: one slot for K and one for V, each refilled as soon as it has been read into registers.  A
 // tile is 64 keys, as many bytes as 32 keys of 16 bits, so that as many are in flight.
 #pragma once
-#include "cache8_args.h"
-#include "sdpa_fwd_kernel.h"
+#include "sdpa_cache8_values.h"
 
 namespace tsdpa {
-
-constexpr int kTile8 = 64;                        // keys per tile
-
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-
-// Eight codes as eight 16-bit numbers (exact).
-template <typename T> struct Codes;
-template <> struct Codes<_Float16> {
-    static __device__ __forceinline__ f16x8 wide(uint32_t lo, uint32_t hi)
-    {
-        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
-        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
-        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-    }
-};
-template <> struct Codes<__bf16> {
-    static __device__ __forceinline__ bf16x8 wide(uint32_t lo, uint32_t hi)
-    {
-        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
-        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-    }
-};
 
 // LDS layout of a tile: 64 rows of D bytes, unpadded; 16-byte chunks are permuted within each row (chunk c at c ^ swizzle(row)).
 //   K: 16 lanes read one chunk of 16 consecutive rows.
@@ -162,19 +136,6 @@ template <> struct Read8<160> {
 #undef TSDPA_RD_V
 #undef TSDPA_RD_WAIT
 
-// Values that are NaN, in keys that only some rows see (the causal mask): the product with a weight of 0 would be NaN for the others.
-// Eight codes: 1 (FP16) where one is NaN, and the codes without those.
-struct Nan8 {
-    static __device__ __forceinline__ uint32_t marks(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-    static __device__ __forceinline__ uint32_t whole(uint32_t m) { return (m >> 7) * 0xffu; }
-    static __device__ __forceinline__ f16x8 ones(u32x2 x)
-    {
-        const uint32_t a = whole(marks(x[0])) & 0x38383838u, b = whole(marks(x[1])) & 0x38383838u;      // (0x38: the code of 1)
-        return Codes<_Float16>::wide(a, b);
-    }
-    static __device__ __forceinline__ u32x2 without(u32x2 x) { return u32x2{x[0] & ~whole(marks(x[0])), x[1] & ~whole(marks(x[1]))}; }
-};
-
 // A workgroup: NW wavefronts, one (run of keys, 16 * NQ query rows of a key/value head).  a.S query rows per head, of which rows_per_head
 // (the query positions) belong to each query head.
 template <typename T, int D, int NQ, int NW, bool PAGED>
@@ -278,20 +239,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
         for (int u = 0; u < NU; ++u)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(s.vr, (TSDPA_LDS void *)(vslot + u * 1024), 16, vgoff[u % G::P], s.soff + u / G::P * (32 * G::ROW), 0, 0);
     };
-    // the four exponents of a tile: lane 0 and 1 of every four K's, 2 and 3 V's (of a block past the end the last one's)
-    const unsigned char *scales = (lane & 2) ? cache.scales[1] : cache.scales[0];
-    auto load_scale = [&](int tile, int page) __attribute__((always_inline)) {
-        int block = 2 * tile + (lane & 1);
-        size_t first;
-        if constexpr (PAGED) {
-            block &= cache.blocks - 1;
-            first = ((size_t)page * hpb + h) * (size_t)cache.blocks;
-        } else {
-            block = block < cache.blocks ? block : cache.blocks - 1;
-            first = (size_t)head * (size_t)cache.blocks;
-        }
-        return (int)scales[first + block];
-    };
+    auto load_scale = [&](int tile, int page) __attribute__((always_inline)) { return tile_scale_bytes<PAGED>(cache, tile, PAGED ? page : b, h); };
     const int mine = (n - wave + NW - 1) / NW;       // tiles of this wavefront (n - wave > -NW)
     const int rot = n > NW ? (int)((((unsigned)blockIdx.x * 2654435761u) >> 12) % (unsigned)n) : 0;
     int cur = wave + rot;                         // within the run
@@ -355,34 +303,33 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
     }
 
     f16x8 pb[NQ][2];
-    float ck[2], ev[2], ew[2];                    // of the tile's two blocks: c * 2^EK, EV, 2^-EV
     // weights of one tile: their sum (what the lazy limit looks at) and their part of l
     struct Sums { float p, l; };
-    auto exponentials = [&](const f32x4 (&s)[4], int nq, int key0, auto mask_tag) __attribute__((always_inline)) {
+    auto exponentials = [&](const f32x4 (&s)[4], int nq, int key0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
         float sum[2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const float off = ev[kb] - m_ref[nq];
+            const float off = x8.ev[kb] - m_ref[nq];
             sum[kb] = 0.f;
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb * 2 + (x >> 2)][x & 3], ck[kb], off));
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb * 2 + (x >> 2)][x & 3], x8.ck[kb], off));
                 if (decltype(mask_tag)::value && key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim[nq]) p = 0.f;
                 sum[kb] += p;
                 pb[nq][kb][x] = (_Float16)p;
             }
         }
-        return Sums{sum[0] + sum[1], sum[0] * ew[0] + sum[1] * ew[1]};
+        return Sums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1]};
     };
-    auto softmax = [&](f32x4 (&s)[4], int nq, int key0, auto mask_tag) __attribute__((always_inline)) {
-        Sums ps = exponentials(s, nq, key0, mask_tag);
+    auto softmax = [&](f32x4 (&s)[4], int nq, int key0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
+        Sums ps = exponentials(s, nq, key0, x8, mask_tag);
         if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit)) != 0) {            // also inf (first score) and NaN
             // Eq. 2 for all rows of the wavefront: the tile's maximum, new reference and the rescale of Eqs. 3-4
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int x = 0; x < 16; ++x)
                 if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim[nq]) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
-            float m_tile = fmaxf(mx[0] * ck[0] + ev[0], mx[1] * ck[1] + ev[1]);
+            float m_tile = fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1]);
             m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 16, 64));
             m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
             const bool grow = m_tile > m_ref[nq];      // (a row without finite scores so far: -inf or NaN, left alone)
@@ -393,7 +340,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) oacc[nq][db][e] *= alpha;
-            ps = exponentials(s, nq, key0, mask_tag);
+            ps = exponentials(s, nq, key0, x8, mask_tag);
         }
         l_run[nq] += ps.l;
     };
@@ -412,17 +359,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
         Read8<D>::keys(kf, kt, kptr);
         const int scale_now = scale_next;
         load_k(s);
-        {
-            int x = scale_now;
-            x = x < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x < kScaleBias + kScaleMost ? x : kScaleBias + kScaleMost);
-            const float power = __builtin_bit_cast(float, x << 23) * c, e = (float)(x - kScaleBias), inverse = __builtin_bit_cast(float, (2 * kScaleBias - x) << 23);
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                ck[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, power), kb));
-                ev[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), 2 + kb));
-                ew[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), 2 + kb));
-            }
-        }
+        const TileScales scale(scale_now, c);
         f32x4 sacc[NQ][4];
 #pragma unroll
         for (int blk = 0; blk < 4; ++blk) {
@@ -446,8 +383,8 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
         const bool masked = (t0 + cur) * kTile8 + kTile8 - 1 > klim_least;
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
-            if (masked) softmax(sacc[nq], nq, key0, std::true_type{});
-            else softmax(sacc[nq], nq, key0, std::false_type{});
+            if (masked) softmax(sacc[nq], nq, key0, scale, std::true_type{});
+            else softmax(sacc[nq], nq, key0, scale, std::false_type{});
         }
         u32x2 vf[DB][2];
         TSDPA_WAIT_VMCNT(NU);

@@ -1,0 +1,74 @@
+// The values of an 8-bit cache in the attention kernels: codes as 16-bit numbers, the scales of a tile, values that are NaN.
+#pragma once
+#include "cache8_args.h"
+#include "sdpa_fwd_kernel.h"
+
+namespace tsdpa {
+
+constexpr int kTile8 = 64;                        // keys per tile: two blocks of rows that share a scale
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+// Eight codes as eight 16-bit numbers (exact).
+template <typename T> struct Codes;
+template <> struct Codes<_Float16> {
+    static __device__ __forceinline__ f16x8 wide(uint32_t lo, uint32_t hi)
+    {
+        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+};
+template <> struct Codes<__bf16> {
+    static __device__ __forceinline__ bf16x8 wide(uint32_t lo, uint32_t hi)
+    {
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+};
+
+// The four scale bytes of a tile: in lanes 0 and 1 of every four K's, in 2 and 3 V's (of a block past the end the last one's).  `page`: of a dense cache
+// the entry.
+template <bool PAGED> __device__ __forceinline__ int tile_scale_bytes(const Cache8Args &cache, int tile, int page, int h)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned char *scales = (lane & 2) ? cache.scales[1] : cache.scales[0];
+    int block = 2 * tile + (lane & 1);
+    if constexpr (PAGED) block &= cache.blocks - 1;
+    else block = block < cache.blocks ? block : cache.blocks - 1;
+    return (int)scales[((size_t)page * cache.heads + h) * (size_t)cache.blocks + block];
+}
+
+// Of a tile's two blocks: c * 2^EK, EV, 2^-EV.
+struct TileScales {
+    float ck[2], ev[2], ew[2];
+    __device__ __forceinline__ TileScales(int x, float c)
+    {
+        x = x < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x < kScaleBias + kScaleMost ? x : kScaleBias + kScaleMost);
+        const float power = __builtin_bit_cast(float, x << 23) * c, e = (float)(x - kScaleBias), inverse = __builtin_bit_cast(float, (2 * kScaleBias - x) << 23);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            ck[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, power), kb));
+            ev[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), 2 + kb));
+            ew[kb] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), 2 + kb));
+        }
+    }
+};
+
+// Values that are NaN, in keys that only some rows see (the causal mask): the product with a weight of 0 would be NaN for the others.
+// Eight codes: 1 (FP16) where one is NaN, and the codes without those.
+struct Nan8 {
+    static __device__ __forceinline__ uint32_t marks(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+    static __device__ __forceinline__ uint32_t whole(uint32_t m) { return (m >> 7) * 0xffu; }
+    static __device__ __forceinline__ f16x8 ones(u32x2 x)
+    {
+        const uint32_t a = whole(marks(x[0])) & 0x38383838u, b = whole(marks(x[1])) & 0x38383838u;      // (0x38: the code of 1)
+        return Codes<_Float16>::wide(a, b);
+    }
+    static __device__ __forceinline__ u32x2 without(u32x2 x) { return u32x2{x[0] & ~whole(marks(x[0])), x[1] & ~whole(marks(x[1]))}; }
+};
+
+}  // namespace tsdpa

@@ -448,6 +448,8 @@ void tsdpa::merge_states(const LaunchArgs &a, int D, int dtype, bool wide)
     else launch_merge<__bf16>(a, a.o, wide, D);
 }
 
+int tsdpa::row_tile_splits(int heads, int rows, int Skv, int D) { return pick_splits(heads, rows, Skv, D, 128, 64); }
+
 unsigned long long tsdpa::new_ticket() { return call_ticket(); }
 
 extern "C" {
