@@ -20,11 +20,10 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     using vec8 = typename Elem<T>::vec8;
     using vec4 = typename Elem<T>::vec4;
     using G = TileGeom<D, kTile8>;
-    constexpr int TM = NW * 32, TN = kTile8, NB = 2, KK = D / 16, DB = D / 32;
+        constexpr int TM = NW * 32, TN = kTile8, NB = 2, KK = D / 16, DB = D / 32;
     constexpr int GCPR = D / 16;                  // 16-byte chunks of codes per row
     constexpr int U = TN * GCPR / 64;             // loads of a wavefront's 64 lanes per K or V tile
-    constexpr int NL = 2 * U / NW;                // ... of one wavefront for the pair
-    static_assert(2 * U % NW == 0 && NL >= 1, "the tile pair divides over the wavefronts");
+    constexpr int NL = (2 * U + NW - 1) / NW;     // ... of one wavefront for the pair, the last one for some of them only
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const lds_ptr lds = (lds_ptr)smem;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -120,28 +119,26 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
         at_lds[i] = r * G::ROW + (u < U ? (ch ^ G::kswz(r)) << 4 : (((ch >> 2) ^ G::vswz(r)) << 6) + (ch & 3) * 16);
     }
     u32x4 raw[NL];
+    // Whether load i is one of K's.  It is K's for some wavefronts and V's for the others in one i at most, and there chosen by scalar selects.
+    auto is_k = [&](int i) __attribute__((always_inline)) { return (i + 1) * NW <= U || (i * NW < U && i * NW + wave < U); };
     auto load = [&](const Src &s) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int u = i * NW + wave;
-            const bool is_k = u < U;              // (the same for all wavefronts but in one i, and there chosen by scalar selects)
-            const int unit = is_k ? u : u - U;
-            raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(is_k ? s.kr : s.vr, lane * 16, s.soff + unit * 1024, 0));
+            if ((i + 1) * NW > 2 * U && u >= 2 * U) break;
+            raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(is_k(i) ? s.kr : s.vr, lane * 16, s.soff + (is_k(i) ? u : u - U) * 1024, 0));
         }
     };
     constexpr int KSLOT0 = 0, KSLOT1 = G::TILE, VSLOT0 = 2 * G::TILE, VSLOT1 = 3 * G::TILE;
     auto store = [&](int i, int kslot, int vslot) __attribute__((always_inline)) {
-        const int u = i * NW + wave;
-        if (std::is_same<T, _Float16>::value || u >= U) {
-            const lds_ptr at = lds + (u < U ? kslot : vslot) + at_lds[i];
-            const f16x8 lo = Codes<_Float16>::wide(raw[i][0], raw[i][1]), hi = Codes<_Float16>::wide(raw[i][2], raw[i][3]);
-            const int other = u < U ? at_lds[i] ^ 16 : at_lds[i] + 16;
-            lds_write128(at, __builtin_bit_cast(u32x4, lo));
-            lds_write128(lds + (u < U ? kslot : vslot) + other, __builtin_bit_cast(u32x4, hi));
+        if ((i + 1) * NW > 2 * U && i * NW + wave >= 2 * U) return;
+        const lds_ptr slot = lds + (is_k(i) ? kslot : vslot);
+        if (std::is_same<T, _Float16>::value || !is_k(i)) {
+            lds_write128(slot + at_lds[i], __builtin_bit_cast(u32x4, Codes<_Float16>::wide(raw[i][0], raw[i][1])));
+            lds_write128(slot + (is_k(i) ? at_lds[i] ^ 16 : at_lds[i] + 16), __builtin_bit_cast(u32x4, Codes<_Float16>::wide(raw[i][2], raw[i][3])));
         } else {
-            const vec8 lo = Codes<T>::wide(raw[i][0], raw[i][1]), hi = Codes<T>::wide(raw[i][2], raw[i][3]);
-            lds_write128(lds + kslot + at_lds[i], __builtin_bit_cast(u32x4, lo));
-            lds_write128(lds + kslot + (at_lds[i] ^ 16), __builtin_bit_cast(u32x4, hi));
+            lds_write128(slot + at_lds[i], __builtin_bit_cast(u32x4, Codes<T>::wide(raw[i][0], raw[i][1])));
+            lds_write128(slot + (at_lds[i] ^ 16), __builtin_bit_cast(u32x4, Codes<T>::wide(raw[i][2], raw[i][3])));
         }
     };
 
@@ -266,6 +263,14 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
                     sacc[nb] = Elem<T>::mfma(__builtin_bit_cast(vec8, lds_read128(k_rptr[kk] + KS + nb * 32 * G::ROW)), qf[kk], sacc[nb]);
+            // reads four products ahead (left to itself the compiler has the operands of two on their way: 1-2 % of the time)
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < KK * NB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (i < KK * NB - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
             const TileScales x8(scale_now, c);
             softmax(j * TN, x8, mask_tag);

@@ -18,7 +18,9 @@ template <> struct Codes<_Float16> {
     {
         const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
         const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
-        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+        // (whole registers: put together value by value, each pair is taken apart and joined again)
+        return __builtin_bit_cast(f16x8, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
+                                               __builtin_bit_cast(uint32_t, d)});
     }
 };
 template <> struct Codes<__bf16> {
@@ -26,7 +28,8 @@ template <> struct Codes<__bf16> {
     {
         const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
         const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
-        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+        return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
+                                                __builtin_bit_cast(uint32_t, d)});
     }
 };
 
