@@ -304,13 +304,14 @@ bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !
 // Most query rows per key/value head that the decoding kernel takes.
 constexpr int kDecodeRows = 32;
 
-// Splits along the key axis.  Decoding: two workgroups per CU in all, of two tiles or more.
+// Splits along the key axis.  Decoding: one workgroup per CU in all, of runs of at least 256 keys.
 int default_splits(int heads, int rows, int Skv, int D)
 {
     if (rows > kDecodeRows) return tsdpa::row_tile_splits(heads, rows, Skv, D);
     const int64_t tiles = (int64_t)heads * ((rows + 15) / 16);
-    int64_t want = (512 + tiles - 1) / tiles;
-    const int64_t most = Skv / 128 > 1 ? Skv / 128 : 1;
+    if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 400000 : 210000)) return 1;
+    int64_t want = tiles >= 128 ? 1 : 256 / tiles;
+    const int64_t most = Skv / 256 > 1 ? Skv / 256 : 1;
     if (want > most) want = most;
     return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
 }
@@ -434,11 +435,13 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     a.splits = splits;
     a.ws = (float *)workspace;
     a.stream = (hipStream_t)stream;
+    // The decoding kernel combines the runs itself while their states are few (the conditions of the 16-bit caches' in tiled_sdpa.hip)
+    if (rows <= 8 && splits > 1 && splits * rows <= 32 && splits <= rows * c->D / 4 && rows * c->D <= 1024) a.ticket = tsdpa::new_ticket();
     int err;
     if (rows > kDecodeRows) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_chunk_f16(c->D, x) : tsdpa::launch_cache8_chunk_bf16(c->D, x);
     else err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_decode_f16(c->D, x) : tsdpa::launch_cache8_decode_bf16(c->D, x);
     if (err != 0) return TSDPA_ERR_LAUNCH;
-    if (splits > 1) {
+    if (splits > 1 && a.ticket == 0) {
         tsdpa::merge_states(a, c->D, dtype, (int64_t)heads * rows <= 2048 && (splits > 8 || rows <= kDecodeRows));
         if (hipGetLastError() != hipSuccess) return TSDPA_ERR_LAUNCH;
     }

@@ -12,6 +12,7 @@
 // tile is 64 keys, as many bytes as 32 keys of 16 bits, so that as many are in flight.
 #pragma once
 #include "sdpa_cache8_values.h"
+#include "sdpa_runs.h"
 
 namespace tsdpa {
 
@@ -140,8 +141,8 @@ template <> struct Read8<160> {
 // (the query positions) belong to each query head.
 template <typename T, int D, int NQ, int NW, bool PAGED>
 __global__ void __launch_bounds__(NW * 64, 2)
-sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__restrict__ lse, Cache8Args cache, int S, int heads, int row_tiles, float c,
-                          uint32_t qsign, int causal, int Skv_cap, int splits, float *__restrict__ ws, int rows_per_head, const int *__restrict__ kv_lens, int batches)
+sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse, Cache8Args cache, int S, int heads, int row_tiles, float c,
+                          uint32_t qsign, int causal, int Skv_cap, int splits, float *ws, int rows_per_head, const int *__restrict__ kv_lens, int batches, unsigned long long ticket)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using vec8 = typename Elem<T>::vec8;
@@ -185,10 +186,9 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
     const size_t states = (size_t)heads * splits * S * D;
     if (n == 0 && splits > 1) {                   // the state of no keys (o is not looked at then)
         if (tid < TM && r0 + tid < S) {
-            float *ml = ws + states + ((size_t)(head * splits + sp) * S + r0 + tid) * 2;
-            ml[0] = -INFINITY;
-            ml[1] = 0.f;
+            put_pair(ws + states + ((size_t)(head * splits + sp) * S + r0 + tid) * 2, -INFINITY, 0.f);
         }
+        if (ticket != 0) finish_runs<T, D, NW>(o, lse, ws, lds, head, sp, S, heads, splits, ticket, tid, wave, lane);
         return;
     }
 
@@ -489,9 +489,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
             const int row = r0 + nq * 16 + l16;
             if (row >= S) continue;
             if (splits > 1) {
-                float *ml = ws + states + ((size_t)(head * splits + sp) * S + row) * 2;
-                ml[0] = M[nq];
-                ml[1] = L[nq];
+                put_pair(ws + states + ((size_t)(head * splits + sp) * S + row) * 2, M[nq], L[nq]);
             } else if (lse != nullptr) {
                 lse[(size_t)head * S + row] = L[nq] != 0.f ? (M[nq] + __builtin_amdgcn_logf(L[nq])) * 0.69314718055994530942f : -INFINITY;
             }
@@ -502,7 +500,9 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
 #pragma unroll
         for (int w = 1; w < NW; ++w) sum += *(TSDPA_LDS f32x4 *)(lds + w * (TM * D * 4) + x * 16);
         if (splits > 1) {
-            *(f32x4 *)(ws + ((size_t)(head * splits + sp) * S + r0) * D + (size_t)x * 4) = sum;
+            float *part = ws + ((size_t)(head * splits + sp) * S + r0) * D + (size_t)x * 4;
+            put_pair(part, sum[0], sum[1]);
+            put_pair(part + 2, sum[2], sum[3]);
         } else {
             vec4 out;
 #pragma unroll
@@ -510,6 +510,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *__restrict__ o, float *__r
             *(vec4 *)(o + ((size_t)head * S + r0) * D + (size_t)x * 4) = out;
         }
     }
+    if (ticket != 0) finish_runs<T, D, NW>(o, lse, ws, lds, head, sp, S, heads, splits, ticket, tid, wave, lane);
 #endif
 }
 
@@ -525,7 +526,7 @@ template <typename T, int D, int NQ, int NW, bool PAGED> int launch_cache8_decod
     const LaunchArgs &a = x.a;
     const int row_tiles = (a.S + NQ * 16 - 1) / (NQ * 16);
     hipLaunchKernelGGL(kern, dim3((unsigned)((long long)a.BH * a.splits * row_tiles)), dim3(NW * 64), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c,
-                       a.S, a.BH, row_tiles, a.c, a.qsign, a.causal, a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.batches);
+                       a.S, a.BH, row_tiles, a.c, a.qsign, a.causal, a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.batches, a.ticket);
     return (int)hipGetLastError();
 }
 

@@ -322,19 +322,20 @@ def test_nan_reaches_the_rows_that_see_it(Sq, R):
     check_attention(q, host, dev, lens, table, cap, causal=False)
 
 
-def test_workspace_and_out():
-    host, dev, table = filled(1, 2, 2000, 64, [2000], 0, seed=4)
-    q = torch.randn(1, 8, 1, 64, device="cuda").half()
+@pytest.mark.parametrize("Skv,Sq", [(2000, 1), (9000, 1), (2000, 60)])
+def test_workspace_and_out(Skv, Sq):
+    host, dev, table = filled(1, 2, Skv, 64, [Skv], 0, seed=4)
+    q = torch.randn(1, 8, Sq, 64, device="cuda").half()
     want = lib.sdpa_kv8(q, *dev)
-    n = lib.cache8_default_splits(1, 8, 2, 1, 2000, 64, lib.F16)
-    assert n > 1
+    n = lib.cache8_default_splits(1, 8, 2, Sq, Skv, 64, lib.F16)
+    assert n > 1 or Skv == 2000
     out = torch.empty_like(q)
-    ws = torch.empty(lib.kv_workspace_bytes(1, 8, 1, 64, n), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(lib.kv_workspace_bytes(1, 8, Sq, 64, max(n, 2)), dtype=torch.uint8, device="cuda")
     assert lib.sdpa_kv8(q, *dev, out=out, workspace=ws) is out and torch.equal(out, want)
     for part in (0, 1, ws.numel() // 2, ws.numel() - 16):  # fewer runs, or one
-        check_attention(q, host, dev, None, table, 2000, workspace=ws[:part])
+        check_attention(q, host, dev, None, table, Skv, workspace=ws[:part])
     with pytest.raises(lib.TiledSdpaError):
-        lib.sdpa_kv8(q, *dev, splits=n, workspace=ws[:-16])
+        lib.sdpa_kv8(q, *dev, splits=max(n, 2), workspace=ws[:-16])
 
 
 def test_pages_that_do_not_exist_are_read_as_the_nearest():
