@@ -30,16 +30,6 @@ template <> struct Half<__bf16> {
     static __device__ __forceinline__ float value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
 };
 
-// The maximum over a wavefront's lanes, of numbers that are not negative: within rows of 16 lanes, then across them.
-__device__ __forceinline__ int lanes_max(int x)
-{
-#define TSDPA_MAX_STEP(ctrl, rows) { const int y = __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false); x = x > y ? x : y; }
-    TSDPA_MAX_STEP(0x111, 0xf) TSDPA_MAX_STEP(0x112, 0xf) TSDPA_MAX_STEP(0x114, 0xf) TSDPA_MAX_STEP(0x118, 0xf)      // row_shr
-    TSDPA_MAX_STEP(0x142, 0xa) TSDPA_MAX_STEP(0x143, 0xc)                                                          // row_bcast
-#undef TSDPA_MAX_STEP
-    return __builtin_amdgcn_readlane(x, 63);
-}
-
 // The least exponent E with which `largest` (not negative) is at most the largest code, 448 = 1.75 * 2^8, times 2^E.
 __device__ __forceinline__ int exponent_for(float largest)
 {
@@ -304,14 +294,14 @@ bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !
 // Most query rows per key/value head that the decoding kernel takes.
 constexpr int kDecodeRows = 32;
 
-// Splits along the key axis.  Decoding: one workgroup per CU in all, of runs of at least 256 keys.
+// Splits along the key axis.  Decoding: one workgroup per CU in all, of runs of at least 512 keys.
 int default_splits(int heads, int rows, int Skv, int D)
 {
     if (rows > kDecodeRows) return tsdpa::row_tile_splits(heads, rows, Skv, D);
     const int64_t tiles = (int64_t)heads * ((rows + 15) / 16);
-    if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 400000 : 210000)) return 1;
+    if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000)) return 1;
     int64_t want = tiles >= 128 ? 1 : 256 / tiles;
-    const int64_t most = Skv / 256 > 1 ? Skv / 256 : 1;
+    const int64_t most = Skv / 512 > 1 ? Skv / 512 : 1;
     if (want > most) want = most;
     return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
 }

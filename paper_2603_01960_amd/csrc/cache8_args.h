@@ -46,6 +46,22 @@ struct Cache8Attend {
     LaunchArgs a;                                 // q, o, lse, BH, S, rows_per_head, kv_lens, heads_per_batch, batches, c, qsign, causal, Skv, splits, ws, ticket, stream
 };
 
+#if defined(__HIPCC__)
+// The maximum over a wavefront's lanes, of numbers that are not negative: within rows of 16 lanes, then across them.
+__device__ __forceinline__ int lanes_max(int x)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+#define TSDPA_MAX_STEP(ctrl, rows) { const int y = __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false); x = x > y ? x : y; }
+    TSDPA_MAX_STEP(0x111, 0xf) TSDPA_MAX_STEP(0x112, 0xf) TSDPA_MAX_STEP(0x114, 0xf) TSDPA_MAX_STEP(0x118, 0xf)      // row_shr
+    TSDPA_MAX_STEP(0x142, 0xa) TSDPA_MAX_STEP(0x143, 0xc)                                                          // row_bcast
+#undef TSDPA_MAX_STEP
+    return __builtin_amdgcn_readlane(x, 63);
+#else
+    return x;
+#endif
+}
+#endif
+
 int launch_cache8_decode_f16(int D, const Cache8Attend &x);
 int launch_cache8_decode_bf16(int D, const Cache8Attend &x);
 int launch_cache8_chunk_f16(int D, const Cache8Attend &x);

@@ -1,4 +1,4 @@
-// Attention of few query rows (16 or 32 per workgroup, the grouped query heads' rows together) over an 8-bit cache.
+// Attention of few query rows (16 per workgroup and up to 32, the grouped query heads' rows together) over an 8-bit cache.
 //
 // The values of a cache are code * 2^E, E4M3 codes, one E for each head and 32 rows of K, one of V.  With c = scale * log2(e)
 //     s_j = <q, codes of key j>,   p_j = 2^(s_j * (c * 2^EK) + EV - m),   o = sum_j p_j * codes of value j,   l = sum_j p_j * 2^-EV,
@@ -137,57 +137,71 @@ template <> struct Read8<160> {
 #undef TSDPA_RD_V
 #undef TSDPA_RD_WAIT
 
-// A workgroup: NW wavefronts, one (run of keys, 16 * NQ query rows of a key/value head).  a.S query rows per head, of which rows_per_head
-// (the query positions) belong to each query head.
-template <typename T, int D, int NQ, int NW, bool PAGED>
+// What the launch fixes: divisors of numbers that the prologue divides by (a division by a variable is a serial chain of some thirty
+// instructions; with those, and shuffles through the LDS, the prologue took 1.2 us, now 0.6).
+struct Decode8Order {
+    int units;                                    // (run, key/value head) pairs
+    int step;                                     // heads that a run's first one is further on than the run's before
+    int row_tiles;                                // workgroups of 16 query rows for each: 1 or 2
+    Divisor by_heads, by_entry_heads, by_splits, by_rows;        // key/value heads in all, of an entry; runs; query positions
+};
+
+// A workgroup: NW wavefronts, one (run of keys, 16 query rows of a key/value head).  S query rows per head, of which rows_per_head (the
+// query positions) belong to each query head.
+template <typename T, int D, int NW, bool PAGED>
 __global__ void __launch_bounds__(NW * 64, 2)
-sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse, Cache8Args cache, int S, int heads, int row_tiles, float c,
-                          uint32_t qsign, int causal, int Skv_cap, int splits, float *ws, int rows_per_head, const int *__restrict__ kv_lens, int batches, unsigned long long ticket)
+sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse, Cache8Args cache, int S, int heads, Decode8Order order, float c,
+                          uint32_t qsign, int causal, int Skv_cap, int splits, float *ws, int rows_per_head, const int *__restrict__ kv_lens, int batches,
+                          unsigned long long ticket)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using vec8 = typename Elem<T>::vec8;
     using vec4 = typename Elem<T>::vec4;
     using G = Geom8<D>;
-    constexpr int KS = D / 32, DB = D / 16, NU = G::UNITS, TM = NQ * 16;
+    constexpr int KS = D / 32, DB = D / 16, NU = G::UNITS, TM = 16;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const lds_ptr lds = (lds_ptr)smem;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int t = lane >> 4, l16 = lane & 15;
+    // (all arguments that the prologue needs, at once)
+    asm volatile("" : : "s"(q), "s"(cache.data[0]), "s"(cache.data[1]), "s"(cache.scales[0]), "s"(cache.scales[1]), "s"(cache.block_table), "s"(S), "s"(heads),
+                 "s"(order.step), "s"(order.by_heads.mul), "s"(order.by_entry_heads.mul), "s"(order.by_splits.mul), "s"(Skv_cap), "s"(splits), "s"(kv_lens));
 
-    // (runs in the order of sdpa_decode_kernel.h; a head's tiles of query rows next to each other)
-    const int unit = blockIdx.x / row_tiles, r0 = (blockIdx.x - unit * row_tiles) * TM;
-    const int sp = unit / heads;
-    int head = unit - sp * heads + (int)((long long)sp * heads / splits);
+    // Run by run, each from another head on (run fastest would put the runs of one long entry next to each other: see sdpa_decode_kernel.h).  The
+    // two tiles of a head's rows next to each other on one XCD, so that one of them reads the keys from its L2.
+    int unit = blockIdx.x, r0 = 0;
+    if (order.row_tiles == 2) {
+        const int y = blockIdx.x >> 3;
+        unit = (y >> 1) * 8 + (blockIdx.x & 7);
+        r0 = (y & 1) * TM;
+        if (unit >= order.units) return;
+    }
+    const int sp = divide(unit, order.by_heads);
+    int head = unit - sp * heads + sp * order.step;
     if (head >= heads) head -= heads;
-    const int hpb = cache.heads, b = head / hpb, h = head - b * hpb;
+    const int hpb = cache.heads, b = divide(head, order.by_entry_heads), h = head - b * hpb;
     auto clamped = [&](int x) __attribute__((always_inline)) { return x < 0 ? 0 : (x < Skv_cap ? x : Skv_cap); };
     int len = Skv_cap, longest = len;             // keys of this entry, and (runs are a share of these) of the longest one
     if (kv_lens != nullptr) {
-        len = longest = clamped(kv_lens[b]);
         if (splits > 1 && batches > 1 && batches <= 64) {
-            longest = clamped(lane < batches ? kv_lens[lane] : 0);
-#pragma unroll
-            for (int w = 1; w < 64; w <<= 1) {
-                const int y = __shfl_xor(longest, w, 64);
-                longest = longest > y ? longest : y;
-            }
+            const int own = clamped(lane < batches ? kv_lens[lane] : 0);
+            len = __builtin_amdgcn_readlane(own, b);
+            longest = lanes_max(own);
+        } else {
+            len = longest = clamped(kv_lens[b]);
         }
-        len = __builtin_amdgcn_readfirstlane(len);
-        longest = __builtin_amdgcn_readfirstlane(longest);
     }
     // this workgroup's run of tiles: [t0, t0 + n)
     const int nT = (len + kTile8 - 1) / kTile8;
-    int run = ((longest + kTile8 - 1) / kTile8 + splits - 1) / splits;
+    int run = divide((longest + kTile8 - 1) / kTile8 + splits - 1, order.by_splits);
     if (run < 2) run = 2;
     const int t0 = sp * run;
     int n = nT - t0 < run ? nT - t0 : run;
     if (n < 0) n = 0;
     const size_t states = (size_t)heads * splits * S * D;
     if (n == 0 && splits > 1) {                   // the state of no keys (o is not looked at then)
-        if (tid < TM && r0 + tid < S) {
-            put_pair(ws + states + ((size_t)(head * splits + sp) * S + r0 + tid) * 2, -INFINITY, 0.f);
-        }
+        if (tid < TM && r0 + tid < S) put_pair(ws + states + ((size_t)(head * splits + sp) * S + r0 + tid) * 2, -INFINITY, 0.f);
         if (ticket != 0) finish_runs<T, D, NW>(o, lse, ws, lds, head, sp, S, heads, splits, ticket, tid, wave, lane);
         return;
     }
@@ -201,12 +215,10 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     const auto v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(vbase + (PAGED ? 0 : head_off)), (short)0, len * G::ROW, 0x00020000);
     const int *pages = PAGED ? cache.block_table + (size_t)b * cache.max_blocks : nullptr;
     int kgoff[G::P], vgoff[G::P];
-#pragma unroll
-    for (int u = 0; u < G::P; ++u) {
+    auto offset = [&](int u, auto swizzle) __attribute__((always_inline)) {
         const int p = u * 64 + lane, r = p / G::CPR, cp = p % G::CPR;
-        kgoff[u] = r * G::ROW + ((cp ^ G::kx(r)) << 4);
-        vgoff[u] = r * G::ROW + ((cp ^ G::vx(r)) << 4);
-    }
+        return r * G::ROW + ((cp ^ swizzle(r)) << 4);
+    };
     const int shift = PAGED ? __builtin_ctz(cache.block_rows) : 0;
     // (a page that does not exist is none of the cache's memory: the nearest that does is read in its place)
     auto page_of = [&](int tile) __attribute__((always_inline)) {
@@ -241,52 +253,46 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     };
     auto load_scale = [&](int tile, int page) __attribute__((always_inline)) { return tile_scale_bytes<PAGED>(cache, tile, PAGED ? page : b, h); };
     const int mine = (n - wave + NW - 1) / NW;       // tiles of this wavefront (n - wave > -NW)
-    const int rot = n > NW ? (int)((((unsigned)blockIdx.x * 2654435761u) >> 12) % (unsigned)n) : 0;
+    const int rot = n > NW ? (int)__umulhi((unsigned)blockIdx.x * 2654435761u, (unsigned)n) : 0;
     int cur = wave + rot;                         // within the run
     if (cur >= n) cur -= n;
     auto advance = [&](int x) __attribute__((always_inline)) { x += NW; return x >= n ? x - n : x; };
 
+    // The first tile's K goes out before anything else is worked out, then its exponents, Q, and V, in the order in which they are needed.
+    int page_next = 0, scale_next = 0;
+    if constexpr (PAGED) page_next = page_of(mine > 0 ? t0 + cur : 0);
+    const Src first = src_of(t0 + cur, mine > 0, page_next);
+#pragma unroll
+    for (int u = 0; u < G::P; ++u) kgoff[u] = offset(u, G::kx);
+    load_k(first);
+    __builtin_amdgcn_sched_barrier(0);
+    scale_next = load_scale(mine > 0 ? t0 + cur : 0, page_next);
     // ---- Q rows as MFMA B-operands.  The order of the products over D is free: lane t of a row takes bytes t * 16 ... of each 64 columns of K,
     // of the last 32 (D = 96, 160) t * 8 ..., and Q's columns are those.
-    vec8 qf[NQ][KS];
-    int klim[NQ], klim_least = 0x7fffffff;        // key j contributes to this lane's row iff j <= klim
+    vec8 qf[KS];
+    const int row = r0 + l16 < S ? r0 + l16 : S - 1;
+    u32x4 raw[KS];
 #pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-        const int row = r0 + nq * 16 + l16 < S ? r0 + nq * 16 + l16 : S - 1;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int col = (G::TAIL && ks == KS - 1) ? ks * 32 + t * 8 : (ks >> 1) * 64 + t * 16 + (ks & 1) * 8;
-            u32x4 raw = *(const u32x4 *)(q + ((size_t)head * S + row) * D + col);
-            raw ^= qsign;
-            qf[nq][ks] = __builtin_bit_cast(vec8, raw);
-        }
-        klim[nq] = causal ? row % rows_per_head + len - rows_per_head : len - 1;
-    }
-    if (causal) {                                 // (wave-uniform: every tile that ends behind it takes the masked path)
-        klim_least = len - rows_per_head;
-    } else {
-        klim_least = len - 1;
+    for (int ks = 0; ks < KS; ++ks) {
+        const int col = (G::TAIL && ks == KS - 1) ? ks * 32 + t * 8 : (ks >> 1) * 64 + t * 16 + (ks & 1) * 8;
+        raw[ks] = *(const u32x4 *)(q + ((size_t)head * S + row) * D + col);
     }
     __builtin_amdgcn_sched_barrier(0);
-    int page_next = 0, scale_next = 0;
-    if (mine > 0) {
-        if constexpr (PAGED) page_next = page_of(t0 + cur);
-        const Src s = src_of(t0 + cur, true, page_next);
-        load_k(s);
-        scale_next = load_scale(t0 + cur, page_next);
-        load_v(s);
-        if constexpr (PAGED) page_next = page_of(mine > 1 ? t0 + advance(cur) : t0);
-    }
+#pragma unroll
+    for (int u = 0; u < G::P; ++u) vgoff[u] = offset(u, G::vx);
+    load_v(first);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PAGED) page_next = page_of(mine > 1 ? t0 + advance(cur) : mine > 0 ? t0 : 0);
+    // key j contributes to this lane's row iff j <= klim; every tile that ends behind klim_least takes the masked path
+    const int klim = causal ? row - divide(row, order.by_rows) * rows_per_head + len - rows_per_head : len - 1;
+    const int klim_least = causal ? len - rows_per_head : len - 1;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(vec8, raw[ks] ^ qsign);
 
-    f32x4 oacc[NQ][DB];
-    float m_ref[NQ], l_run[NQ];                   // the lazy reference of sdpa_fwd_kernel.h, this lane's share of the normaliser
+    f32x4 oacc[DB];
+    float m_ref = klim >= t0 * kTile8 ? kNoWeight : -INFINITY, l_run = 0.f;      // the lazy reference of sdpa_fwd_kernel.h, this lane's share of the normaliser
 #pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-        m_ref[nq] = klim[nq] >= t0 * kTile8 ? kNoWeight : -INFINITY;
-        l_run[nq] = 0.f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) oacc[nq][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int db = 0; db < DB; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr float kLazyLimit = 256.f;
 
     // ---- pointers of the reads
@@ -302,47 +308,46 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
             vptr[i] = __builtin_bit_cast(uint32_t, vslot) + v_row * G::ROW + ((i ^ G::vx(v_row)) << 4) + (l16 & 1) * 8;
     }
 
-    f16x8 pb[NQ][2];
+    f16x8 pb[2];
     // weights of one tile: their sum (what the lazy limit looks at) and their part of l
     struct Sums { float p, l; };
-    auto exponentials = [&](const f32x4 (&s)[4], int nq, int key0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
+    auto exponentials = [&](const f32x4 (&s)[4], int key0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
         float sum[2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const float off = x8.ev[kb] - m_ref[nq];
+            const float off = x8.ev[kb] - m_ref;
             sum[kb] = 0.f;
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
                 float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb * 2 + (x >> 2)][x & 3], x8.ck[kb], off));
-                if (decltype(mask_tag)::value && key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim[nq]) p = 0.f;
+                if (decltype(mask_tag)::value && key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim) p = 0.f;
                 sum[kb] += p;
-                pb[nq][kb][x] = (_Float16)p;
+                pb[kb][x] = (_Float16)p;
             }
         }
         return Sums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1]};
     };
-    auto softmax = [&](f32x4 (&s)[4], int nq, int key0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
-        Sums ps = exponentials(s, nq, key0, x8, mask_tag);
-        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit)) != 0) {            // also inf (first score) and NaN
+    auto softmax = [&](f32x4 (&s)[4], int key0, const TileScales &x8, bool first_tile, auto mask_tag) __attribute__((always_inline)) {
+        Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
+        if (!first_tile) ps = exponentials(s, key0, x8, mask_tag);
+        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit)) != 0) {            // also inf and NaN
             // Eq. 2 for all rows of the wavefront: the tile's maximum, new reference and the rescale of Eqs. 3-4
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int x = 0; x < 16; ++x)
-                if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim[nq]) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
-            float m_tile = fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1]);
-            m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 16, 64));
-            m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
-            const bool grow = m_tile > m_ref[nq];      // (a row without finite scores so far: -inf or NaN, left alone)
-            const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref[nq] - m_tile) : 1.f;
-            m_ref[nq] = grow ? m_tile : m_ref[nq];
-            l_run[nq] *= alpha;
+                if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
+            const float m_tile = quad_max(fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1]));
+            const bool grow = m_tile > m_ref;     // (a row without finite scores so far: -inf or NaN, left alone)
+            const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref - m_tile) : 1.f;
+            m_ref = grow ? m_tile : m_ref;
+            l_run *= alpha;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) oacc[nq][db][e] *= alpha;
-            ps = exponentials(s, nq, key0, x8, mask_tag);
+                for (int e = 0; e < 4; ++e) oacc[db][e] *= alpha;
+            ps = exponentials(s, key0, x8, mask_tag);
         }
-        l_run[nq] += ps.l;
+        l_run += ps.l;
     };
 
     for (int i = 0; i < mine; ++i) {
@@ -360,32 +365,22 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         const int scale_now = scale_next;
         load_k(s);
         const TileScales scale(scale_now, c);
-        f32x4 sacc[NQ][4];
+        f32x4 sacc[4];
 #pragma unroll
         for (int blk = 0; blk < 4; ++blk) {
-#pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) sacc[nq][blk] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sacc[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 vec8 a;
-                if constexpr (G::TAIL) {
-                    if (ks == KS - 1) a = Codes<T>::wide(kt[blk][0], kt[blk][1]);
-                    else a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
-                } else {
-                    a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
-                }
-#pragma unroll
-                for (int nq = 0; nq < NQ; ++nq) sacc[nq][blk] = Elem16<T>::mfma(a, qf[nq][ks], sacc[nq][blk]);
+                if (G::TAIL && ks == KS - 1) a = Codes<T>::wide(kt[blk][0], kt[blk][1]);
+                else a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
+                sacc[blk] = Elem16<T>::mfma(a, qf[ks], sacc[blk]);
             }
-            __builtin_amdgcn_sched_barrier(0);    // (or all blocks are converted first, and spill)
         }
         const int key0 = (t0 + cur) * kTile8 + t * 4;
         const bool masked = (t0 + cur) * kTile8 + kTile8 - 1 > klim_least;
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) {
-            if (masked) softmax(sacc[nq], nq, key0, scale, std::true_type{});
-            else softmax(sacc[nq], nq, key0, scale, std::false_type{});
-        }
+        if (masked) softmax(sacc, key0, scale, i == 0, std::true_type{});
+        else softmax(sacc, key0, scale, i == 0, std::false_type{});
         u32x2 vf[DB][2];
         TSDPA_WAIT_VMCNT(NU);
         Read8<D>::values(vf, vptr);
@@ -404,23 +399,17 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
             // a row gets NaN if it sees one
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                f16x8 seen[NQ];
+                f16x8 seen;
 #pragma unroll
-                for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) seen[nq][x] = key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim[nq] ? (_Float16)0.f : (_Float16)1.f;
+                for (int x = 0; x < 8; ++x) seen[x] = key0 + kb * 32 + (x >> 2) * 16 + (x & 3) > klim ? (_Float16)0.f : (_Float16)1.f;
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
                     const f16x8 ones = Nan8::ones(vf[db][kb]);
                     const u32x2 rest = Nan8::without(vf[db][kb]);
-                    const f16x8 a = Codes<_Float16>::wide(rest[0], rest[1]);
+                    const f32x4 count = Elem16<_Float16>::mfma(ones, seen, f32x4{0.f, 0.f, 0.f, 0.f});
+                    oacc[db] = Elem16<_Float16>::mfma(Codes<_Float16>::wide(rest[0], rest[1]), pb[kb], oacc[db]);
 #pragma unroll
-                    for (int nq = 0; nq < NQ; ++nq) {
-                        const f32x4 count = Elem16<_Float16>::mfma(ones, seen[nq], f32x4{0.f, 0.f, 0.f, 0.f});
-                        oacc[nq][db] = Elem16<_Float16>::mfma(a, pb[nq][kb], oacc[nq][db]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) oacc[nq][db][e] += count[e] > 0.f ? __builtin_nanf("") : 0.f;
-                    }
+                    for (int e = 0; e < 4; ++e) oacc[db][e] += count[e] > 0.f ? __builtin_nanf("") : 0.f;
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -428,111 +417,85 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    const f16x8 a = Codes<_Float16>::wide(vf[db][kb][0], vf[db][kb][1]);
-#pragma unroll
-                    for (int nq = 0; nq < NQ; ++nq) oacc[nq][db] = Elem16<_Float16>::mfma(a, pb[nq][kb], oacc[nq][db]);
-                    if ((db & 3) == 3) __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int db = 0; db < DB; ++db)
+                    oacc[db] = Elem16<_Float16>::mfma(Codes<_Float16>::wide(vf[db][kb][0], vf[db][kb][1]), pb[kb], oacc[db]);
         }
         cur = next;
     }
 
-    // ---- the wavefronts' states, over the LDS (no load may still be on its way into it)
+    // ---- the wavefronts' states, over the LDS: [wave][row][D] floats, then [wave][row] (m, l)  (no load may still be on its way into it)
+    float l_row = l_run;
+    l_row = quad_sum(l_row);
     TSDPA_WAIT_VMCNT0();
     __syncthreads();
-    typedef TSDPA_LDS float *lds_f;
-    const lds_f mem = (lds_f)lds;
-    float wgt[NQ], M[NQ], L[NQ];                  // this wavefront's weight 2^(m - M); the workgroup's m and l
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    constexpr int ML = NW * TM * D * 4;
+    if (r0 + l16 < S) {
 #pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-        float l = l_run[nq];
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
-        if (t == 0) {
-            mem[((wave * NQ + nq) * 16 + l16) * 2] = m_ref[nq];
-            mem[((wave * NQ + nq) * 16 + l16) * 2 + 1] = l;
-        }
+        for (int db = 0; db < DB; ++db) *(TSDPA_LDS f32x4 *)(lds + ((wave * TM + l16) * D + db * 16 + t * 4) * 4) = oacc[db];
+        if (t == 0) *(TSDPA_LDS f32x2 *)(lds + ML + (wave * TM + l16) * 8) = f32x2{m_ref, l_row};
     }
     __syncthreads();
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-        M[nq] = -INFINITY;
-        L[nq] = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) M[nq] = fmaxf(M[nq], mem[((w * NQ + nq) * 16 + l16) * 2]);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float m = mem[((w * NQ + nq) * 16 + l16) * 2];
-            L[nq] += (m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M[nq])) * mem[((w * NQ + nq) * 16 + l16) * 2 + 1];
-        }
-        wgt[nq] = m_ref[nq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[nq] - M[nq]);
-        // one split: the division by the normaliser on the way (no key at all: O = 0)
-        if (splits == 1) wgt[nq] *= M[nq] == -INFINITY ? 0.f : 1.f / L[nq];
-    }
-    __syncthreads();
-    // [wave][row][D] floats
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq)
-        if (r0 + nq * 16 + l16 < S)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                f32x4 part;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) part[e] = oacc[nq][db][e] * wgt[nq];
-                *(TSDPA_LDS f32x4 *)(lds + ((wave * TM + nq * 16 + l16) * D + db * 16 + t * 4) * 4) = part;
-            }
-    __syncthreads();
-    if (wave == 0 && t == 0)
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) {
-            const int row = r0 + nq * 16 + l16;
-            if (row >= S) continue;
-            if (splits > 1) {
-                put_pair(ws + states + ((size_t)(head * splits + sp) * S + row) * 2, M[nq], L[nq]);
-            } else if (lse != nullptr) {
-                lse[(size_t)head * S + row] = L[nq] != 0.f ? (M[nq] + __builtin_amdgcn_logf(L[nq])) * 0.69314718055994530942f : -INFINITY;
-            }
-        }
+    // a thread: four columns of a row
     const int rows = S - r0 < TM ? S - r0 : TM;
     for (int x = tid; x < rows * (D / 4); x += NW * 64) {
-        f32x4 sum = *(TSDPA_LDS f32x4 *)(lds + x * 16);
+        const int r = x / (D / 4);
+        f32x2 ml[NW];
+        float M = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int w = 1; w < NW; ++w) sum += *(TSDPA_LDS f32x4 *)(lds + w * (TM * D * 4) + x * 16);
+        for (int w = 0; w < NW; ++w) {
+            ml[w] = *(TSDPA_LDS f32x2 *)(lds + ML + (w * TM + r) * 8);
+            M = fmaxf(M, ml[w][0]);
+        }
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float weight = ml[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][0] - M);      // (2^(m - M); -inf: no key)
+            L += weight * ml[w][1];
+            const f32x4 part = *(TSDPA_LDS f32x4 *)(lds + w * (TM * D * 4) + x * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += weight * part[e];
+        }
+        const bool of_row = x - r * (D / 4) == 0;
         if (splits > 1) {
             float *part = ws + ((size_t)(head * splits + sp) * S + r0) * D + (size_t)x * 4;
             put_pair(part, sum[0], sum[1]);
             put_pair(part + 2, sum[2], sum[3]);
+            if (of_row) put_pair(ws + states + ((size_t)(head * splits + sp) * S + r0 + r) * 2, M, L);
         } else {
+            const float inv = M == -INFINITY ? 0.f : 1.f / L;     // (no key at all: O = 0, LSE = -inf)
             vec4 out;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = (T)sum[e];
+            for (int e = 0; e < 4; ++e) out[e] = (T)(sum[e] * inv);
             *(vec4 *)(o + ((size_t)head * S + r0) * D + (size_t)x * 4) = out;
+            if (of_row && lse != nullptr) lse[(size_t)head * S + r0 + r] = L != 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
         }
     }
     if (ticket != 0) finish_runs<T, D, NW>(o, lse, ws, lds, head, sp, S, heads, splits, ticket, tid, wave, lane);
 #endif
 }
 
-template <typename T, int D, int NQ, int NW, bool PAGED> int launch_cache8_decode_one(const Cache8Attend &x)
+template <typename T, int D, int NW, bool PAGED> int launch_cache8_decode_one(const Cache8Attend &x)
 {
-    auto kern = sdpa_cache8_decode_kernel<T, D, NQ, NW, PAGED>;
+    auto kern = sdpa_cache8_decode_kernel<T, D, NW, PAGED>;
     constexpr int lds_bytes = NW * 2 * Geom8<D>::TILE;
-    static_assert(NW * NQ * 16 * D * 4 <= lds_bytes, "the states of all wavefronts must fit");
+    static_assert(NW * 16 * (D * 4 + 8) <= lds_bytes, "the states of all wavefronts must fit");
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
     std::call_once(once, [&] { attr_err = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes); });
     if (attr_err != hipSuccess) return (int)attr_err;
     const LaunchArgs &a = x.a;
-    const int row_tiles = (a.S + NQ * 16 - 1) / (NQ * 16);
-    hipLaunchKernelGGL(kern, dim3((unsigned)((long long)a.BH * a.splits * row_tiles)), dim3(NW * 64), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c,
-                       a.S, a.BH, row_tiles, a.c, a.qsign, a.causal, a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.batches, a.ticket);
+    const int units = a.BH * a.splits, row_tiles = a.S > 16 ? 2 : 1;
+    const Decode8Order order{units, a.splits > 1 ? a.BH / a.splits : 0, row_tiles, divisor((uint32_t)a.BH), divisor((uint32_t)a.heads_per_batch),
+                             divisor((uint32_t)a.splits), divisor((uint32_t)a.rows_per_head)};
+    hipLaunchKernelGGL(kern, dim3((unsigned)(row_tiles == 1 ? units : (units + 7) / 8 * 16)), dim3(NW * 64), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c,
+                       a.S, a.BH, order, a.c, a.qsign, a.causal, a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens, a.batches, a.ticket);
     return (int)hipGetLastError();
 }
 
 template <typename T, int D> int launch_cache8_decode_dim(const Cache8Attend &x)
 {
-    return x.c.block_table ? launch_cache8_decode_one<T, D, 1, 4, true>(x) : launch_cache8_decode_one<T, D, 1, 4, false>(x);
+    return x.c.block_table ? launch_cache8_decode_one<T, D, 4, true>(x) : launch_cache8_decode_one<T, D, 4, false>(x);
 }
 
 template <typename T> int launch_cache8_decode(int D, const Cache8Attend &x)

@@ -33,6 +33,28 @@ template <> struct Codes<__bf16> {
     }
 };
 
+// The maximum and the sum over the four lanes (lane, lane ^ 16, ^ 32, ^ 48) that share a row, in all of them.
+__device__ __forceinline__ float pair16(float x, float &other)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    other = __builtin_bit_cast(float, r1);
+    return __builtin_bit_cast(float, r0);
+}
+__device__ __forceinline__ float quad_max(float x)
+{
+    float b;
+    const float a = pair16(x, b);
+    return pair_max(fmaxf(a, b));
+}
+__device__ __forceinline__ float quad_sum(float x)
+{
+    float b;
+    const float a = pair16(x, b);
+    return pair_sum(a + b);
+}
+
 // The four scale bytes of a tile: in lanes 0 and 1 of every four K's, in 2 and 3 V's (of a block past the end the last one's).  `page`: of a dense cache
 // the entry.
 template <bool PAGED> __device__ __forceinline__ int tile_scale_bytes(const Cache8Args &cache, int tile, int page, int h)
