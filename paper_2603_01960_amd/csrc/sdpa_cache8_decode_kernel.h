@@ -367,16 +367,16 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         const TileScales scale(scale_now, c);
         f32x4 sacc[4];
 #pragma unroll
-        for (int blk = 0; blk < 4; ++blk) {
-            sacc[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int blk = 0; blk < 4; ++blk) sacc[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int blk = 0; blk < 4; ++blk) {   // blk innermost: independent products follow one another
                 vec8 a;
                 if (G::TAIL && ks == KS - 1) a = Codes<T>::wide(kt[blk][0], kt[blk][1]);
                 else a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
                 sacc[blk] = Elem16<T>::mfma(a, qf[ks], sacc[blk]);
             }
-        }
         const int key0 = (t0 + cur) * kTile8 + t * 4;
         const bool masked = (t0 + cur) * kTile8 + kTile8 - 1 > klim_least;
         if (masked) softmax(sacc, key0, scale, i == 0, std::true_type{});
