@@ -456,11 +456,7 @@ def cache8_read(k_cache, v_cache, k_scales, v_scales, slots, dtype, *, out=None)
     """(k, v) [B, Hkv, n, D] in ``dtype`` (torch.float16 or torch.bfloat16): the rows ``slots`` (int32 [B, n], page * block_rows + row, as of
     :func:`cache_step`; rows of zeros where negative) of an 8-bit cache.  ``out=(k, v)`` must overlap neither each other nor the
     cache.  See tiled_sdpa_cache8_read."""
-    import torch
-
-    if dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError("dtype must be float16 or bfloat16")
-    return _checked(_calls().cache8_read(k_cache, v_cache, k_scales, v_scales, slots, dtype == torch.bfloat16, out))
+    return _checked(_calls().cache8_read(k_cache, v_cache, k_scales, v_scales, slots, dtype, out))
 
 
 def sdpa_kv8(q, k_cache, v_cache, k_scales, v_scales, causal: bool = False, scale=None, *, kv_lens=None, splits: int = 0,

@@ -20,14 +20,29 @@ __device__ __forceinline__ int quotient(int n, const Divisor &d) { return (int)(
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (e + 127) << 23); }
 
+// 16-bit numbers: the value of one, and the codes of four of them divided by `scale`, a power of two (|x| <= 448 * scale; one rounding).
 template <typename T> struct Half;
 template <> struct Half<_Float16> {
     static constexpr uint32_t INF = 0x7c00u;
     static __device__ __forceinline__ float value(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (unsigned short)bits); }
+    static __device__ __forceinline__ uint32_t codes(uint32_t lo, uint32_t hi, float scale)
+    {
+        typedef _Float16 pair __attribute__((ext_vector_type(2)));
+        typedef short out __attribute__((ext_vector_type(2)));
+        const out a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(out{0, 0}, __builtin_bit_cast(pair, lo), scale, false);
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(a, __builtin_bit_cast(pair, hi), scale, true));
+    }
 };
 template <> struct Half<__bf16> {
     static constexpr uint32_t INF = 0x7f80u;
     static __device__ __forceinline__ float value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+    static __device__ __forceinline__ uint32_t codes(uint32_t lo, uint32_t hi, float scale)
+    {
+        typedef __bf16 pair __attribute__((ext_vector_type(2)));
+        typedef short out __attribute__((ext_vector_type(2)));
+        const out a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(out{0, 0}, __builtin_bit_cast(pair, lo), scale, false);
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(pair, hi), scale, true));
+    }
 };
 
 // The least exponent E with which `largest` (not negative) is at most the largest code, 448 = 1.75 * 2^8, times 2^E.
@@ -111,7 +126,7 @@ cache8_write_kernel(Cache8Args c, Cache8Rows xk, Cache8Rows xv, const int *__res
     if (held > 0 && old > e) e = old;
     if (held > 0 && e > old) {
         // the rows that are there already keep their values: code * 2^(old - e), rounded (exact but below the normal codes)
-        const float down = power_of_two(old - e);
+        const float move = power_of_two(old - e);
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {
             const int p = j * 64 + lane;
@@ -121,37 +136,34 @@ cache8_write_kernel(Cache8Args c, Cache8Rows xk, Cache8Rows xv, const int *__res
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false), z = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
-                int out = __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * down, a[1] * down, 0, false);
-                y[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[0] * down, z[1] * down, out, true);
+                int out = __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * move, a[1] * move, 0, false);
+                y[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[0] * move, z[1] * move, out, true);
             }
             *at = y;
         }
     }
     // new rows: x * 2^-e, at most 448 unless e is the largest exponent there is, to the nearest code, of two the even one
-    const float up = power_of_two(-e);
-    const bool plain = finite && e < kScaleMost;
+    const float down = power_of_two(e);
+    if (finite && e < kScaleMost) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const int p = j * 64 + lane, r = row0 + p / CPR;
-        if (r < first || r >= end) continue;
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = Half<T>::value(in[j][i >> 1] >> (i & 1) * 16 & 0xffffu) * up;
-        if (!plain) {
-#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int p = j * 64 + lane, r = row0 + p / CPR;
+            if (r < first || r >= end) continue;
+            *(u32x2 *)(codes + p * 8) = u32x2{Half<T>::codes(in[j][0], in[j][1], down), Half<T>::codes(in[j][2], in[j][3], down)};
+        }
+    } else {
+        // value by value: NaN for what is no finite number, the largest code for what is beyond it
+#pragma unroll 1
+        for (int j = 0; j < N; ++j) {
+            const int p = j * 64 + lane, r = row0 + p / CPR;
+            if (r < first || r >= end) continue;
+            const T *at = from + (long long)(r - before) * x.row + p % CPR * 8;
             for (int i = 0; i < 8; ++i) {
-                const bool number = (in[j][i >> 1] >> (i & 1) * 16 & 0x7fffu) < Half<T>::INF;
-                const float cut = fminf(fmaxf(y[i], -448.f), 448.f);
-                y[i] = number ? cut : __builtin_nanf("");
+                const uint32_t bits = ((const unsigned short *)at)[i];
+                const float y = fminf(fmaxf(Half<T>::value(bits) * power_of_two(-e), -448.f), 448.f);
+                codes[p * 8 + i] = (bits & 0x7fffu) < Half<T>::INF ? (unsigned char)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) : (unsigned char)0x7f;
             }
         }
-        u32x2 out;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int pair = __builtin_amdgcn_cvt_pk_fp8_f32(y[i * 4], y[i * 4 + 1], 0, false);
-            out[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[i * 4 + 2], y[i * 4 + 3], pair, true);
-        }
-        *(u32x2 *)(codes + p * 8) = out;
     }
     if (lane == 0) *scale = (unsigned char)(e + kScaleBias);
 #endif
@@ -294,15 +306,20 @@ bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !
 // Most query rows per key/value head that the decoding kernel takes.
 constexpr int kDecodeRows = 32;
 
-// Splits along the key axis.  Decoding: one workgroup per CU in all, of runs of at least 512 keys.
+// Splits along the key axis.  Decoding: one workgroup per CU in all, of runs of at least 512 keys, or 256 while there are up to eight, which
+// the kernel combines itself.  None from half as many key/value heads as CUs on, and none where a pass over a head's keys takes no longer than the
+// second look at the states.  (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 4 rows per head: 8 heads of 1024 keys 7.8 / 8.7 / 8.0 / 8.1; of 2048
+// 11.5 / 10.5 / 8.9 / 8.1 / 9.6; of 8192 33.5 / 21.8 / 14.7 / 11.1 / 10.0, 32 splits 9.6; 64 heads of 1024 keys 7.9 / 8.9 / 8.6, of 4096 18.8 / 15.7
+// / 15.8 / 16.2; 128 heads of 2048 13.3 / 16.4 / 16.7, of 4096 28.0 / 28.7 / 29.6; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6.)
 int default_splits(int heads, int rows, int Skv, int D)
 {
     if (rows > kDecodeRows) return tsdpa::row_tile_splits(heads, rows, Skv, D);
     const int64_t tiles = (int64_t)heads * ((rows + 15) / 16);
     if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000)) return 1;
     int64_t want = tiles >= 128 ? 1 : 256 / tiles;
-    const int64_t most = Skv / 512 > 1 ? Skv / 512 : 1;
+    const int64_t few = Skv / 256 < 8 ? Skv / 256 : 8, most = Skv / 512 > few ? Skv / 512 : few;
     if (want > most) want = most;
+    if (want < 1) want = 1;
     return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
 }
 

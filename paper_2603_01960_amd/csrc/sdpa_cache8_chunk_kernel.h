@@ -48,9 +48,22 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     }
     int head = hs / splits;
     const int sp = hs - head * splits, hpb = cache.heads;
-    if (kv_lens != nullptr && nQ > 1) {           // entries differ in length: they vary fastest over the workgroups
+    // Entries differ in length: they vary fastest over the workgroups, the longest first, so that no XCD has more of them than another and (in the
+    // causal order) the second workgroup of a CU is of a short entry where the first is of a long one.  (4 entries of 1408 ... 3712 keys, 500
+    // queries of 32 heads over 8, D = 128, FP16, in pages: RANKED.)
+    if (kv_lens != nullptr && nQ > 1) {
         const int x = divide(head, by_batches);
-        head = (head - x * batches) * hpb + x;
+        int entry = head - x * batches;
+        if (batches > 1 && batches <= 64) {
+            const int mine = lane < batches ? kv_lens[lane] : -1;
+            int rank = 0;
+            for (int j = 0; j < batches; ++j) {
+                const int other = __builtin_amdgcn_readlane(mine, j);
+                rank += other > mine || (other == mine && j < lane) ? 1 : 0;
+            }
+            entry = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == entry && lane < batches));
+        }
+        head = entry * hpb + x;
     }
     const int b = head / hpb, h = head - b * hpb;
     int Skv = Skv_cap;
@@ -150,19 +163,23 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     float m_ref = klim >= t0 * TN ? kNoWeight : -INFINITY, l_run = 0.f;
     constexpr float kLazyLimit = 256.f;
 
-    // ---- per-lane LDS read pointers (sdpa_fwd_kernel.h's)
-    lds_ptr k_rptr[KK], v_rptr[DB];
+    // ---- per-lane LDS read pointers (sdpa_fwd_kernel.h's; in compact rows the swizzle of K touches the low two bits of a chunk's index only and V has
+    // none, so that two pointers and one serve all columns)
+    constexpr int NKP = G::COMPACT ? 2 : KK, NVP = G::COMPACT ? 1 : DB;
+    lds_ptr k_ptr[NKP], v_ptr[NVP];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-        k_rptr[kk] = lds + l32 * G::ROW + (((2 * kk + g) ^ G::kswz(l32)) << 4);
-        TSDPA_OPAQUE(k_rptr[kk]);
+    for (int i = 0; i < NKP; ++i) {
+        k_ptr[i] = lds + l32 * G::ROW + (((2 * i + g) ^ G::kswz(l32)) << 4);
+        TSDPA_OPAQUE(k_ptr[i]);
     }
     const int v_row = g * 4 + ((lane & 15) >> 2);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-        v_rptr[db] = lds + v_row * G::ROW + ((db ^ G::vswz(v_row)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-        TSDPA_OPAQUE(v_rptr[db]);
+    for (int i = 0; i < NVP; ++i) {
+        v_ptr[i] = lds + v_row * G::ROW + ((i ^ G::vswz(v_row)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+        TSDPA_OPAQUE(v_ptr[i]);
     }
+    auto k_at = [&](int kk) __attribute__((always_inline)) { return G::COMPACT ? k_ptr[kk & 1] + (kk >> 1) * 64 : k_ptr[kk % NKP]; };
+    auto v_at = [&](int db) __attribute__((always_inline)) { return G::COMPACT ? v_ptr[0] + db * 64 : v_ptr[db % NVP]; };
 
     f32x16 sacc[NB];
     f16x8 pb[NB][2];
@@ -215,22 +232,52 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
         }
         l_run += ps.l;
     };
-    // what is not finite in the fragment a of V goes to the rows that see it, and out of a (masked tiles)
-    auto take_not_finite = [&](i16x8 &a, int key0, int db, int nb, int ks) __attribute__((always_inline)) {
-        const u32x4 bits = __builtin_bit_cast(u32x4, a);
-        if (__builtin_amdgcn_ballot_w64(NotFinite<_Float16>::any(bits)) == 0) return;
-        u32x4 finite, up, down, seen;
-        NotFinite<_Float16>::take_apart(bits, finite, up, down);
+    // Values that are NaN, in keys that only some rows see: the product with a weight of 0 would be NaN for the others.  So a tile that the causal
+    // mask cuts is looked through (by every wavefront, so that all agree: 0.25 us); if it has one, the rows that see it get NaN in its
+    // column, and the tile a 0 in its place.
+    auto has_nan = [&](int vslot) __attribute__((always_inline)) {
+        uint32_t any = 0;
+#pragma unroll 4
+        for (int at = lane * 16; at < G::TILE; at += 1024) {
+            const u32x4 x = lds_read128(lds + vslot + at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            seen[i] = (hidden(key0, nb, ks * 8 + 2 * i) ? 0u : NotFinite<_Float16>::ONE & 0xffffu) | (hidden(key0, nb, ks * 8 + 2 * i + 1) ? 0u : NotFinite<_Float16>::ONE & 0xffff0000u);
-        f32x16 zero;
+            for (int i = 0; i < 4; ++i) any |= NotFinite<_Float16>::marks(x[i]);
+        }
+        return __builtin_amdgcn_ballot_w64(any != 0) != 0;
+    };
+    auto take_nan = [&](int key0, int vslot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) zero[i] = 0.f;
-        const f32x16 count = Elem<_Float16>::mfma(__builtin_bit_cast(f16x8, up), __builtin_bit_cast(f16x8, seen), zero);       // (NaN: both up and down)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[db][i] += count[i] > 0.f ? __builtin_nanf("") : 0.f;
-        a = __builtin_bit_cast(i16x8, finite);
+            for (int ks = 0; ks < 2; ++ks) {
+                u32x4 seen;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    seen[i] = (hidden(key0, nb, ks * 8 + 2 * i) ? 0u : 0x3c00u) | (hidden(key0, nb, ks * 8 + 2 * i + 1) ? 0u : 0x3c000000u);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const lds_ptr p0 = v_at(db) + vslot + (nb * 32 + ks * 16) * G::ROW;
+                    const i16x4 lo = lds_read_tr16(p0), hi = lds_read_tr16(p0 + 8 * G::ROW);
+                    u32x4 ones = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ones[i] = NotFinite<_Float16>::whole(NotFinite<_Float16>::marks(ones[i])) & NotFinite<_Float16>::ONE;
+                    f32x16 count;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) count[i] = 0.f;
+                    count = Elem<_Float16>::mfma(__builtin_bit_cast(f16x8, ones), __builtin_bit_cast(f16x8, seen), count);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) oacc[db][i] += count[i] > 0.f ? __builtin_nanf("") : 0.f;
+                    asm volatile("" : "+v"(oacc[db]));       // (now: put off to the end, all counts are held at once)
+                }
+            }
+        __syncthreads();
+        for (int at = tid * 16; at < G::TILE; at += NW * 1024) {
+            u32x4 x = lds_read128(lds + vslot + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] &= ~NotFinite<_Float16>::whole(NotFinite<_Float16>::marks(x[i]));
+            lds_write128(lds + vslot + at, x);
+        }
+        __syncthreads();
     };
 
     if (t0 < t1) {
@@ -262,7 +309,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
             for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
-                    sacc[nb] = Elem<T>::mfma(__builtin_bit_cast(vec8, lds_read128(k_rptr[kk] + KS + nb * 32 * G::ROW)), qf[kk], sacc[nb]);
+                    sacc[nb] = Elem<T>::mfma(__builtin_bit_cast(vec8, lds_read128(k_at(kk) + KS + nb * 32 * G::ROW)), qf[kk], sacc[nb]);
             // reads four products ahead (left to itself the compiler has the operands of two on their way: 1-2 % of the time)
             __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -274,6 +321,9 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
             __builtin_amdgcn_s_setprio(0);
             const TileScales x8(scale_now, c);
             softmax(j * TN, x8, mask_tag);
+            if constexpr (MASK) {
+                if (causal && has_nan(VS)) take_nan(j * TN + g * 4, VS);
+            }
             __builtin_amdgcn_s_setprio(2);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -281,10 +331,9 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
                 for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
                     for (int db = 0; db < DB; ++db) {
-                        const lds_ptr p0 = v_rptr[db] + VS + (nb * 32 + ks * 16) * G::ROW;
+                        const lds_ptr p0 = v_at(db) + VS + (nb * 32 + ks * 16) * G::ROW;
                         const i16x4 lo = lds_read_tr16(p0), hi = lds_read_tr16(p0 + 8 * G::ROW);
-                        i16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                        if constexpr (MASK) take_not_finite(a, j * TN + g * 4, db, nb, ks);
+                        const i16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                         oacc[db] = Elem<_Float16>::mfma(__builtin_bit_cast(f16x8, a), pb[nb][ks], oacc[db]);
                     }
                     const int part = nb * 2 + ks;

@@ -19,6 +19,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "rows_overlap.h"
@@ -1045,7 +1046,7 @@ PyObject *call_cache8_write(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
-// cache8_read(k_cache, v_cache, k_scales, v_scales, slots, bf16, out)
+// cache8_read(k_cache, v_cache, k_scales, v_scales, slots, dtype, out)
 PyObject *call_cache8_read(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
@@ -1054,19 +1055,20 @@ PyObject *call_cache8_read(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor &slots = device_tensor(args[4], "slots");
         if (slots.scalar_type() != at::kInt || slots.dim() != 2 || !slots.is_contiguous()) fail("slots must be contiguous int32 [B, n]");
         cache.same_device(slots, "slots");
-        const bool bf16 = as_bool(args[5]);
+        if (!THPDtype_Check(args[5])) fail("dtype must be float16 or bfloat16");
+        const at::ScalarType type = ((THPDtype *)args[5])->scalar_type;
+        if (type != at::kHalf && type != at::kBFloat16) fail("dtype must be float16 or bfloat16");
         const at::IntArrayRef s = slots.sizes();
         const int64_t shape[4] = {s[0], cache.c.Hkv, s[1], cache.c.D};
         const int B = as_dimension(s[0]), rows = as_dimension(s[1]);
         static const char text[] = "out must be (k, v): contiguous [B, Hkv, n, D] of the dtype asked for, on the device of the cache";
         const Given<2> given(args[6], text);
-        const at::ScalarType type = bf16 ? at::kBFloat16 : at::kHalf;
         const at::Tensor k = made(given.t[0], shape, type, slots, text), v = made(given.t[1], shape, type, slots, text);
         if (args[6] != Py_None)
             distinct({Extent(k), Extent(v)}, {Extent(cache.codes[0]), Extent(cache.codes[1]), Extent(cache.scales[0]), Extent(cache.scales[1]), Extent(slots)},
                      "k and v must overlap neither each other nor what the call reads");
         const Launch on(slots);
-        const int st = without_gil(tiled_sdpa_cache8_read, &cache.c, (const int *)data(slots), data(k), data(v), B, rows, bf16 ? TSDPA_BF16 : TSDPA_F16, on.stream);
+        const int st = without_gil(tiled_sdpa_cache8_read, &cache.c, (const int *)data(slots), data(k), data(v), B, rows, type == at::kBFloat16 ? TSDPA_BF16 : TSDPA_F16, on.stream);
         return tuple_of(st, {&k, &v});
     });
 }
