@@ -303,21 +303,50 @@ tsdpa::Cache8Args args_of(const tsdpa_cache8 &c)
 
 bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !c.v_scales; }
 
-// Most query rows per key/value head that the decoding kernel takes.
+// Which kernel: decoding up to 32 query rows per key/value head (two tiles of 16), beyond that tiles of 32 rows (sdpa_cache8_rows_kernel.h) or of 128
+// (sdpa_cache8_chunk_kernel.h).  Tiles of 128 do a seventh less work per row, but have to be filled, and a wavefront of theirs passes over four times
+// as many keys: tiles of 32 where those of 128 would be half empty (3.5 of them cost as much as one), and up to 2^27 scores.  Entries of a batch differ in
+// length as a rule, which costs large tiles more, and the capacity is an upper bound of all of them: 2^28.
+// (us, tiles of 32 / of 128, BF16, D = 128: 8 heads of 64 rows, 8192 keys 13.0 / 22.3; 8 of 256 rows, 2048 keys 12.4 / 22.6, 8192 keys 20.5 / 32.5, 65536 keys
+// 88 / 90; 32 of 512, 2048 keys 25.5 / 38.7; 8 of 1024, 8192 keys 45 / 51, 65536 keys 307 / 271; 64 of 512, 4096 keys 83 / 84; 8 of 4096, 8192 keys 149 / 141;
+// 8 of 16384, 16384 keys 1042 / 899; 1024 of 64, 2048 keys 124 / 164; 4 entries of 8 heads of 2000 rows, 2560 keys each 102 / 93, 1408 ... 3712 keys 103 / 112.)
+enum class Form { decode, rows, chunk };
 constexpr int kDecodeRows = 32;
+Form form_of(int B, int heads, int rows, int Skv)
+{
+    if (rows <= kDecodeRows) return Form::decode;
+    const int64_t small = ((int64_t)rows + 31) / 32, large = ((int64_t)rows + 127) / 128;
+    // (rows * Skv < 2^61)
+    if (2 * small <= 7 * large || (int64_t)rows * Skv <= ((int64_t)1 << (B > 1 ? 28 : 27)) / heads) return Form::rows;
+    return Form::chunk;
+}
 
-// Splits along the key axis.  Decoding: one workgroup per CU in all, of runs of at least 512 keys, or 256 while there are up to eight, which
+// Splits along the key axis.
+// Decoding: one workgroup per CU in all, of runs of at least 512 keys, or 256 while there are up to eight, which
 // the kernel combines itself.  None from half as many key/value heads as CUs on, and none where a pass over a head's keys takes no longer than the
 // second look at the states.  (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 4 rows per head: 8 heads of 1024 keys 7.8 / 8.7 / 8.0 / 8.1; of 2048
 // 11.5 / 10.5 / 8.9 / 8.1 / 9.6; of 8192 33.5 / 21.8 / 14.7 / 11.1 / 10.0, 32 splits 9.6; 64 heads of 1024 keys 7.9 / 8.9 / 8.6, of 4096 18.8 / 15.7
 // / 15.8 / 16.2; 128 heads of 2048 13.3 / 16.4 / 16.7, of 4096 28.0 / 28.7 / 29.6; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6.)
-int default_splits(int heads, int rows, int Skv, int D)
+// Tiles of 32 rows: the same, of runs of at least 256 keys and none up to 1024; two workgroups per CU where the runs are longer than 8192 keys all the same.
+// (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 8 heads of 64 rows: 1024 keys 10.6 / 10.5 / - / 10.2 / 11.4, 2048 15.0 / 12.9 / - / 10.4 / 11.5, 4096 23.9 / 17.5 / - /
+// 11.5 / 11.8; of 256 rows: 1024 10.7 / 11.2 / 11.1, 2048 15.5 / 13.4 / 12.4 / 16.0, 8192 42.9 / - / 20.5 / 21.3 / 27.4, 65536 309 / - / 101 / 88 / 96.)
+int default_splits(int B, int heads, int rows, int Skv, int D)
 {
-    if (rows > kDecodeRows) return tsdpa::row_tile_splits(heads, rows, Skv, D);
-    const int64_t tiles = (int64_t)heads * ((rows + 15) / 16);
-    if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000)) return 1;
-    int64_t want = tiles >= 128 ? 1 : 256 / tiles;
-    const int64_t few = Skv / 256 < 8 ? Skv / 256 : 8, most = Skv / 512 > few ? Skv / 512 : few;
+    const Form form = form_of(B, heads, rows, Skv);
+    if (form == Form::chunk) return tsdpa::row_tile_splits(heads, rows, Skv, D);
+    int64_t want, most;
+    if (form == Form::rows) {
+        if (Skv <= 1024) return 1;
+        const int64_t tiles = (int64_t)heads * (((int64_t)rows + 31) / 32);
+        want = tiles > 128 ? 1 : 256 / tiles;
+        if (tiles <= 256 && Skv / want > 8192) want *= 2;
+        most = Skv / 256;
+    } else {
+        if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000)) return 1;
+        const int64_t tiles = (int64_t)heads * ((rows + 15) / 16), few = Skv / 256 < 8 ? Skv / 256 : 8;
+        want = tiles >= 128 ? 1 : 256 / tiles;
+        most = Skv / 512 > few ? Skv / 512 : few;
+    }
     if (want > most) want = most;
     if (want < 1) want = 1;
     return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
@@ -392,7 +421,7 @@ int tiled_sdpa_cache8_default_splits(int B, int H, int Hkv, int Sq, int Skv, int
     if (!splits) return TSDPA_ERR_NULL_PTR;
     const int st = check_attention(B, H, Hkv, Sq, Skv, D, dtype, flags);
     if (st != TSDPA_OK) return st;
-    *splits = (int64_t)B * H * Sq == 0 ? 1 : default_splits(B * Hkv, H / Hkv * Sq, Skv, D);
+    *splits = (int64_t)B * H * Sq == 0 ? 1 : default_splits(B, B * Hkv, H / Hkv * Sq, Skv, D);
     return TSDPA_OK;
 }
 
@@ -416,7 +445,7 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     if (splits < 0 || splits > TSDPA_MAX_SPLITS) return TSDPA_ERR_BAD_SPLITS;
     const int rows = H / c->Hkv * Sq, heads = B * c->Hkv;
     if (splits == 0) {
-        splits = default_splits(heads, rows, capacity, c->D);
+        splits = default_splits(B, heads, rows, capacity, c->D);
         // (with less memory than that takes: as many as fit)
         const unsigned long long each = tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, 2) / 2, given = workspace ? workspace_bytes / each : 0;
         if ((unsigned long long)splits > given) splits = given > 1 ? (int)given : 1;
@@ -444,8 +473,10 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     a.stream = (hipStream_t)stream;
     // The decoding kernel combines the runs itself while their states are few (the conditions of the 16-bit caches' in tiled_sdpa.hip)
     if (rows <= 8 && splits > 1 && splits * rows <= 32 && splits <= rows * c->D / 4 && rows * c->D <= 1024) a.ticket = tsdpa::new_ticket();
+    const Form form = form_of(B, heads, rows, capacity);
     int err;
-    if (rows > kDecodeRows) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_chunk_f16(c->D, x) : tsdpa::launch_cache8_chunk_bf16(c->D, x);
+    if (form == Form::chunk) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_chunk_f16(c->D, x) : tsdpa::launch_cache8_chunk_bf16(c->D, x);
+    else if (form == Form::rows) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_rows_f16(c->D, x) : tsdpa::launch_cache8_rows_bf16(c->D, x);
     else err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_decode_f16(c->D, x) : tsdpa::launch_cache8_decode_bf16(c->D, x);
     if (err != 0) return TSDPA_ERR_LAUNCH;
     if (splits > 1 && a.ticket == 0) {

@@ -64,6 +64,8 @@ __device__ __forceinline__ int lanes_max(int x)
 
 int launch_cache8_decode_f16(int D, const Cache8Attend &x);
 int launch_cache8_decode_bf16(int D, const Cache8Attend &x);
+int launch_cache8_rows_f16(int D, const Cache8Attend &x);
+int launch_cache8_rows_bf16(int D, const Cache8Attend &x);
 int launch_cache8_chunk_f16(int D, const Cache8Attend &x);
 int launch_cache8_chunk_bf16(int D, const Cache8Attend &x);
 

@@ -20,7 +20,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     using vec8 = typename Elem<T>::vec8;
     using vec4 = typename Elem<T>::vec4;
     using G = TileGeom<D, kTile8>;
-        constexpr int TM = NW * 32, TN = kTile8, NB = 2, KK = D / 16, DB = D / 32;
+    constexpr int TM = NW * 32, TN = kTile8, NB = 2, KK = D / 16, DB = D / 32;
     constexpr int GCPR = D / 16;                  // 16-byte chunks of codes per row
     constexpr int U = TN * GCPR / 64;             // loads of a wavefront's 64 lanes per K or V tile
     constexpr int NL = (2 * U + NW - 1) / NW;     // ... of one wavefront for the pair, the last one for some of them only

@@ -322,6 +322,94 @@ def test_nan_reaches_the_rows_that_see_it(Sq, R):
     check_attention(q, host, dev, lens, table, cap, causal=False)
 
 
+# Large tiles of query rows are taken for many scores only, counted by the capacity: a cache of a large one whose entries are short.
+def in_large(dev, table, rows):
+    """The cache and block table with a capacity of `rows`; what is added holds NaN codes, pages that do not exist."""
+    if table is not None:
+        wide = torch.full((table.shape[0], rows // dev[0].shape[2]), 2 ** 31 - 1, dtype=torch.int32)
+        wide[:, :table.shape[1]] = table
+        return dev, wide
+    B, Hkv, cap, D = dev[0].shape
+    out = []
+    for x, shape in zip(dev, [(B, Hkv, rows, D)] * 2 + [(B, Hkv, rows // 32)] * 2):
+        y = torch.full(shape, 0x7f, dtype=torch.uint8, device="cuda")
+        y[:, :, :x.shape[2]] = x.view(torch.uint8)
+        out.append(y.view(x.dtype))
+    return out, None
+
+
+def check_large(q, host, dev, lens, table, cap, rows, causal, scale=None, **more):
+    dev, wide = in_large(dev, table, rows)
+    lens_gpu = i32(lens)
+    if wide is None:
+        got = lib.sdpa_kv8(q, *dev, causal=causal, scale=scale, kv_lens=lens_gpu, return_lse=True, **more)
+    else:
+        got = lib.sdpa_paged8(q, *dev, lens_gpu, wide.cuda(), causal=causal, scale=scale, return_lse=True, **more)
+    k, v = ref.gathered(host[0], host[2], lens, table, cap), ref.gathered(host[1], host[3], lens, table, cap)
+    o, lse, eo, el = ref.attention(q.cpu(), k, v, U[q.dtype], causal, scale)
+    assert torch.equal(got[0].isnan().cpu(), o.isnan())
+    off, fine = (got[0].cpu().double() - o).abs(), ~o.isnan()
+    assert not fine.any() or (off - eo)[fine].max() <= 0
+    number, fine = ~lse.isnan(), lse.isfinite()
+    assert torch.equal(torch.isneginf(got[1]).cpu()[number], torch.isneginf(lse)[number])
+    assert ((got[1].cpu().double() - lse).abs() <= el)[fine].all()
+    return got
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 96, 128, 160])
+@pytest.mark.parametrize("G,Sq,R", [(1, 125, 0), (3, 42, 64), (2, 1153, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_large_tiles(dtype, D, G, Sq, R, causal):
+    B, Hkv, cap = 2, 2, 384
+    lens = [371, 70]
+    host, dev, table = filled(B, Hkv, cap, D, lens, R, seed=Sq + R, dtype=dtype)
+    q = torch.randn(B, G * Hkv, Sq, D, generator=torch.Generator().manual_seed(Sq)).to(dtype).cuda()
+    check_large(q, host, dev, lens, table, cap, 1 << 20, causal)
+    check_large(q, host, dev, lens, table, cap, 1 << 20, causal, splits=1)
+
+
+@pytest.mark.parametrize("splits", [2, 3, 128])
+@pytest.mark.parametrize("R", [0, 64])
+@pytest.mark.parametrize("scale", [0.0, -0.3])
+def test_large_tiles_in_runs(splits, R, scale):
+    B, Hkv, cap, D = 3, 2, 512, 128
+    lens = [512, 77, 0]
+    host, dev, table = filled(B, Hkv, cap, D, lens, R, seed=splits, spread=0.5)
+    q = torch.randn(B, 2 * Hkv, 64, D, generator=torch.Generator().manual_seed(splits)).to(torch.bfloat16).cuda()
+    a = check_large(q, host, dev, lens, table, cap, 1 << 20, True, scale, splits=splits)
+    b = check_large(q, host, dev, lens, table, cap, 1 << 20, True, scale, splits=splits)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("Sq", [64, 250])
+@pytest.mark.parametrize("R", [0, 64])
+def test_nan_in_large_tiles(Sq, R):
+    B, Hkv, cap, D = 2, 2, 256, 128
+    lens = [256, 150]
+    host, dev, table = filled(B, Hkv, cap, D, lens, R, seed=2)
+    for codes, row, col in ((1, 255, 3), (1, 252, 77), (0, 254, 5), (1, 149, 9), (0, 148, 127)):
+        b = 0 if row > 200 else 1
+        page, r = ref.place(b, row, R or cap, table)
+        host[codes][page, 1, r, col] = 0x7f if col & 1 else 0xff
+    dev = on_gpu(host)
+    q = torch.randn(B, 2 * Hkv, Sq, D, generator=torch.Generator().manual_seed(Sq)).to(torch.bfloat16).cuda()
+    check_large(q, host, dev, lens, table, cap, 1 << 20, True)
+    check_large(q, host, dev, lens, table, cap, 1 << 20, False)
+
+
+# Tiles of 32 rows: units (heads of all entries times runs) that divide over the XCDs in every way, more and fewer tiles than parts.
+@pytest.mark.parametrize("B,Hkv", [(1, 1), (1, 2), (1, 3), (3, 4), (2, 4), (5, 1), (1, 30)])
+@pytest.mark.parametrize("Sq", [33, 65, 97, 300])
+@pytest.mark.parametrize("splits", [1, 2, 3])
+def test_small_tiles_over_the_chip(B, Hkv, Sq, splits):
+    cap, D = 400, 64
+    lens = [400, 1, 333, 64, 390][:B]
+    host, dev, table = filled(B, Hkv, cap, D, lens, 0, seed=Hkv + Sq)
+    q = torch.randn(B, Hkv, Sq, D, generator=torch.Generator().manual_seed(Sq)).to(torch.bfloat16).cuda()
+    check_attention(q, host, dev, lens, table, cap, causal=True, splits=splits)
+
+
 @pytest.mark.parametrize("Skv,Sq", [(2000, 1), (9000, 1), (2000, 60)])
 def test_workspace_and_out(Skv, Sq):
     host, dev, table = filled(1, 2, Skv, 64, [Skv], 0, seed=4)
