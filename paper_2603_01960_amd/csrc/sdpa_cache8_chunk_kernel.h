@@ -50,7 +50,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     const int sp = hs - head * splits, hpb = cache.heads;
     // Entries differ in length: they vary fastest over the workgroups, the longest first, so that no XCD has more of them than another and (in the
     // causal order) the second workgroup of a CU is of a short entry where the first is of a long one.  (4 entries of 1408 ... 3712 keys, 500
-    // queries of 32 heads over 8, D = 128, FP16, in pages: RANKED.)
+    // queries of 32 heads over 8, D = 128, FP16: 110 -> 107 us.)
     if (kv_lens != nullptr && nQ > 1) {
         const int x = divide(head, by_batches);
         int entry = head - x * batches;
