@@ -125,11 +125,20 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
                        __builtin_amdgcn_make_buffer_rsrc((void *)(vbase + at), (short)0, bytes, 0x00020000), 0};
         }
     };
-    int at_lds[NL];                               // where the chunk's first 8 columns go in a 16-bit tile
+    // Where a chunk's first 8 columns go in a 16-bit tile (its other 8: 16 bytes further on or back).  Eight consecutive lanes write at a time, 128 bytes; were
+    // all these first halves the even 16 bytes of their rows, half of the banks would be left alone.  So four of the lanes have a row in which they are the
+    // odd ones, by the swizzle of K, and by one of its own (vhalf) in a tile of V: no conflicts, where they took 13 % of the cycles (2048 queries of 32 heads over 8,
+    // 16384 keys: 519 -> 513 us, D = 64 297 -> 294; with the halves exchanged in registers instead 488 -> 510).  In compact rows the rows' ends do some of that.
+    auto vhalf = [](int r) __attribute__((always_inline)) { return G::COMPACT ? 0 : (D == 64 ? r & 2 : (r & 1) * 2) * 8; };
+    const int lane_row = G::COMPACT ? 0 : D == 64 ? (lane >> 4) * 4 + ((lane >> 2) & 1) * 2 + ((lane >> 3) & 1) : (lane >> 4) * 2 + ((lane >> 2) & 1);
+    const int lane_chunk = D == 64 ? lane & 3 : (lane & 3) + ((lane >> 3) & 1) * 4;
+    const int lane_at = G::COMPACT ? lane * 16 : lane_row * D + lane_chunk * 16;
+    int at_lds[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-        const int u = i * NW + wave, p = (u < U ? u : u - U) * 64 + lane, r = p / GCPR, ch = p % GCPR * 2;
-        at_lds[i] = r * G::ROW + (u < U ? (ch ^ G::kswz(r)) << 4 : (((ch >> 2) ^ G::vswz(r)) << 6) + (ch & 3) * 16);
+        const int u = i * NW + wave, p = (u < U ? u : u - U) * 64 + lane, r = G::COMPACT ? p / GCPR : (u < U ? u : u - U) * (64 / GCPR) + lane_row;
+        const int ch = (G::COMPACT ? p % GCPR : lane_chunk) * 2;
+        at_lds[i] = r * G::ROW + (u < U ? (ch ^ G::kswz(r)) << 4 : (((ch >> 2) ^ G::vswz(r)) << 6) + ((ch & 3) * 16 ^ vhalf(r)));
     }
     u32x4 raw[NL];
     // Whether load i is one of K's.  It is K's for some wavefronts and V's for the others in one i at most, and there chosen by scalar selects.
@@ -139,7 +148,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
         for (int i = 0; i < NL; ++i) {
             const int u = i * NW + wave;
             if ((i + 1) * NW > 2 * U && u >= 2 * U) break;
-            raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(is_k(i) ? s.kr : s.vr, lane * 16, s.soff + (is_k(i) ? u : u - U) * 1024, 0));
+            raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(is_k(i) ? s.kr : s.vr, lane_at, s.soff + (is_k(i) ? u : u - U) * 1024, 0));
         }
     };
     constexpr int KSLOT0 = 0, KSLOT1 = G::TILE, VSLOT0 = 2 * G::TILE, VSLOT1 = 3 * G::TILE;
@@ -148,7 +157,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
         const lds_ptr slot = lds + (is_k(i) ? kslot : vslot);
         if (std::is_same<T, _Float16>::value || !is_k(i)) {
             lds_write128(slot + at_lds[i], __builtin_bit_cast(u32x4, Codes<_Float16>::wide(raw[i][0], raw[i][1])));
-            lds_write128(slot + (is_k(i) ? at_lds[i] ^ 16 : at_lds[i] + 16), __builtin_bit_cast(u32x4, Codes<_Float16>::wide(raw[i][2], raw[i][3])));
+            lds_write128(slot + (at_lds[i] ^ 16), __builtin_bit_cast(u32x4, Codes<_Float16>::wide(raw[i][2], raw[i][3])));
         } else {
             lds_write128(slot + at_lds[i], __builtin_bit_cast(u32x4, Codes<T>::wide(raw[i][0], raw[i][1])));
             lds_write128(slot + (at_lds[i] ^ 16), __builtin_bit_cast(u32x4, Codes<T>::wide(raw[i][2], raw[i][3])));
@@ -175,7 +184,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     const int v_row = g * 4 + ((lane & 15) >> 2);
 #pragma unroll
     for (int i = 0; i < NVP; ++i) {
-        v_ptr[i] = lds + v_row * G::ROW + ((i ^ G::vswz(v_row)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+        v_ptr[i] = lds + v_row * G::ROW + ((i ^ G::vswz(v_row)) << 6) + ((lane >> 4) & 1) * 32 + ((lane & 3) * 8 ^ vhalf(v_row));
         TSDPA_OPAQUE(v_ptr[i]);
     }
     auto k_at = [&](int kk) __attribute__((always_inline)) { return G::COMPACT ? k_ptr[kk & 1] + (kk >> 1) * 64 : k_ptr[kk % NKP]; };
