@@ -537,7 +537,7 @@ typedef struct {
  * (E of a block falls only when its rows are written from the first on, new: dropped rows leave it as it is.)  Values go to the nearest
  * code, of two equally near ones to that with the even mantissa; magnitudes beyond 448 * 2^62 to the largest, NaN and infinities to NaN,
  * and neither counts for E.  Rows from new_lens[b] on are left as they are, byte for byte; so is what other entries hold, as long as no
- * page is in two entries.  A page number that is none (below 0 or from `pages` on) is not written to.  The cache must not overlap the inputs.
+ * page is in two entries.  A page number that is none (below 0 or from `pages` on) is not written to.  (B * Hkv * (S / 32 + 2) is below 2^25.)  The cache must not overlap the inputs.
  *
  * Validation order, of all calls of this section: null structs, dtype, D, shape, empty problem, null pointers, alignment, strides, scale,
  * splits, workspace, launch.
@@ -565,7 +565,8 @@ int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out,
  *   kv_lens      : device int32 [B], rows of each entry, clamped to [0, capacity]; of a dense cache NULL = all of them hold block_rows.
  *   flags        : TSDPA_FLAG_CAUSAL (the queries are the last Sq positions: needs a capacity of Sq or more) or 0.
  *   splits, workspace : as for tiled_sdpa_fwd_kv; 0 = tiled_sdpa_cache8_default_splits of the capacity, or fewer, as many as the workspace
- *                  has room for.  tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, n) bytes hold n.
+ *                  has room for.  tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, n) bytes hold n.  B * H * ceil(Sq / 16), times splits, is at
+ *                  most 2^23 - 16.
  *
  * Scores and sums are FP32.  K is multiplied as 16-bit numbers of q's type, which its codes are; the weights are rounded to FP16 for the
  * product with V, each times its scale, against the greatest such product of the row, so that what contributes most keeps 11 bits.

@@ -55,6 +55,11 @@ __device__ __forceinline__ int exponent_for(float largest)
 
 // One wavefront: the new rows of one block of 32 rows of one head of K or V, a block being what shares a scale.  It holds them in registers
 // between their largest magnitude and their codes, so that they are read once; the block's older rows are read only if the scale grows.
+//
+// Bound by memory where there is much to write (4 entries of up to 2048 tokens, 8 heads, D = 128, BF16: 37.8 MB in 8.5 us, a copy's rate at that size 5.0 ... 6.3
+// TB/s), and else by the launch and a chain of loads, lengths, page, rows (one token: 3.3 us of the GPU, 4.4 from call to call).  One
+// conversion makes two codes and divides by the scale: with it a wavefront holds its rows in 44 to 72 registers; clamping, scaling and packing value by value took
+// up to 229, and is left to blocks that hold NaN, infinities or magnitudes that the largest scale does not reach.
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
 cache8_write_kernel(Cache8Args c, Cache8Rows xk, Cache8Rows xv, const int *__restrict__ kv_lens, const int *__restrict__ new_lens, int S, int capacity,
@@ -74,8 +79,9 @@ cache8_write_kernel(Cache8Args c, Cache8Rows xk, Cache8Rows xv, const int *__res
     const int before = new_lens[b] - S;            // row of token 0
     const int lo = now > before ? now : before;
     if (lo >= next) return;
-    const int row0 = (lo / kScaleRows + w) * kScaleRows;
-    if (row0 >= next) return;
+    const int block0 = lo & ~(kScaleRows - 1);
+    if ((unsigned)w * kScaleRows >= (unsigned)(next - block0)) return;
+    const int row0 = block0 + w * kScaleRows;
     const int first = lo > row0 ? lo : row0, end = next - row0 < kScaleRows ? next : row0 + kScaleRows;
     const int held = (now < first ? now : first) - row0;         // rows of the block that the entry has already (if > 0)
     int page = b, row = row0;
@@ -169,8 +175,9 @@ cache8_write_kernel(Cache8Args c, Cache8Rows xk, Cache8Rows xv, const int *__res
 #endif
 }
 
-// One thread: eight columns of one token, in HEADS heads of K and V.
-template <typename T, int D, int HEADS>
+// One thread: eight columns of one token, in one head of K and V.  Bound by memory (2 entries of 16384 rows, 8 heads, D = 128: 201 MB, a third of it
+// read, in 42 us from call to call, 35.6 of the GPU), and for few rows by the launch and two loads, one behind the other (256 rows 2.7 us of the GPU).
+template <typename T, int D>
 __global__ void __launch_bounds__(256)
 cache8_read_kernel(Cache8Args c, const int *__restrict__ slots, T *__restrict__ k_out, T *__restrict__ v_out, int n, int tokens, Divisor by_n, Divisor by_rows)
 {
@@ -183,43 +190,34 @@ cache8_read_kernel(Cache8Args c, const int *__restrict__ slots, T *__restrict__ 
     const int slot = slots[token];
     const int b = quotient(token, by_n), i = token - b * n;
     const bool inside = slot >= 0 && slot < c.pages * c.block_rows;
-    const int page = inside ? quotient(slot, by_rows) : 0, row = inside ? slot - page * c.block_rows : 0;
-    const int h0 = blockIdx.y * HEADS;
-    u32x2 raw[HEADS][2];
-    int e[HEADS][2];
+    const int page = inside ? quotient(slot, by_rows) : 0, row = inside ? slot - page * c.block_rows : 0, h = blockIdx.y;
+    const size_t head = (size_t)page * c.heads + h;
+    u32x2 raw[2];
+    int e[2];
 #pragma unroll
-    for (int j = 0; j < HEADS; ++j) {
-        const int h = h0 + j < c.heads ? h0 + j : c.heads - 1;
-        const size_t head = (size_t)page * c.heads + h;
-#pragma unroll
-        for (int tensor = 0; tensor < 2; ++tensor) {
-            raw[j][tensor] = u32x2{0u, 0u};
-            e[j][tensor] = kScaleBias;
-            if (inside) {
-                raw[j][tensor] = *(const u32x2 *)((const unsigned char *)c.data[tensor] + (head * c.block_rows + row) * D + col);
-                e[j][tensor] = c.scales[tensor][head * c.blocks + row / kScaleRows];
-            }
+    for (int tensor = 0; tensor < 2; ++tensor) {
+        raw[tensor] = u32x2{0u, 0u};
+        e[tensor] = kScaleBias;
+        if (inside) {
+            raw[tensor] = *(const u32x2 *)((const unsigned char *)c.data[tensor] + (head * c.block_rows + row) * D + col);
+            e[tensor] = c.scales[tensor][head * c.blocks + row / kScaleRows];
         }
     }
 #pragma unroll
-    for (int j = 0; j < HEADS; ++j) {
-        if (h0 + j >= c.heads) break;
+    for (int tensor = 0; tensor < 2; ++tensor) {
+        int x8 = e[tensor];
+        x8 = x8 < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x8 < kScaleBias + kScaleMost ? x8 : kScaleBias + kScaleMost);
+        const float scale = __builtin_bit_cast(float, x8 << 23);
+        vec8 out;
 #pragma unroll
-        for (int tensor = 0; tensor < 2; ++tensor) {
-            int x8 = e[j][tensor];
-            x8 = x8 < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x8 < kScaleBias + kScaleMost ? x8 : kScaleBias + kScaleMost);
-            const float scale = __builtin_bit_cast(float, x8 << 23);
-            vec8 out;
-#pragma unroll
-            for (int i4 = 0; i4 < 2; ++i4) {
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(raw[j][tensor][i4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(raw[j][tensor][i4], true);
-                out[i4 * 4] = (T)(lo[0] * scale);
-                out[i4 * 4 + 1] = (T)(lo[1] * scale);
-                out[i4 * 4 + 2] = (T)(hi[0] * scale);
-                out[i4 * 4 + 3] = (T)(hi[1] * scale);
-            }
-            *(vec8 *)((tensor ? v_out : k_out) + (((size_t)b * c.heads + h0 + j) * n + i) * D + col) = out;
+        for (int i4 = 0; i4 < 2; ++i4) {
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(raw[tensor][i4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(raw[tensor][i4], true);
+            out[i4 * 4] = (T)(lo[0] * scale);
+            out[i4 * 4 + 1] = (T)(lo[1] * scale);
+            out[i4 * 4 + 2] = (T)(hi[0] * scale);
+            out[i4 * 4 + 3] = (T)(hi[1] * scale);
         }
+        *(vec8 *)((tensor ? v_out : k_out) + (((size_t)b * c.heads + h) * n + i) * D + col) = out;
     }
 #endif
 }
@@ -232,15 +230,13 @@ template <typename T, int D> int launch_write(const Cache8Write &x)
     return (int)hipGetLastError();
 }
 
-template <typename T, int D, int HEADS> int launch_read_heads(const Cache8Read &x)
+template <typename T, int D> int launch_read(const Cache8Read &x)
 {
     const int tokens = x.B * x.n;
-    hipLaunchKernelGGL((cache8_read_kernel<T, D, HEADS>), dim3((unsigned)(((long long)tokens * (D / 8) + 255) / 256), (unsigned)((x.c.heads + HEADS - 1) / HEADS)),
-                       dim3(256), 0, x.stream, x.c, x.slots, (T *)x.out[0], (T *)x.out[1], x.n, tokens, divisor((uint32_t)x.n), divisor((uint32_t)x.c.block_rows));
+    hipLaunchKernelGGL((cache8_read_kernel<T, D>), dim3((unsigned)(((long long)tokens * (D / 8) + 255) / 256), (unsigned)x.c.heads), dim3(256), 0, x.stream, x.c,
+                       x.slots, (T *)x.out[0], (T *)x.out[1], x.n, tokens, divisor((uint32_t)x.n), divisor((uint32_t)x.c.block_rows));
     return (int)hipGetLastError();
 }
-
-template <typename T, int D> int launch_read(const Cache8Read &x) { return launch_read_heads<T, D, 1>(x); }
 
 template <typename T> int launch_write_dim(int D, const Cache8Write &x)
 {
@@ -267,6 +263,8 @@ template <typename T> int launch_read_dim(int D, const Cache8Read &x)
 namespace {
 
 constexpr int64_t kMost = std::numeric_limits<int>::max();
+// Most workgroups, of 256 threads, of a launch: their threads are counted in 32 bits.
+constexpr int64_t kMostGroups = (1 << 24) - 1;
 
 bool misaligned(const void *at, uintptr_t bytes) { return ((uintptr_t)at & (bytes - 1)) != 0; }
 
@@ -358,8 +356,8 @@ int check_attention(int B, int H, int Hkv, int Sq, int Skv, int D, int dtype, un
     if (D != 64 && D != 96 && D != 128 && D != 160) return TSDPA_ERR_UNSUPPORTED_D;
     if (B < 0 || H < 0 || Hkv < 0 || Sq < 0 || Skv < 0) return TSDPA_ERR_BAD_SHAPE;
     const int64_t bh = (int64_t)B * H;
-    // B * H * ceil(Sq / 16) * splits workgroups must fit an int
-    if (bh > kMost || (bh > 0 && Sq > 0 && ((int64_t)Sq + 15) / 16 > kMost / TSDPA_MAX_SPLITS / bh)) return TSDPA_ERR_BAD_SHAPE;
+    // (no form has more than two workgroups for each; how many runs of the keys that leaves room for is for the call to see)
+    if (bh > kMost || (bh > 0 && Sq > 0 && ((int64_t)Sq + 15) / 16 > (kMostGroups - 8) / 2 / bh)) return TSDPA_ERR_BAD_SHAPE;
     // a head is addressed through 32 bits, with room for a "fetch nothing" offset above it
     if (((int64_t)Skv + 1024) * D >= ((int64_t)1 << 30)) return TSDPA_ERR_BAD_SHAPE;
     if (bh > 0 && Sq > 0 && Skv == 0) return TSDPA_ERR_BAD_SHAPE;
@@ -385,7 +383,7 @@ int tiled_sdpa_cache8_write(const tsdpa_cache8 *c, const tsdpa_rows *k, const ts
     // (S tokens of an entry touch a block more than they fill if they begin inside one; none past the capacity)
     const int64_t most = S < capacity ? S : capacity, windows = most <= 1 ? most : (most + 2 * (tsdpa::kScaleRows - 1)) / tsdpa::kScaleRows;
     const int64_t per_entry = windows * c->Hkv;
-    if (B > 0 && per_entry > (kMost - 3) / 2 / B) return TSDPA_ERR_BAD_SHAPE;
+    if (B > 0 && per_entry > kMostGroups * 4 / 2 / B) return TSDPA_ERR_BAD_SHAPE;      // (four units to a workgroup)
     if (B * per_entry == 0 || c->pages == 0) return TSDPA_OK;
     if (incomplete(*c) || !k->data || !v->data || !kv_lens || !new_lens) return TSDPA_ERR_NULL_PTR;
     if (misaligned(c->k, 16) || misaligned(c->v, 16) || misaligned(k->data, 16) || misaligned(v->data, 16) || misaligned(kv_lens, 4) || misaligned(new_lens, 4) ||
@@ -450,6 +448,8 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
         const unsigned long long each = tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, 2) / 2, given = workspace ? workspace_bytes / each : 0;
         if ((unsigned long long)splits > given) splits = given > 1 ? (int)given : 1;
     }
+    // (a tile of 32 or 128 rows takes the place of two of 16 or more; the padding to whole XCDs at most doubles it)
+    if (splits > 1 && splits > (kMostGroups - 16) / ((int64_t)B * H * (((int64_t)Sq + 15) / 16) * 2)) return TSDPA_ERR_BAD_SPLITS;
     if (splits > 1 && (!workspace || misaligned(workspace, 16) || workspace_bytes < tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, splits)))
         return TSDPA_ERR_WORKSPACE;
     tsdpa::Cache8Attend x{args_of(*c), {}};

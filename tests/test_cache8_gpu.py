@@ -322,6 +322,25 @@ def test_nan_reaches_the_rows_that_see_it(Sq, R):
     check_attention(q, host, dev, lens, table, cap, causal=False)
 
 
+def test_write_up_to_the_last_row_that_can_be_counted():
+    """An entry of nearly 2^31 rows, all but the last of whose pages do not exist, and more tokens (one in memory) than it has room for."""
+    blocks, D = (2 ** 31 - 1) // 64, 64
+    table = torch.full((1, blocks), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    dev = on_gpu(new_cache(3, 1, 64, D, 1))
+    before = [x.clone().view(torch.uint8) for x in dev]
+    x = torch.randn(1, 1, 1, D, generator=torch.Generator().manual_seed(1)).half().cuda()
+    S = 2 ** 29
+    lib.cache8_write(x.expand(1, S, 1, D), (2 * x).expand(1, S, 1, D), *dev, i32([blocks * 64 - 64]), i32([blocks * 64]), block_table=table)
+    for got, old in zip(dev, before):
+        got = got.view(torch.uint8)
+        assert torch.equal(got[0], old[0]) and torch.equal(got[2], old[2])
+    k, v = lib.cache8_read(*dev, torch.arange(64, 128, dtype=torch.int32, device="cuda").view(1, 64), torch.float16)
+    for got, want in ((k, x), (v, 2 * x)):
+        want = want.cpu().double().view(1, 1, 1, D)
+        assert ((got.cpu().double() - want).abs() <= want.abs() * 2 ** -4 + 2.0 ** -10 * 2 ** -6).all()
+
+
 # Large tiles of query rows are taken for many scores only, counted by the capacity: a cache of a large one whose entries are short.
 def in_large(dev, table, rows):
     """The cache and block table with a capacity of `rows`; what is added holds NaN codes, pages that do not exist."""

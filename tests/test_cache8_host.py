@@ -110,6 +110,20 @@ def test_default_splits_refuses(lib, kwargs, expect):
     assert lib.tiled_sdpa_cache8_default_splits(*a.values(), ctypes.byref(n)) == expect
 
 
+def test_more_workgroups_than_a_launch_can_have(lib):
+    """A launch's threads are counted in 32 bits: 2^24 - 1 workgroups of 256."""
+    c, r, z = cache(block_table=P, block_rows=64, max_blocks=(1 << 25) - 1, pages=4, Hkv=1), rows(batch=0, row=0, head=0), ctypes.byref
+    args = [z(c), z(r), z(r), None, P, 1]
+    assert lib.tiled_sdpa_cache8_write(*args, (1 << 30) - 96, 0, None) == NULL
+    assert lib.tiled_sdpa_cache8_write(*args, (1 << 30), 0, None) == SHAPE
+    assert lib.tiled_sdpa_cache8_write(*args, (1 << 31) - 1, 0, None) == SHAPE
+    n, c = ctypes.c_int(0), cache(pages=1 << 20, Hkv=1, block_rows=64)
+    for Sq, splits, expect in ((1, 7, WORKSPACE), (1, 8, SPLITS), (1, 128, SPLITS), (100, 1, NULL), (112, 1, NULL), (113, 1, SHAPE)):
+        o = None if expect == NULL else P
+        assert lib.tiled_sdpa_fwd_cache8(z(c), P, o, None, P, 1 << 20, 1, Sq, 0.1, 0, 0, splits, None, 0, None) == expect
+        assert lib.tiled_sdpa_cache8_default_splits(1 << 20, 1, 1, Sq, 64, 64, 0, 0, z(n)) == (SHAPE if expect == SHAPE else OK)
+
+
 def test_default_splits(lib):
     """At least one, at most TSDPA_MAX_SPLITS, one where heads are many, and never fewer for a longer cache of few rows (a workspace for the capacity)."""
     for D in (64, 96, 128, 160):
