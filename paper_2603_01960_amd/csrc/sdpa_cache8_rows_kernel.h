@@ -136,11 +136,17 @@ template <> struct ReadRows<160> {
 #undef TSDPA_RD_V
 #undef TSDPA_RD_WAIT
 
+// Entries of up to this number that differ in length come longest first where there are more workgroups than start at once: else a long one may be the last, and
+// others wait for it.  (us, in an order of chance that is least / most in favour of it: 4 entries of 500 queries of 32 heads over 8, 1408 ... 3712 keys, D = 128,
+// FP16 107.9 -> 101.7 / 100.2 -> 100.9; 16 of 64 queries, 314 ... 4000 keys, D = 64 35.0 -> 30.0 / 29.7 -> 30.0; all of 2560 keys 100.0 -> 100.9.  For 64 entries
+// finding the order took as long as it gained.)
+constexpr int kRanked = 16;
 // Which workgroup has which tile of query rows of which unit (a head's run of keys).  A unit's tiles follow one another on one XCD, whose L2
 // the keys then come from; where the units are no multiple of the 8 XCDs each is dealt to several, tile by tile, so that all have as many
 // (4 heads of 64 tiles, 4096 keys, D = 128: 37.4 -> 27.4 us).
 struct RowsOrder {
     int row_tiles, tiles, log2_parts;             // tiles of a unit, of one of its parts
+    int ranked;                                   // entries, where they come longest first; else 0
     Divisor by_tiles, by_splits, by_entry_heads, by_rows;
 };
 
@@ -165,13 +171,26 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
     const int unit = part >> order.log2_parts;
     const int qt = order.row_tiles - 1 - (((y - yt * order.tiles) << order.log2_parts) + (part & ((1 << order.log2_parts) - 1)));
     if (unit >= units || qt < 0) return;
-    const int head = divide(unit, order.by_splits), sp = unit - head * splits;
-    const int hpb = cache.heads, b = divide(head, order.by_entry_heads), h = head - b * hpb;
+    int head = divide(unit, order.by_splits);
+    const int sp = unit - head * splits, hpb = cache.heads;
+    int b = divide(head, order.by_entry_heads);
+    const int h = head - b * hpb;
     int len = Skv_cap;
-    if (kv_lens != nullptr) {
+    if (order.ranked > 0) {
+        const int own = lane < order.ranked ? (kv_lens[lane] > 0 ? kv_lens[lane] : 0) : -1;
+        int rank = 0;
+#pragma unroll
+        for (int j = 0; j < kRanked; ++j) {
+            const int other = __builtin_amdgcn_readlane(own, j);
+            rank += other > own || (other == own && j < lane) ? 1 : 0;
+        }
+        b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == b && lane < order.ranked));
+        head = b * hpb + h;
+        len = __builtin_amdgcn_readlane(own, b);
+    } else if (kv_lens != nullptr) {
         len = kv_lens[b];
-        len = len < 0 ? 0 : (len < Skv_cap ? len : Skv_cap);
     }
+    len = len < 0 ? 0 : (len < Skv_cap ? len : Skv_cap);
     // the run of tiles [t0, t0 + n) of those that the tile's last row sees
     const int Sp = rows_per_head, koff = len - Sp, r0 = qt * TM, last_row = (r0 + TM < S ? r0 + TM : S) - 1;
     const int g0 = divide(r0, order.by_rows), g1 = divide(last_row, order.by_rows);
@@ -329,20 +348,15 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sacc[nb][e] = 0.f;
-            // (each operand is converted one product ahead, and no further: all at once do not fit the registers)
-            auto keys = [&](int x) __attribute__((always_inline)) {
-                const int kk = x / NB, nb = x % NB;
-                return Codes<T>::wide(kf[nb][kk >> 1][(kk & 1) * 2], kf[nb][kk >> 1][(kk & 1) * 2 + 1]);
-            };
-            vec8 next = keys(0);
+            // (the wavefront that has products to do goes before the other one's softmax: 1 ... 4 % where the GPU is full)
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int x = 0; x < KK * NB; ++x) {
-                const vec8 now = next;
-                if (x + 1 < KK * NB) next = keys(x + 1);
-                sacc[x % NB] = Elem<T>::mfma(now, qf[x / NB], sacc[x % NB]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    sacc[nb] = Elem<T>::mfma(Codes<T>::wide(kf[nb][kk >> 1][(kk & 1) * 2], kf[nb][kk >> 1][(kk & 1) * 2 + 1]), qf[kk], sacc[nb]);
         }
+        __builtin_amdgcn_s_setprio(0);
         TileScales x8(scale_next, c);
         const bool masked = tile * TN + TN - 1 > klim_least;
         const int last = klim - (tile * TN + g * 4);          // the last of the tile's keys that this lane's row sees, from the lane's first
@@ -394,15 +408,13 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
                 }
             }
         }
-        auto values = [&](int x) __attribute__((always_inline)) { return Codes<_Float16>::wide(vf[x % DB][x / DB][0], vf[x % DB][x / DB][1]); };
-        f16x8 next = values(0);
+        __builtin_amdgcn_s_setprio(2);
 #pragma unroll
-        for (int x = 0; x < 4 * DB; ++x) {
-            const f16x8 now = next;
-            if (x + 1 < 4 * DB) next = values(x + 1);
-            oacc[x % DB] = Elem<_Float16>::mfma(now, pb[x / DB >> 1][x / DB & 1], oacc[x % DB]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                oacc[db] = Elem<_Float16>::mfma(Codes<_Float16>::wide(vf[db][x][0], vf[db][x][1]), pb[x >> 1][x & 1], oacc[db]);
+        __builtin_amdgcn_s_setprio(0);
         tile += NW;
     }
 
@@ -477,9 +489,10 @@ template <typename T, int D, bool PAGED> int launch_cache8_rows_one(const Cache8
     while (log2_parts < 3 && ((units << log2_parts) & 7) != 0) ++log2_parts;
     if (row_tiles < 2 << log2_parts) log2_parts = 0;
     const int tiles = (row_tiles + (1 << log2_parts) - 1) >> log2_parts;
-    const RowsOrder order{row_tiles, tiles, log2_parts, divisor((uint32_t)tiles), divisor((uint32_t)a.splits), divisor((uint32_t)a.heads_per_batch),
-                          divisor((uint32_t)a.rows_per_head)};
     const long long groups = ((((long long)units << log2_parts) + 7) / 8) * 8 * tiles;
+    const int ranked = a.kv_lens && a.splits == 1 && groups > 512 && a.batches > 1 && a.batches <= kRanked ? a.batches : 0;
+    const RowsOrder order{row_tiles, tiles, log2_parts, ranked, divisor((uint32_t)tiles), divisor((uint32_t)a.splits), divisor((uint32_t)a.heads_per_batch),
+                          divisor((uint32_t)a.rows_per_head)};
     hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c, a.S, a.BH, units, order, a.c, a.qsign, a.causal,
                        a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens);
     return (int)hipGetLastError();

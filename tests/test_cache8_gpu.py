@@ -429,6 +429,18 @@ def test_small_tiles_over_the_chip(B, Hkv, Sq, splits):
     check_attention(q, host, dev, lens, table, cap, causal=True, splits=splits)
 
 
+@pytest.mark.parametrize("lens", [[128, -7, 50, 0, -1], [1, 2, 128, 2, 128], [-3] * 5, [70, 69, 68, 67, 66]])
+def test_small_tiles_longest_entry_first(lens):
+    """More workgroups than start at once; entries in any order, lengths that are none."""
+    B, Hkv, cap, D, Sq = 5, 8, 128, 64, 412
+    have = [max(0, x) for x in lens]
+    host, dev, table = filled(B, Hkv, cap, D, have, 0, seed=3)
+    q = torch.randn(B, Hkv, Sq, D, generator=torch.Generator().manual_seed(Sq)).to(torch.bfloat16).cuda()
+    want, want_lse = check_attention(q, host, dev, have, table, cap, causal=False)
+    o, lse = lib.sdpa_kv8(q, *dev, kv_lens=i32(lens), return_lse=True)
+    assert torch.equal(o, want) and torch.equal(lse, want_lse)
+
+
 @pytest.mark.parametrize("Skv,Sq", [(2000, 1), (9000, 1), (2000, 60)])
 def test_workspace_and_out(Skv, Sq):
     host, dev, table = filled(1, 2, Skv, 64, [Skv], 0, seed=4)
