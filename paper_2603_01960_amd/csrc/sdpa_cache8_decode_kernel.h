@@ -53,7 +53,7 @@ template <int D> struct Read8;
 template <> struct Read8<64> {
     static __device__ __forceinline__ void keys(u32x4 (&x)[4][1], u32x2 (&)[4], const uint32_t (&p)[1])
     {
-        asm volatile(TSDPA_RD_K(0, 4, 0) TSDPA_RD_K(1, 4, 1024) TSDPA_RD_K(2, 4, 2048) TSDPA_RD_K(3, 4, 3072) TSDPA_RD_WAIT
+        asm volatile(TSDPA_RD_K(0, 4, 0) TSDPA_RD_K(1, 4, 1024) TSDPA_RD_K(2, 4, 2048) TSDPA_RD_K(3, 4, 3 * 1024) TSDPA_RD_WAIT
                      : "=&v"(x[0][0]), "=&v"(x[1][0]), "=&v"(x[2][0]), "=&v"(x[3][0])
                      : "v"(p[0])
                      : "memory");
@@ -71,15 +71,15 @@ template <> struct Read8<64> {
 template <> struct Read8<96> {
     static __device__ __forceinline__ void keys(u32x4 (&x)[4][1], u32x2 (&y)[4], const uint32_t (&p)[2])
     {
-        asm volatile(TSDPA_RD_K(0, 8, 0) TSDPA_RD_K(1, 8, 1536) TSDPA_RD_K(2, 8, 3072) TSDPA_RD_K(3, 8, 4608)
-                     TSDPA_RD_K8(4, 9, 0) TSDPA_RD_K8(5, 9, 1536) TSDPA_RD_K8(6, 9, 3072) TSDPA_RD_K8(7, 9, 4608) TSDPA_RD_WAIT
+        asm volatile(TSDPA_RD_K(0, 8, 0) TSDPA_RD_K(1, 8, 1536) TSDPA_RD_K(2, 8, 3 * 1024) TSDPA_RD_K(3, 8, 4608)
+                     TSDPA_RD_K8(4, 9, 0) TSDPA_RD_K8(5, 9, 1536) TSDPA_RD_K8(6, 9, 3 * 1024) TSDPA_RD_K8(7, 9, 4608) TSDPA_RD_WAIT
                      : "=&v"(x[0][0]), "=&v"(x[1][0]), "=&v"(x[2][0]), "=&v"(x[3][0]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
                      : "v"(p[0]), "v"(p[1])
                      : "memory");
     }
     static __device__ __forceinline__ void values(u32x2 (&x)[6][2], const uint32_t (&p)[2])
     {
-        asm volatile(TSDPA_RD_V(0, 12, 0) TSDPA_RD_V(1, 12, 3072) TSDPA_RD_V(2, 13, 0) TSDPA_RD_V(3, 13, 3072)
+        asm volatile(TSDPA_RD_V(0, 12, 0) TSDPA_RD_V(1, 12, 3 * 1024) TSDPA_RD_V(2, 13, 0) TSDPA_RD_V(3, 13, 3 * 1024)
                      TSDPA_RD_V(4, 12, 32) TSDPA_RD_V(5, 12, 3104) TSDPA_RD_V(6, 13, 32) TSDPA_RD_V(7, 13, 3104)
                      TSDPA_RD_V(8, 12, 64) TSDPA_RD_V(9, 12, 3136) TSDPA_RD_V(10, 13, 64) TSDPA_RD_V(11, 13, 3136) TSDPA_RD_WAIT
                      : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),

@@ -55,8 +55,8 @@ template <> struct ReadRows<64> {
     }
     static __device__ __forceinline__ void values(u32x2 (&x)[2][4], const uint32_t (&p)[2])
     {
-        asm volatile(TSDPA_RD_V(0, 8, 0) TSDPA_RD_V(1, 8, 1024) TSDPA_RD_V(2, 8, 2048) TSDPA_RD_V(3, 8, 3072)
-                     TSDPA_RD_V(4, 9, 0) TSDPA_RD_V(5, 9, 1024) TSDPA_RD_V(6, 9, 2048) TSDPA_RD_V(7, 9, 3072) TSDPA_RD_WAIT
+        asm volatile(TSDPA_RD_V(0, 8, 0) TSDPA_RD_V(1, 8, 1024) TSDPA_RD_V(2, 8, 2048) TSDPA_RD_V(3, 8, 3 * 1024)
+                     TSDPA_RD_V(4, 9, 0) TSDPA_RD_V(5, 9, 1024) TSDPA_RD_V(6, 9, 2048) TSDPA_RD_V(7, 9, 3 * 1024) TSDPA_RD_WAIT
                      : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]),
                        "=&v"(x[1][2]), "=&v"(x[1][3])
                      : "v"(p[0]), "v"(p[1])
@@ -66,7 +66,7 @@ template <> struct ReadRows<64> {
 template <> struct ReadRows<96> {
     static __device__ __forceinline__ void keys(u32x4 (&x)[2][3], const uint32_t (&p)[1])
     {
-        asm volatile(TSDPA_RD_K(0, 6, 0) TSDPA_RD_K(1, 6, 32) TSDPA_RD_K(2, 6, 64) TSDPA_RD_K(3, 6, 3072)
+        asm volatile(TSDPA_RD_K(0, 6, 0) TSDPA_RD_K(1, 6, 32) TSDPA_RD_K(2, 6, 64) TSDPA_RD_K(3, 6, 3 * 1024)
                      TSDPA_RD_K(4, 6, 3104) TSDPA_RD_K(5, 6, 3136) TSDPA_RD_WAIT
                      : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2])
                      : "v"(p[0])
@@ -74,9 +74,9 @@ template <> struct ReadRows<96> {
     }
     static __device__ __forceinline__ void values(u32x2 (&x)[3][4], const uint32_t (&p)[3])
     {
-        asm volatile(TSDPA_RD_V(0, 12, 0) TSDPA_RD_V(1, 12, 1536) TSDPA_RD_V(2, 12, 3072) TSDPA_RD_V(3, 12, 4608)
-                     TSDPA_RD_V(4, 13, 0) TSDPA_RD_V(5, 13, 1536) TSDPA_RD_V(6, 13, 3072) TSDPA_RD_V(7, 13, 4608)
-                     TSDPA_RD_V(8, 14, 0) TSDPA_RD_V(9, 14, 1536) TSDPA_RD_V(10, 14, 3072) TSDPA_RD_V(11, 14, 4608) TSDPA_RD_WAIT
+        asm volatile(TSDPA_RD_V(0, 12, 0) TSDPA_RD_V(1, 12, 1536) TSDPA_RD_V(2, 12, 3 * 1024) TSDPA_RD_V(3, 12, 4608)
+                     TSDPA_RD_V(4, 13, 0) TSDPA_RD_V(5, 13, 1536) TSDPA_RD_V(6, 13, 3 * 1024) TSDPA_RD_V(7, 13, 4608)
+                     TSDPA_RD_V(8, 14, 0) TSDPA_RD_V(9, 14, 1536) TSDPA_RD_V(10, 14, 3 * 1024) TSDPA_RD_V(11, 14, 4608) TSDPA_RD_WAIT
                      : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]),
                        "=&v"(x[1][2]), "=&v"(x[1][3]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[2][2]), "=&v"(x[2][3])
                      : "v"(p[0]), "v"(p[1]), "v"(p[2])
