@@ -321,10 +321,15 @@ Form form_of(int B, int heads, int rows, int Skv)
 
 // Splits along the key axis.
 // Decoding: one workgroup per CU in all, of runs of at least 512 keys, or 256 while there are up to eight, which
-// the kernel combines itself.  None from half as many key/value heads as CUs on, and none where a pass over a head's keys takes no longer than the
-// second look at the states.  (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 4 rows per head: 8 heads of 1024 keys 7.8 / 8.7 / 8.0 / 8.1; of 2048
+// the kernel combines itself.  None where a pass over a head's keys takes no longer than the second look at the states.
+// (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 4 rows per head: 8 heads of 1024 keys 7.8 / 8.7 / 8.0 / 8.1; of 2048
 // 11.5 / 10.5 / 8.9 / 8.1 / 9.6; of 8192 33.5 / 21.8 / 14.7 / 11.1 / 10.0, 32 splits 9.6; 64 heads of 1024 keys 7.9 / 8.9 / 8.6, of 4096 18.8 / 15.7
-// / 15.8 / 16.2; 128 heads of 2048 13.3 / 16.4 / 16.7, of 4096 28.0 / 28.7 / 29.6; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6.)
+// / 15.8 / 16.2; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6.)
+// From half as many key/value heads as CUs on none either, with two exceptions where runs are long.  CUs get equal shares of the memory's rate, and one
+// reaches 2.4 times that at most (58 GB/s): so 128 heads do not reach it all, and of 257 ... 448 heads those that share a CU take twice as
+// long (1 / 2 / 3 splits, FP16: 128 heads of 2048 keys 13.3 / 16.4, of 4096 28.0 / 28.7, of 8192 54 / 51, in pages 60 / 54, of 16384 100 / 96, 113 / 99; 192 of 16384 133 / 145;
+// 256 of 8192 95 / 98 / 98; 264 of 16384 260 / 218 / 209, of 4096 ... 16384 134 / 138 / 144; 320 of 8192 136 / 124 / 122; 384 of 16384 301 / 273 / 281, of 4096 ... 16384 208 / 195
+// / 193; 512 of 16384 353 / 357 / 368).
 // Tiles of 32 rows: the same, of runs of at least 256 keys and none up to 1024; two workgroups per CU where the runs are longer than 8192 keys all the same.
 // (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 8 heads of 64 rows: 1024 keys 10.6 / 10.5 / - / 10.2 / 11.4, 2048 15.0 / 12.9 / - / 10.4 / 11.5, 4096 23.9 / 17.5 / - /
 // 11.5 / 11.8; of 256 rows: 1024 10.7 / 11.2 / 11.1, 2048 15.5 / 13.4 / 12.4 / 16.0, 8192 42.9 / - / 20.5 / 21.3 / 27.4, 65536 309 / - / 101 / 88 / 96.)
@@ -343,6 +348,7 @@ int default_splits(int B, int heads, int rows, int Skv, int D)
         if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000)) return 1;
         const int64_t tiles = (int64_t)heads * ((rows + 15) / 16), few = Skv / 256 < 8 ? Skv / 256 : 8;
         want = tiles >= 128 ? 1 : 256 / tiles;
+        if ((int64_t)Skv * D >= 1 << 20) want = tiles > 256 && tiles <= 448 ? 3 : tiles >= 128 && tiles <= 160 ? 2 : want;
         most = Skv / 512 > few ? Skv / 512 : few;
     }
     if (want > most) want = most;

@@ -211,8 +211,10 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         return;
     }
 
-    // ---- tiles: HBM -> LDS.  Wavefront w takes the tiles w, w + NW, ... of the run, entered at a tile that depends on the workgroup (heads of
-    // a dense cache lie a power of two apart: in step they would keep hitting the same memory channels).
+    // ---- tiles: HBM -> LDS.  Wavefront w takes the tiles w, w + NW, ... of the run, entered at a tile that depends on the workgroup and exchanged by a
+    // number that does too (heads of a dense cache lie a power of two apart: in step they would keep hitting the same memory channels, and so would
+    // those of them that a start of its own has brought together by chance.  The exchange, one run per head, us: 128 heads of 16384 keys, D = 128 123 -> 100,
+    // 192 150 -> 133, 256 195 -> 181, 512 406 -> 353; in pages, as they come, and with 20000 keys 0 ... 3 %).
     const lds_ptr kslot = lds + wave * 2 * G::TILE, vslot = kslot + G::TILE;
     const unsigned char *kbase = (const unsigned char *)cache.data[0], *vbase = (const unsigned char *)cache.data[1];
     const size_t head_off = (size_t)head * (size_t)Skv_cap * D;
@@ -262,16 +264,19 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     int cur = wave + rot;                         // within the run
     if (cur >= n) cur -= n;
     auto advance = [&](int x) __attribute__((always_inline)) { x += NW; return x >= n ? x - n : x; };
+    const int most = n >= 256 ? 255 : 0x7fffffff >> __builtin_clz(n | 1);        // (the largest 2^i - 1 below n)
+    const int mix = n > NW ? (int)((blockIdx.x * 2654435761u) >> 16) & most : 0;
+    auto tile_of = [&](int x) __attribute__((always_inline)) { return t0 + ((x | most) < n ? x ^ mix : x); };
 
     // The first tile's K goes out before anything else is worked out, then its exponents, Q, and V, in the order in which they are needed.
     int page_next = 0, scale_next = 0;
-    if constexpr (PAGED) page_next = page_of(mine > 0 ? t0 + cur : 0);
-    const Src first = src_of(t0 + cur, mine > 0, page_next);
+    if constexpr (PAGED) page_next = page_of(mine > 0 ? tile_of(cur) : 0);
+    const Src first = src_of(tile_of(cur), mine > 0, page_next);
 #pragma unroll
     for (int u = 0; u < G::P; ++u) kgoff[u] = offset(u, G::kx);
     load_k(first);
     __builtin_amdgcn_sched_barrier(0);
-    scale_next = load_scale(mine > 0 ? t0 + cur : 0, page_next);
+    scale_next = load_scale(mine > 0 ? tile_of(cur) : 0, page_next);
     // ---- Q rows as MFMA B-operands.  The order of the products over D is free: lane t of a row takes bytes t * 16 ... of each 64 columns of K,
     // of the last 32 (D = 96, 160) t * 8 ..., and Q's columns are those.
     vec8 qf[KS];
@@ -287,7 +292,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     for (int u = 0; u < G::P; ++u) vgoff[u] = offset(u, G::vx);
     load_v(first);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (PAGED) page_next = page_of(mine > 1 ? t0 + advance(cur) : mine > 0 ? t0 : 0);
+    if constexpr (PAGED) page_next = page_of(mine > 1 ? tile_of(advance(cur)) : mine > 0 ? t0 : 0);
     // key j contributes to this lane's row iff j <= klim; every tile that ends behind klim_least takes the masked path
     const int klim = causal ? row - divide(row, order.by_rows) * rows_per_head + len - rows_per_head : len - 1;
     const int klim_least = causal ? len - rows_per_head : len - 1;
@@ -356,11 +361,11 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     };
 
     for (int i = 0; i < mine; ++i) {
-        const int next = advance(cur);
+        const int next = advance(cur), tile = tile_of(cur);
         const bool more = i + 1 < mine;
-        const Src s = src_of(t0 + next, more, page_next);
+        const Src s = src_of(tile_of(next), more, page_next);
         const int page_of_next = page_next;
-        if constexpr (PAGED) page_next = page_of(i + 2 < mine ? t0 + advance(next) : t0);
+        if constexpr (PAGED) page_next = page_of(i + 2 < mine ? tile_of(advance(next)) : t0);
         // In flight, in this order: the tile's K, its exponents, its V.  (K has landed when at most V's loads are outstanding, V when at most
         // the next K's are.  A load of the exponents that the compiler moves makes these waits longer, never shorter.)
         u32x4 kf[4][G::KC];
@@ -382,14 +387,14 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
                 else a = Codes<T>::wide(kf[blk][ks >> 1][(ks & 1) * 2], kf[blk][ks >> 1][(ks & 1) * 2 + 1]);
                 sacc[blk] = Elem16<T>::mfma(a, qf[ks], sacc[blk]);
             }
-        const int key0 = (t0 + cur) * kTile8 + t * 4;
-        const bool masked = (t0 + cur) * kTile8 + kTile8 - 1 > klim_least;
+        const int key0 = tile * kTile8 + t * 4;
+        const bool masked = tile * kTile8 + kTile8 - 1 > klim_least;
         if (masked) softmax(sacc, key0, scale, i == 0, std::true_type{});
         else softmax(sacc, key0, scale, i == 0, std::false_type{});
         u32x2 vf[DB][2];
         TSDPA_WAIT_VMCNT(NU);
         Read8<D>::values(vf, vptr);
-        scale_next = load_scale(more ? t0 + next : t0 + cur, page_of_next);
+        scale_next = load_scale(more ? tile_of(next) : tile, page_of_next);
         load_v(s);
         bool nan = false;
         if (masked && causal) {
