@@ -211,10 +211,11 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         return;
     }
 
-    // ---- tiles: HBM -> LDS.  Wavefront w takes the tiles w, w + NW, ... of the run, entered at a tile that depends on the workgroup and exchanged by a
-    // number that does too (heads of a dense cache lie a power of two apart: in step they would keep hitting the same memory channels, and so would
+    // ---- tiles: HBM -> LDS.  Wavefront w takes the tiles w, w + NW, ... of the run, entered at a tile that depends on the workgroup, and in a dense cache
+    // exchanged by a number that does too (heads lie a power of two apart: in step they would keep hitting the same memory channels, and so would
     // those of them that a start of its own has brought together by chance.  The exchange, one run per head, us: 128 heads of 16384 keys, D = 128 123 -> 100,
-    // 192 150 -> 133, 256 195 -> 181, 512 406 -> 353; in pages, as they come, and with 20000 keys 0 ... 3 %).
+    // 192 150 -> 133, 256 195 -> 181, 512 406 -> 353, of 20000 keys 0 ... 4 %; in pages, which lie as they come, entries of one length are level with it and
+    // unequal ones 1 ... 2 % slower, 69.4 -> 70.5).
     const lds_ptr kslot = lds + wave * 2 * G::TILE, vslot = kslot + G::TILE;
     const unsigned char *kbase = (const unsigned char *)cache.data[0], *vbase = (const unsigned char *)cache.data[1];
     const size_t head_off = (size_t)head * (size_t)Skv_cap * D;
@@ -265,8 +266,8 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     if (cur >= n) cur -= n;
     auto advance = [&](int x) __attribute__((always_inline)) { x += NW; return x >= n ? x - n : x; };
     const int most = n >= 256 ? 255 : 0x7fffffff >> __builtin_clz(n | 1);        // (the largest 2^i - 1 below n)
-    const int mix = n > NW ? (int)((blockIdx.x * 2654435761u) >> 16) & most : 0;
-    auto tile_of = [&](int x) __attribute__((always_inline)) { return t0 + ((x | most) < n ? x ^ mix : x); };
+    const int mix = !PAGED && n > NW ? (int)((blockIdx.x * 2654435761u) >> 16) & most : 0;
+    auto tile_of = [&](int x) __attribute__((always_inline)) { return t0 + (!PAGED && (x | most) < n ? x ^ mix : x); };
 
     // The first tile's K goes out before anything else is worked out, then its exponents, Q, and V, in the order in which they are needed.
     int page_next = 0, scale_next = 0;
