@@ -564,7 +564,7 @@ int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out,
  *   lse          : NULL or FP32 [B, H, Sq].
  *   kv_lens      : device int32 [B], rows of each entry, clamped to [0, capacity]; of a dense cache NULL = all of them hold block_rows.
  *   flags        : TSDPA_FLAG_CAUSAL (the queries are the last Sq positions: needs a capacity of Sq or more) or 0.
- *   splits, workspace : as for tiled_sdpa_fwd_kv; 0 = tiled_sdpa_cache8_default_splits of the capacity, or fewer, as many as the workspace
+ *   splits, workspace : as for tiled_sdpa_fwd_kv; 0 = at most tiled_sdpa_cache8_default_splits of the capacity, and no more than the workspace
  *                  has room for.  tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, n) bytes hold n.  B * H * ceil(Sq / 16), times splits, is at
  *                  most 2^23 - 16.
  *

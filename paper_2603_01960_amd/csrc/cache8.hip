@@ -303,20 +303,21 @@ bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !
 
 // Which kernel: decoding up to 32 query rows per key/value head (two tiles of 16), beyond that tiles of 32 rows (sdpa_cache8_rows_kernel.h) or of 128
 // (sdpa_cache8_chunk_kernel.h).  Tiles of 128 do a seventh less work per row, but have to be filled, and a wavefront of theirs passes over four times
-// as many keys: tiles of 32 where those of 128 would be half empty (3.5 of them cost as much as one), and up to 2^27 scores.  Entries of a batch differ in
-// length as a rule, which costs large tiles more, and the capacity is an upper bound of all of them: 2^28.
+// as many keys: tiles of 32 where those of 128 would be half empty (3.5 of them cost as much as one), and up to 2^27 scores.  Where entries have
+// lengths of their own, these may be much shorter than the capacity, and unequal, both of which cost large tiles more: up to 2^28 scores, or 1024 tiles.
 // (us, tiles of 32 / of 128, BF16, D = 128: 8 heads of 64 rows, 8192 keys 13.0 / 22.3; 8 of 256 rows, 2048 keys 12.4 / 22.6, 8192 keys 20.5 / 32.5, 65536 keys
 // 88 / 90; 32 of 512, 2048 keys 25.5 / 38.7; 8 of 1024, 8192 keys 45 / 51, 65536 keys 307 / 271; 64 of 512, 4096 keys 83 / 84; 8 of 4096, 8192 keys 149 / 141;
-// 8 of 16384, 16384 keys 1042 / 899; 1024 of 64, 2048 keys 124 / 164; 4 entries of 8 heads of 2000 rows, 2560 keys each 102 / 93, 1408 ... 3712 keys 103 / 112.)
+// 8 of 16384, 16384 keys 1042 / 899; 1024 of 64, 2048 keys 124 / 164; 4 entries of 8 heads of 2000 rows, 2560 keys each 102 / 93, 1408 ... 3712 keys 103 / 112.  In
+// pages, a capacity of 131072 keys: 8 heads of 256 rows, 2000 keys 17 / 30, 120000 keys 150 / 165; of 2048 rows 26 / 43, 1112 / 1023; of 4096 rows 43 / 59, 2186 / 2017; 8
+// entries of 8 heads, capacity 32768: 512 rows, 800 ... 1500 keys 37 / 49, 15300 ... 16000 keys 296 / 296; 2048 rows 109 / 103, 1132 / 1068.)
 enum class Form { decode, rows, chunk };
 constexpr int kDecodeRows = 32;
-Form form_of(int B, int heads, int rows, int Skv)
+Form form_of(int heads, int rows, int Skv, bool lengths)
 {
     if (rows <= kDecodeRows) return Form::decode;
     const int64_t small = ((int64_t)rows + 31) / 32, large = ((int64_t)rows + 127) / 128;
-    // (rows * Skv < 2^61)
-    if (2 * small <= 7 * large || (int64_t)rows * Skv <= ((int64_t)1 << (B > 1 ? 28 : 27)) / heads) return Form::rows;
-    return Form::chunk;
+    if (2 * small <= 7 * large || (lengths && heads * small <= 1024)) return Form::rows;
+    return (int64_t)rows * Skv <= ((int64_t)1 << (lengths ? 28 : 27)) / heads ? Form::rows : Form::chunk;       // (rows * Skv < 2^61)
 }
 
 // Splits along the key axis.
@@ -333,9 +334,8 @@ Form form_of(int B, int heads, int rows, int Skv)
 // Tiles of 32 rows: the same, of runs of at least 256 keys and none up to 1024; two workgroups per CU where the runs are longer than 8192 keys all the same.
 // (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 8 heads of 64 rows: 1024 keys 10.6 / 10.5 / - / 10.2 / 11.4, 2048 15.0 / 12.9 / - / 10.4 / 11.5, 4096 23.9 / 17.5 / - /
 // 11.5 / 11.8; of 256 rows: 1024 10.7 / 11.2 / 11.1, 2048 15.5 / 13.4 / 12.4 / 16.0, 8192 42.9 / - / 20.5 / 21.3 / 27.4, 65536 309 / - / 101 / 88 / 96.)
-int default_splits(int B, int heads, int rows, int Skv, int D)
+int default_splits(Form form, int heads, int rows, int Skv, int D)
 {
-    const Form form = form_of(B, heads, rows, Skv);
     if (form == Form::chunk) return tsdpa::row_tile_splits(heads, rows, Skv, D);
     int64_t want, most;
     if (form == Form::rows) {
@@ -425,7 +425,13 @@ int tiled_sdpa_cache8_default_splits(int B, int H, int Hkv, int Sq, int Skv, int
     if (!splits) return TSDPA_ERR_NULL_PTR;
     const int st = check_attention(B, H, Hkv, Sq, Skv, D, dtype, flags);
     if (st != TSDPA_OK) return st;
-    *splits = (int64_t)B * H * Sq == 0 ? 1 : default_splits(B, B * Hkv, H / Hkv * Sq, Skv, D);
+    *splits = 1;
+    if ((int64_t)B * H * Sq == 0) return TSDPA_OK;
+    const int heads = B * Hkv, rows = H / Hkv * Sq;
+    for (const bool lengths : {false, true}) {    // (room for either)
+        const int n = default_splits(form_of(heads, rows, Skv, lengths), heads, rows, Skv, D);
+        if (n > *splits) *splits = n;
+    }
     return TSDPA_OK;
 }
 
@@ -448,8 +454,9 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     if (std::isinf(scale)) return TSDPA_ERR_BAD_SCALE;
     if (splits < 0 || splits > TSDPA_MAX_SPLITS) return TSDPA_ERR_BAD_SPLITS;
     const int rows = H / c->Hkv * Sq, heads = B * c->Hkv;
+    const Form form = form_of(heads, rows, capacity, kv_lens != nullptr);
     if (splits == 0) {
-        splits = default_splits(B, heads, rows, capacity, c->D);
+        splits = default_splits(form, heads, rows, capacity, c->D);
         // (with less memory than that takes: as many as fit)
         const unsigned long long each = tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, 2) / 2, given = workspace ? workspace_bytes / each : 0;
         if ((unsigned long long)splits > given) splits = given > 1 ? (int)given : 1;
@@ -479,7 +486,6 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     a.stream = (hipStream_t)stream;
     // The decoding kernel combines the runs itself while their states are few (the conditions of the 16-bit caches' in tiled_sdpa.hip)
     if (rows <= 8 && splits > 1 && splits * rows <= 32 && splits <= rows * c->D / 4 && rows * c->D <= 1024) a.ticket = tsdpa::new_ticket();
-    const Form form = form_of(B, heads, rows, capacity);
     int err;
     if (form == Form::chunk) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_chunk_f16(c->D, x) : tsdpa::launch_cache8_chunk_bf16(c->D, x);
     else if (form == Form::rows) err = dtype == TSDPA_F16 ? tsdpa::launch_cache8_rows_f16(c->D, x) : tsdpa::launch_cache8_rows_bf16(c->D, x);

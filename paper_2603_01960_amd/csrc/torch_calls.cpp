@@ -1105,7 +1105,7 @@ PyObject *call_sdpa_cache8(PyObject *, PyObject *const *args, Py_ssize_t n)
             if (st != TSDPA_OK) return PyLong_FromLong(st);
         }
         const Workspace ws(args[12], tiled_sdpa_kv_workspace_bytes(B, H, Sq, cache.c.D, splits), q);
-        if (heuristic && args[12] != Py_None) splits = 0;      // (what fits the caller's buffer: the library decides)
+        if (heuristic) splits = 0;                // (the library decides, within the workspace)
         const Launch on(q);
         const int st = without_gil(tiled_sdpa_fwd_cache8, (const tsdpa_cache8 *)&cache.c, (const void *)data(q), data(out), with_lse ? (float *)data(lse) : nullptr,
                                    lens, B, H, Sq, scale, dtype, flags, splits, ws.ptr, ws.bytes, on.stream);

@@ -341,7 +341,10 @@ def test_write_up_to_the_last_row_that_can_be_counted():
         assert ((got.cpu().double() - want).abs() <= want.abs() * 2 ** -4 + 2.0 ** -10 * 2 ** -6).all()
 
 
-# Large tiles of query rows are taken for many scores only, counted by the capacity: a cache of a large one whose entries are short.
+# Large tiles of query rows are taken for many of them and many scores, counted by the capacity: a cache of many heads and a large capacity whose entries are short.
+LARGE = 1 << 14
+
+
 def in_large(dev, table, rows):
     """The cache and block table with a capacity of `rows`; what is added holds NaN codes, pages that do not exist."""
     if table is not None:
@@ -357,54 +360,63 @@ def in_large(dev, table, rows):
     return out, None
 
 
-def check_large(q, host, dev, lens, table, cap, rows, causal, scale=None, **more):
-    dev, wide = in_large(dev, table, rows)
+def check_large(q, host, dev, lens, table, cap, causal, scale=None, **more):
+    """Some heads of it: the first two and the last."""
+    B, H, Sq, D = q.shape
+    Hkv = host[0].shape[1]
+    G, small = H // Hkv, -(-H // Hkv * Sq // 32)
+    assert B * Hkv * small > 1024 and 2 * small > 7 * -(-small // 4) and B * H * Sq * LARGE > 1 << 28       # (what it takes)
+    dev, wide = in_large(dev, table, LARGE)
     lens_gpu = i32(lens)
     if wide is None:
-        got = lib.sdpa_kv8(q, *dev, causal=causal, scale=scale, kv_lens=lens_gpu, return_lse=True, **more)
+        o, lse = lib.sdpa_kv8(q, *dev, causal=causal, scale=scale, kv_lens=lens_gpu, return_lse=True, **more)
     else:
-        got = lib.sdpa_paged8(q, *dev, lens_gpu, wide.cuda(), causal=causal, scale=scale, return_lse=True, **more)
-    k, v = ref.gathered(host[0], host[2], lens, table, cap), ref.gathered(host[1], host[3], lens, table, cap)
-    o, lse, eo, el = ref.attention(q.cpu(), k, v, U[q.dtype], causal, scale)
-    assert torch.equal(got[0].isnan().cpu(), o.isnan())
-    off, fine = (got[0].cpu().double() - o).abs(), ~o.isnan()
+        o, lse = lib.sdpa_paged8(q, *dev, lens_gpu, wide.cuda(), causal=causal, scale=scale, return_lse=True, **more)
+    groups = [0, 1, Hkv - 1]
+    heads = [g * G + i for g in groups for i in range(G)]
+    some = [x[:, groups] for x in host]
+    k, v = ref.gathered(some[0], some[2], lens, table, cap), ref.gathered(some[1], some[3], lens, table, cap)
+    want, want_lse, eo, el = ref.attention(q[:, heads].cpu(), k, v, U[q.dtype], causal, scale)
+    got, got_lse = o[:, heads].cpu().double(), lse[:, heads].cpu().double()
+    assert torch.equal(got.isnan(), want.isnan())
+    off, fine = (got - want).abs(), ~want.isnan()
     assert not fine.any() or (off - eo)[fine].max() <= 0
-    number, fine = ~lse.isnan(), lse.isfinite()
-    assert torch.equal(torch.isneginf(got[1]).cpu()[number], torch.isneginf(lse)[number])
-    assert ((got[1].cpu().double() - lse).abs() <= el)[fine].all()
-    return got
+    number, fine = ~want_lse.isnan(), want_lse.isfinite()
+    assert torch.equal(torch.isneginf(got_lse)[number], torch.isneginf(want_lse)[number])
+    assert ((got_lse - want_lse).abs() <= el)[fine].all()
+    return o, lse
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D", [64, 96, 128, 160])
-@pytest.mark.parametrize("G,Sq,R", [(1, 125, 0), (3, 42, 64), (2, 1153, 128)])
+@pytest.mark.parametrize("Hkv,G,Sq,R", [(129, 1, 125, 0), (129, 3, 42, 64), (8, 2, 1153, 128)])
 @pytest.mark.parametrize("causal", [False, True])
-def test_large_tiles(dtype, D, G, Sq, R, causal):
-    B, Hkv, cap = 2, 2, 384
+def test_large_tiles(dtype, D, Hkv, G, Sq, R, causal):
+    B, cap = 2, 384
     lens = [371, 70]
     host, dev, table = filled(B, Hkv, cap, D, lens, R, seed=Sq + R, dtype=dtype)
     q = torch.randn(B, G * Hkv, Sq, D, generator=torch.Generator().manual_seed(Sq)).to(dtype).cuda()
-    check_large(q, host, dev, lens, table, cap, 1 << 20, causal)
-    check_large(q, host, dev, lens, table, cap, 1 << 20, causal, splits=1)
+    check_large(q, host, dev, lens, table, cap, causal)
+    check_large(q, host, dev, lens, table, cap, causal, splits=1)
 
 
-@pytest.mark.parametrize("splits", [2, 3, 128])
+@pytest.mark.parametrize("splits", [2, 3, 16])
 @pytest.mark.parametrize("R", [0, 64])
 @pytest.mark.parametrize("scale", [0.0, -0.3])
 def test_large_tiles_in_runs(splits, R, scale):
-    B, Hkv, cap, D = 3, 2, 512, 128
+    B, Hkv, cap, D = 3, 86, 512, 128
     lens = [512, 77, 0]
     host, dev, table = filled(B, Hkv, cap, D, lens, R, seed=splits, spread=0.5)
     q = torch.randn(B, 2 * Hkv, 64, D, generator=torch.Generator().manual_seed(splits)).to(torch.bfloat16).cuda()
-    a = check_large(q, host, dev, lens, table, cap, 1 << 20, True, scale, splits=splits)
-    b = check_large(q, host, dev, lens, table, cap, 1 << 20, True, scale, splits=splits)
+    a = check_large(q, host, dev, lens, table, cap, True, scale, splits=splits)
+    b = check_large(q, host, dev, lens, table, cap, True, scale, splits=splits)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
-@pytest.mark.parametrize("Sq", [64, 250])
+@pytest.mark.parametrize("Hkv,Sq", [(129, 64), (33, 250)])
 @pytest.mark.parametrize("R", [0, 64])
-def test_nan_in_large_tiles(Sq, R):
-    B, Hkv, cap, D = 2, 2, 256, 128
+def test_nan_in_large_tiles(Hkv, Sq, R):
+    B, cap, D = 2, 256, 128
     lens = [256, 150]
     host, dev, table = filled(B, Hkv, cap, D, lens, R, seed=2)
     for codes, row, col in ((1, 255, 3), (1, 252, 77), (0, 254, 5), (1, 149, 9), (0, 148, 127)):
@@ -413,8 +425,24 @@ def test_nan_in_large_tiles(Sq, R):
         host[codes][page, 1, r, col] = 0x7f if col & 1 else 0xff
     dev = on_gpu(host)
     q = torch.randn(B, 2 * Hkv, Sq, D, generator=torch.Generator().manual_seed(Sq)).to(torch.bfloat16).cuda()
-    check_large(q, host, dev, lens, table, cap, 1 << 20, True)
-    check_large(q, host, dev, lens, table, cap, 1 << 20, False)
+    check_large(q, host, dev, lens, table, cap, True)
+    check_large(q, host, dev, lens, table, cap, False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_tiles_of_a_full_cache(dtype):
+    """Without lengths, more than 2^27 scores: some rows against the definition."""
+    B, Hkv, G, Sq, cap, D = 1, 4, 4, 500, 17000, 64
+    host, dev, table = filled(B, Hkv, cap, D, [cap], 0, seed=8, dtype=dtype)
+    q = torch.randn(B, G * Hkv, Sq, D, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    assert B * Hkv * G * Sq * cap > 1 << 27
+    o, lse = lib.sdpa_kv8(q, *dev, causal=True, return_lse=True)
+    k, v = ref.gathered(host[0], host[2], [cap], None, cap), ref.gathered(host[1], host[3], [cap], None, cap)
+    for i in (0, 127, 128, 333, 499):                     # (the keys that row i sees are those of a step that ends there)
+        upto = lambda x: [(a[:, :cap - Sq + i + 1], c[:, :cap - Sq + i + 1]) for a, c in x]
+        want, want_lse, eo, el = ref.attention(q[:, :, i:i + 1].cpu(), upto(k), upto(v), U[dtype], False)
+        assert ((o[:, :, i:i + 1].cpu().double() - want).abs() <= eo).all()
+        assert ((lse[:, :, i:i + 1].cpu().double() - want_lse).abs() <= el).all()
 
 
 # Tiles of 32 rows: units (heads of all entries times runs) that divide over the XCDs in every way, more and fewer tiles than parts.
