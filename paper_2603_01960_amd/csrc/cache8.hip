@@ -320,37 +320,47 @@ Form form_of(int heads, int rows, int Skv, bool lengths)
     return (int64_t)rows * Skv <= ((int64_t)1 << (lengths ? 28 : 27)) / heads ? Form::rows : Form::chunk;       // (rows * Skv < 2^61)
 }
 
+// Splits of tiles of 32 rows: the least of a model of the time.  A workgroup alone on its CU takes 1.8 + 0.0215 D ns per key, two on one CU 1.6 times as long; splits
+// cost 2.5 us and, for their states, 0.08 ns per tile, run and column.  Of more than 64 tiles of entries with lengths of their own, as if these were half the capacity:
+// what splits cost is then more than they gain of a short one.
+// (us at 1 / 2 / 3 / 4 splits, the choice, BF16, D = 128, 8 heads: 16 tiles of 4096 keys 24.5 / 18.0 / 15.5 / 13.8, 13.2; 32 of 8192 43.1 / 28.0 / 21.9 / 19.5, 16.7; 64 of 1024 11.4 /
+// 12.2 / 12.8, 11.4, of 4096 24.8 / 18.9 / 17.1 / 16.4, 15.9, of 32768 148 / 84 / 62 / 52, 48; 96 of 4096 25.5 / 20.2 / 22.2 / 21.3, 22.1; 128 of 4096 25.0 / 20.9 / 23.7, 20.7; 144 of
+// 2048 16.3 / 18.8, 16.0, of 8192 42.4 / 39.2 / 34.3 / 40.3, 34.2; 192 of 8192 42.6 / 42.2 / 47.5 / 40.9, 40.9; 288 of 4096 31.2 / 38.2, 30.8, of 32768 221 / 218 / 185 / 189, 165;
+// 384 of 8192 63.0 / 71.1, 71.2.)
+int row_splits(int64_t tiles, int Skv, int D, bool lengths)
+{
+    const int keys = lengths && tiles > 64 ? Skv / 2 : Skv, most = keys / 256 < TSDPA_MAX_SPLITS ? keys / 256 : TSDPA_MAX_SPLITS;
+    const float alone = (1.8e-3f + 2.15e-5f * D) * keys;
+    int best = 1;
+    float least = std::numeric_limits<float>::max();
+    for (int n = 1; n <= (most > 1 ? most : 1) && (n == 1 || tiles * n <= 2048); ++n) {
+        const int64_t groups = tiles * n, rest = groups % 512;
+        const float time = alone / n * ((float)(groups / 512) * 1.6f + (rest == 0 ? 0.f : rest <= 256 ? 1.f : 1.6f)) + (n > 1 ? 2.5f + 8e-5f * D * (float)groups : 0.f);
+        if (time < least) least = time, best = n;
+    }
+    return best;
+}
+
 // Splits along the key axis.
 // Decoding: one workgroup per CU in all, of runs of at least 512 keys, or 256 while there are up to eight, which
 // the kernel combines itself.  None where a pass over a head's keys takes no longer than the second look at the states.
 // (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 4 rows per head: 8 heads of 1024 keys 7.8 / 8.7 / 8.0 / 8.1; of 2048
 // 11.5 / 10.5 / 8.9 / 8.1 / 9.6; of 8192 33.5 / 21.8 / 14.7 / 11.1 / 10.0, 32 splits 9.6; 64 heads of 1024 keys 7.9 / 8.9 / 8.6, of 4096 18.8 / 15.7
-// / 15.8 / 16.2; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6.)
+// / 15.8 / 16.2; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6; 32 rows per head: 8 heads of 1024 keys 10.1 / 13.0 / 12.6, of 2048 13.9 / 13.9 / 11.7, D = 64 7.3 / 9.7 / 9.4, 10.0 / 10.1
+// / 9.5.)
 // From half as many key/value heads as CUs on none either, with two exceptions where runs are long.  CUs get equal shares of the memory's rate, and one
 // reaches 2.4 times that at most (58 GB/s): so 128 heads do not reach it all, and of 257 ... 448 heads those that share a CU take twice as
 // long (1 / 2 / 3 splits, FP16: 128 heads of 2048 keys 13.3 / 16.4, of 4096 28.0 / 28.7, of 8192 54 / 51, in pages 60 / 54, of 16384 100 / 96, 113 / 99; 192 of 16384 133 / 145;
 // 256 of 8192 95 / 98 / 98; 264 of 16384 260 / 218 / 209, of 4096 ... 16384 134 / 138 / 144; 320 of 8192 136 / 124 / 122; 384 of 16384 301 / 273 / 281, of 4096 ... 16384 208 / 195
 // / 193; 512 of 16384 353 / 357 / 368).
-// Tiles of 32 rows: the same, of runs of at least 256 keys and none up to 1024; two workgroups per CU where the runs are longer than 8192 keys all the same.
-// (us at 1 / 2 / 4 / 8 / 16 splits, BF16, D = 128, 8 heads of 64 rows: 1024 keys 10.6 / 10.5 / - / 10.2 / 11.4, 2048 15.0 / 12.9 / - / 10.4 / 11.5, 4096 23.9 / 17.5 / - /
-// 11.5 / 11.8; of 256 rows: 1024 10.7 / 11.2 / 11.1, 2048 15.5 / 13.4 / 12.4 / 16.0, 8192 42.9 / - / 20.5 / 21.3 / 27.4, 65536 309 / - / 101 / 88 / 96.)
-int default_splits(Form form, int heads, int rows, int Skv, int D)
+int default_splits(Form form, int heads, int rows, int Skv, int D, bool lengths)
 {
     if (form == Form::chunk) return tsdpa::row_tile_splits(heads, rows, Skv, D);
-    int64_t want, most;
-    if (form == Form::rows) {
-        if (Skv <= 1024) return 1;
-        const int64_t tiles = (int64_t)heads * (((int64_t)rows + 31) / 32);
-        want = tiles > 128 ? 1 : 256 / tiles;
-        if (tiles <= 256 && Skv / want > 8192) want *= 2;
-        most = Skv / 256;
-    } else {
-        if (rows <= 16 && (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000)) return 1;
-        const int64_t tiles = (int64_t)heads * ((rows + 15) / 16), few = Skv / 256 < 8 ? Skv / 256 : 8;
-        want = tiles >= 128 ? 1 : 256 / tiles;
-        if ((int64_t)Skv * D >= 1 << 20) want = tiles > 256 && tiles <= 448 ? 3 : tiles >= 128 && tiles <= 160 ? 2 : want;
-        most = Skv / 512 > few ? Skv / 512 : few;
-    }
+    if (form == Form::rows) return row_splits((int64_t)heads * (((int64_t)rows + 31) / 32), Skv, D, lengths);
+    if (rows <= 16 ? (int64_t)Skv * D <= (heads > 64 ? 260000 : 210000) : Skv <= 1024) return 1;
+    const int64_t tiles = (int64_t)heads * ((rows + 15) / 16), few = Skv / 256 < 8 ? Skv / 256 : 8, most = Skv / 512 > few ? Skv / 512 : few;
+    int64_t want = tiles >= 128 ? 1 : 256 / tiles;
+    if ((int64_t)Skv * D >= 1 << 20) want = tiles > 256 && tiles <= 448 ? 3 : tiles >= 128 && tiles <= 160 ? 2 : want;
     if (want > most) want = most;
     if (want < 1) want = 1;
     return (int)(want > TSDPA_MAX_SPLITS ? TSDPA_MAX_SPLITS : want);
@@ -429,7 +439,7 @@ int tiled_sdpa_cache8_default_splits(int B, int H, int Hkv, int Sq, int Skv, int
     if ((int64_t)B * H * Sq == 0) return TSDPA_OK;
     const int heads = B * Hkv, rows = H / Hkv * Sq;
     for (const bool lengths : {false, true}) {    // (room for either)
-        const int n = default_splits(form_of(heads, rows, Skv, lengths), heads, rows, Skv, D);
+        const int n = default_splits(form_of(heads, rows, Skv, lengths), heads, rows, Skv, D, lengths);
         if (n > *splits) *splits = n;
     }
     return TSDPA_OK;
@@ -456,7 +466,7 @@ int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *
     const int rows = H / c->Hkv * Sq, heads = B * c->Hkv;
     const Form form = form_of(heads, rows, capacity, kv_lens != nullptr);
     if (splits == 0) {
-        splits = default_splits(form, heads, rows, capacity, c->D);
+        splits = default_splits(form, heads, rows, capacity, c->D, kv_lens != nullptr);
         // (with less memory than that takes: as many as fit)
         const unsigned long long each = tiled_sdpa_kv_workspace_bytes(B, H, Sq, c->D, 2) / 2, given = workspace ? workspace_bytes / each : 0;
         if ((unsigned long long)splits > given) splits = given > 1 ? (int)given : 1;
