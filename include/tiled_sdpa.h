@@ -567,6 +567,7 @@ int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out,
  *   splits, workspace : as for tiled_sdpa_fwd_kv; 0 = at most tiled_sdpa_cache8_default_splits of the capacity, and no more than the workspace
  *                  has room for.  tiled_sdpa_kv_workspace_bytes(B, H, Sq, D, n) bytes hold n.  B * H * ceil(Sq / 16), times splits, is at
  *                  most 2^23 - 16.
+ *   o, lse and the workspace must overlap neither each other nor what the call reads.
  *
  * Scores and sums are FP32.  K is multiplied as 16-bit numbers of q's type, which its codes are; the weights are rounded to FP16 for the
  * product with V, each times its scale, against the greatest such product of the row, so that what contributes most keeps 11 bits.

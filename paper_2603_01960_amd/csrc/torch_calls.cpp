@@ -1106,6 +1106,13 @@ PyObject *call_sdpa_cache8(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
         const Workspace ws(args[12], tiled_sdpa_kv_workspace_bytes(B, H, Sq, cache.c.D, splits), q);
         if (heuristic) splits = 0;                // (the library decides, within the workspace)
+        if (args[11] != Py_None || args[12] != Py_None) {
+            const int64_t entries = cache.c.max_blocks;
+            distinct({Extent(out), Extent(ws.ptr, (int64_t)ws.bytes)},
+                     {Extent(q), Extent(cache.codes[0]), Extent(cache.codes[1]), Extent(cache.scales[0]), Extent(cache.scales[1]), Extent(lens, lens ? s[0] : 0),
+                      Extent(entries ? cache.c.block_table : nullptr, s[0] * entries)},
+                     "out and workspace must overlap neither each other nor what the call reads");
+        }
         const Launch on(q);
         const int st = without_gil(tiled_sdpa_fwd_cache8, (const tsdpa_cache8 *)&cache.c, (const void *)data(q), data(out), with_lse ? (float *)data(lse) : nullptr,
                                    lens, B, H, Sq, scale, dtype, flags, splits, ws.ptr, ws.bytes, on.stream);

@@ -188,3 +188,20 @@ def test_tensor_arguments_are_checked():
     assert lib.cache8_read(k, v, ks, vs, slots[:, :0], torch.float16)[0].shape == (2, 2, 0, 64)
     lib.cache8_write(x[:, :0], x[:, :0], k, v, ks, vs, n, n)
     same_bytes((k, v, ks, vs), host)
+
+
+def test_results_in_what_the_call_reads_are_refused():
+    k, v, ks, vs = on_gpu(new_cache(2, 2, 2048, 64))
+    q = torch.zeros(2, 4, 1, 64, dtype=torch.float16, device="cuda")
+    n, table, p8 = i32([2000, 3]), i32([[0], [1]]), tuple(on_gpu(new_cache(2, 2, 2048, 64)))
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    inside = ws[:q.numel() * 2].view(torch.float16).view(q.shape)
+    of_k = k.view(torch.uint8).view(-1)[:q.numel() * 2].view(torch.float16).view(q.shape)
+    for call in (lambda: lib.sdpa_kv8(q, k, v, ks, vs, kv_lens=n, out=q), lambda: lib.sdpa_kv8(q, k, v, ks, vs, out=of_k), lambda: lib.sdpa_kv8(q, k, v, ks, vs, workspace=v.view(torch.uint8)),
+                 lambda: lib.sdpa_kv8(q, k, v, ks, vs, out=inside, workspace=ws), lambda: lib.sdpa_kv8(q, k, v, ks, vs, workspace=ks),
+                 lambda: lib.sdpa_paged8(q, *p8, n, table, workspace=table.view(torch.uint8)), lambda: lib.sdpa_paged8(q, *p8, n, table, workspace=n.view(torch.uint8))):
+        with pytest.raises(ValueError, match="overlap"):
+            call()
+    want = lib.sdpa_kv8(q + 1, k, v, ks, vs, kv_lens=n)
+    out = torch.empty_like(q)
+    assert lib.sdpa_kv8(q + 1, k, v, ks, vs, kv_lens=n, out=out, workspace=ws) is out and torch.equal(out.view(torch.int16), want.view(torch.int16))
