@@ -152,7 +152,7 @@ struct RowsOrder {
 
 template <typename T, int D, bool PAGED>
 __global__ void __launch_bounds__(256, 2)
-sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__restrict__ lse, Cache8Args cache, int S, int heads, int units, RowsOrder order, float c,
+sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__restrict__ lse, Cache8Args cache, int S, int units, RowsOrder order, float c,
                         uint32_t qsign, int causal, int Skv_cap, int splits, float *__restrict__ ws, int rows_per_head, const int *__restrict__ kv_lens)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -493,7 +493,7 @@ template <typename T, int D, bool PAGED> int launch_cache8_rows_one(const Cache8
     const int ranked = a.kv_lens && a.splits == 1 && groups > 512 && a.batches > 1 && a.batches <= kRanked ? a.batches : 0;
     const RowsOrder order{row_tiles, tiles, log2_parts, ranked, divisor((uint32_t)tiles), divisor((uint32_t)a.splits), divisor((uint32_t)a.heads_per_batch),
                           divisor((uint32_t)a.rows_per_head)};
-    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c, a.S, a.BH, units, order, a.c, a.qsign, a.causal,
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), lds_bytes, a.stream, (const T *)a.q, (T *)a.o, a.lse, x.c, a.S, units, order, a.c, a.qsign, a.causal,
                        a.Skv, a.splits, a.ws, a.rows_per_head, a.kv_lens);
     return (int)hipGetLastError();
 }
