@@ -171,6 +171,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     float m_ref = klim >= t0 * TN ? kNoWeight : -INFINITY, l_run = 0.f;
     constexpr float kLazyLimit = 256.f;
+    int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
 
     // ---- per-lane LDS read pointers (sdpa_fwd_kernel.h's; in compact rows the swizzle of K touches the low two bits of a chunk's index only and V has
     // none, so that two pointers and one serve all columns)
@@ -216,7 +217,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     auto softmax = [&](int row0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
         Sums ps = exponentials(row0, x8, mask_tag);
         const bool over = !(ps.p <= kLazyLimit);                 // also inf (first score) and NaN
-        if (__builtin_amdgcn_ballot_w64(over) != 0) {
+        if (__builtin_amdgcn_ballot_w64(over || x8.far_lane) != 0) {
             // Eq. 2 for the rows that are over the limit (the two lanes of a row together): the tile's maximum, new reference, the rescale of Eqs. 3-4
             const int key0 = row0 + g * 4;
             float m_tile = -INFINITY;
@@ -230,14 +231,28 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
             }
             m_tile = pair_max(m_tile);
             const bool grow = pair_max(over ? 1.f : 0.f) > 0.f && m_tile > m_ref;
-            const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref - m_tile) : 1.f;
+            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;
-            l_run *= alpha;
+            l_run = l_run * half * half;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
+            float l = 0.f;
+            const bool far = x8.far();
+            if (__builtin_expect(far, 0)) {
+                float m_l = m_ref;
+                asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 32 registers)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[nb][i], x8.ck[nb], x8.ev[nb] - m_l) - x8.ev[nb]);
+                        if (!decltype(mask_tag)::value || !hidden(key0, nb, i)) l += e;
+                    }
+            }
             ps = exponentials(row0, x8, mask_tag);
+            if (far) ps.l = l;
         }
         l_run += ps.l;
     };
@@ -328,7 +343,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
             }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
-            const TileScales x8(scale_now, c);
+            const TileScales x8(scale_now, c, top);
             softmax(j * TN, x8, mask_tag);
             if constexpr (MASK) {
                 if (causal && has_nan(VS)) take_nan(j * TN + g * 4, VS);
@@ -369,6 +384,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     // ---- O_i = o_i / l_i, turned through the LDS to whole rows (sdpa_fwd_kernel.h), or the state of a run of keys
     const float l_tot = pair_sum(l_run);
     if (splits > 1) {
+        const float f = raise_reference(m_ref, l_tot);
         const size_t prow = (size_t)(head * splits + sp) * S + qrow;
         if (qrow < S) {
             float *po = ws + prow * D;
@@ -378,13 +394,13 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
                 for (int q4 = 0; q4 < 4; ++q4) {
                     f32x4 part;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) part[e] = oacc[db][q4 * 4 + e];
+                    for (int e = 0; e < 4; ++e) part[e] = oacc[db][q4 * 4 + e] * f;
                     *(f32x4 *)(po + db * 32 + q4 * 8 + g * 4) = part;
                 }
             if (g == 0) {
                 float *pml = ws + (size_t)(N / nQ) * S * D + prow * 2;
                 pml[0] = m_ref;
-                pml[1] = l_tot;
+                pml[1] = l_tot * f;
             }
         }
         return;

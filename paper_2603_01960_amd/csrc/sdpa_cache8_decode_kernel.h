@@ -5,7 +5,7 @@
 // and O = o / l: the scales cost nothing per value.  EK folds into the factor of the score, EV into the exponent, so that m is the greatest
 // score PLUS exponent seen: the weights that enter the products are sized by what they contribute, and the products, whose weights and
 // values are both FP16 here whatever the type of q (every code is an FP16 number), keep 11 bits of the largest contributions.  l takes
-// the exponent out again, in FP32.
+// the exponent out again, in FP32, and where exponents lie so far apart that p_j may be none of its normal numbers, before the exponential is taken (kFar).
 //
 // Such a call is bound by reading the cache once.  As in sdpa_decode_kernel.h each wavefront streams tiles of its own through LDS slots
 // of its own, with no barrier in the loop: one slot for K and one for V, each refilled as soon as it has been read into registers.  A
@@ -305,6 +305,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr float kLazyLimit = 256.f;
+    int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
 
     // ---- pointers of the reads
     uint32_t kptr[G::NKP], vptr[G::NVP];
@@ -341,7 +342,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     auto softmax = [&](f32x4 (&s)[4], int key0, const TileScales &x8, bool first_tile, auto mask_tag) __attribute__((always_inline)) {
         Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
         if (!first_tile) ps = exponentials(s, key0, x8, mask_tag);
-        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit)) != 0) {            // also inf and NaN
+        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit) || x8.far_lane) != 0) {             // also inf and NaN
             // Eq. 2 for all rows of the wavefront: the tile's maximum, new reference and the rescale of Eqs. 3-4
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
@@ -349,14 +350,26 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
                 if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
             const float m_tile = quad_max(fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1]));
             const bool grow = m_tile > m_ref;     // (a row without finite scores so far: -inf or NaN, left alone)
-            const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref - m_tile) : 1.f;
+            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;
-            l_run *= alpha;
+            l_run = l_run * half * half;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) oacc[db][e] *= alpha;
+            float l = 0.f;
+            const bool far = x8.far();
+            if (__builtin_expect(far, 0)) {
+                float m_l = m_ref;
+                asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 32 registers)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 2][x & 3], x8.ck[x >> 3], x8.ev[x >> 3] - m_l) - x8.ev[x >> 3]);
+                    if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim) l += e;
+                }
+            }
             ps = exponentials(s, key0, x8, mask_tag);
+            if (far) ps.l = l;
         }
         l_run += ps.l;
     };
@@ -373,9 +386,10 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         u32x2 kt[4];
         TSDPA_WAIT_VMCNT(NU);
         Read8<D>::keys(kf, kt, kptr);
-        const int scale_now = scale_next;
         load_k(s);
-        const TileScales scale(scale_now, c);
+        int scale_now = scale_next;
+        asm volatile("" : "+v"(scale_now));       // (not looked at before: a wait for it there would be one for V)
+        const TileScales scale(scale_now, c, top);
         f32x4 sacc[4];
 #pragma unroll
         for (int blk = 0; blk < 4; ++blk) sacc[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -461,8 +475,8 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float weight = ml[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][0] - M);      // (2^(m - M); -inf: no key)
-            L += weight * ml[w][1];
+            const float half = ml[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[w][0] - M) * 0.5f), weight = half * half;      // (2^(m - M); -inf: no key)
+            L += ml[w][1] * half * half;
             const f32x4 part = *(TSDPA_LDS f32x4 *)(lds + w * (TM * D * 4) + x * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[e] += weight * part[e];
@@ -470,9 +484,10 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         const bool of_row = x - r * (D / 4) == 0;
         if (splits > 1) {
             float *part = ws + ((size_t)(head * splits + sp) * S + r0) * D + (size_t)x * 4;
-            put_pair(part, sum[0], sum[1]);
-            put_pair(part + 2, sum[2], sum[3]);
-            if (of_row) put_pair(ws + states + ((size_t)(head * splits + sp) * S + r0 + r) * 2, M, L);
+            const float f = raise_reference(M, L);
+            put_pair(part, sum[0] * f, sum[1] * f);
+            put_pair(part + 2, sum[2] * f, sum[3] * f);
+            if (of_row) put_pair(ws + states + ((size_t)(head * splits + sp) * S + r0 + r) * 2, M, L * f);
         } else {
             const float inv = M == -INFINITY ? 0.f : 1.f / L;     // (no key at all: O = 0, LSE = -inf)
             vec4 out;

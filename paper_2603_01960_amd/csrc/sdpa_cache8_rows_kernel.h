@@ -277,6 +277,7 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     float m_ref = kNoWeight, l_run = 0.f;
     constexpr float kLazyLimit = 256.f;
+    int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
     uint32_t kptr[G::NKP], vptr[DB];
 #pragma unroll
     for (int i = 0; i < G::NKP; ++i) kptr[i] = __builtin_bit_cast(uint32_t, kslot) + l32 * G::ROW + (G::k_at(2 * i + g, l32) << 4);
@@ -306,11 +307,12 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
         }
         return Sums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1]};
     };
-    auto softmax = [&](const TileScales &x8, bool first_tile) __attribute__((always_inline)) {
+    // (of a masked tile the scores have EV already, and x8 has none: `ev` is what it was)
+    auto softmax = [&](const TileScales &x8, const float (&ev)[NB], bool first_tile) __attribute__((always_inline)) {
         Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
         if (!first_tile) ps = exponentials(x8);
         const bool over = !(ps.p <= kLazyLimit);  // also inf and NaN
-        if (__builtin_amdgcn_ballot_w64(over) != 0) {
+        if (__builtin_amdgcn_ballot_w64(over || x8.far_lane) != 0) {
             float m_tile = -INFINITY;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -321,14 +323,25 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
             }
             m_tile = pair_max(m_tile);
             const bool grow = pair_max(over ? 1.f : 0.f) > 0.f && m_tile > m_ref;
-            const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref - m_tile) : 1.f;
+            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;
-            l_run *= alpha;
+            l_run = l_run * half * half;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
+            float l = 0.f;
+            const bool far = x8.far();
+            if (__builtin_expect(far, 0)) {
+                float m_l = m_ref;
+                asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 32 registers)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) l += __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[nb][i], x8.ck[nb], x8.ev[nb] - m_l) - ev[nb]);
+            }
             ps = exponentials(x8);
+            if (far) ps.l = l;
         }
         l_run += ps.l;
     };
@@ -357,9 +370,10 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
                     sacc[nb] = Elem<T>::mfma(Codes<T>::wide(kf[nb][kk >> 1][(kk & 1) * 2], kf[nb][kk >> 1][(kk & 1) * 2 + 1]), qf[kk], sacc[nb]);
         }
         __builtin_amdgcn_s_setprio(0);
-        TileScales x8(scale_next, c);
+        TileScales x8(scale_next, c, top);
         const bool masked = tile * TN + TN - 1 > klim_least;
         const int last = klim - (tile * TN + g * 4);          // the last of the tile's keys that this lane's row sees, from the lane's first
+        const float ev[NB] = {x8.ev[0], x8.ev[1]};
         if (masked) {
             // scores as they enter the softmax, -inf for hidden keys (a factor of 0 would make them NaN)
 #pragma unroll
@@ -370,7 +384,7 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
                 x8.ev[nb] = 0.f;
             }
         }
-        softmax(x8, i == 0);
+        softmax(x8, ev, i == 0);
         u32x2 vf[DB][4];
         TSDPA_WAIT_VMCNT(NU);
         ReadRows<D>::values(vf, vptr);
@@ -453,15 +467,18 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float weight = ml[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][0] - M);      // (-inf: no key)
-                L += weight * ml[w][1];
+                const float half = ml[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[w][0] - M) * 0.5f), weight = half * half;      // (-inf: no key)
+                L += ml[w][1] * half * half;
                 const f32x4 part = *(TSDPA_LDS f32x4 *)(lds + w * PART + ((c4 >> 1) * 64 + (((c4 & 1) * 32 + r) ^ (c4 & 15))) * 16);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e] += weight * part[e];
             }
             if (splits > 1) {
+                const float f = raise_reference(M, L);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] *= f;
                 *(f32x4 *)(ws + (first_state + r) * D + col) = sum;
-                if (col == 0) *(f32x2 *)(ws + (size_t)units * S * D + (first_state + r) * 2) = f32x2{M, L};
+                if (col == 0) *(f32x2 *)(ws + (size_t)units * S * D + (first_state + r) * 2) = f32x2{M, L * f};
             } else {
                 const float inv = M == -INFINITY ? 0.f : 1.f / L;     // (no key at all: O = 0, LSE = -inf)
                 vec4 out;

@@ -67,12 +67,25 @@ template <bool PAGED> __device__ __forceinline__ int tile_scale_bytes(const Cach
     return (int)scales[((size_t)page * cache.heads + h) * (size_t)cache.blocks + block];
 }
 
-// Of a tile's two blocks: c * 2^EK, EV, 2^-EV.
+// A key counts in l by 2^(score - m), and its weight is 2^(score + EV - m), m being the greatest score plus EV: of two keys that count alike one may have EV = 62, the other
+// -62, and keys of 2^-24 of another, or many of less, still count.  So l is the sum of the weights times 2^-EV only as long as these are in FP32's normal range, below which
+// the exponential gives 0: weights that count are 2^-(kFar + 24) of the greatest or more where EV is at most kFar below the greatest that the wavefront
+// has met.  In tiles with a block that is further below, l is the sum of exponentials of its own, from which EV is taken before: 2^(-62 - 24) of the
+// greatest weight at least, and 2^70 at most.  (2^-126 leaves 32 and 40 powers of two to keys that count only because they are many.)
+constexpr int kFar = 70;
+
+// Of a tile's two blocks: c * 2^EK, EV, 2^-EV; and in the lanes that have V's exponents whether one is far below the greatest so far (`top`, of bytes).
 struct TileScales {
     float ck[2], ev[2], ew[2];
-    __device__ __forceinline__ TileScales(int x, float c)
+    bool far_lane;
+    __device__ __forceinline__ bool far() const { return __builtin_amdgcn_ballot_w64(far_lane) != 0; }
+    __device__ __forceinline__ TileScales(int x, float c, int &top)
     {
         x = x < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x < kScaleBias + kScaleMost ? x : kScaleBias + kScaleMost);
+        const int other = __builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, false);       // quad_perm: the other block's
+        top = x > top ? x : top;
+        top = other > top ? other : top;
+        far_lane = x + ((threadIdx.x & 2) ? kFar : 1 << 16) < top;
         const float power = __builtin_bit_cast(float, x << 23) * c, e = (float)(x - kScaleBias), inverse = __builtin_bit_cast(float, (2 * kScaleBias - x) << 23);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -82,6 +95,17 @@ struct TileScales {
         }
     }
 };
+
+// The state (m, l, o) of a run of keys, for whoever combines runs by 2^(m - greatest m): l may be 2^62 times as large as the greatest weight, and count where that factor
+// is 0.  So the reference is raised by what l has over 1, 2^62 at most, and o and l are multiplied by the result.  (A reference so large that it cannot be
+// raised by so little stays as it is, and so do they.)
+__device__ __forceinline__ float raise_reference(float &m, float l)
+{
+    const int e = (int)(__builtin_bit_cast(uint32_t, l) >> 23) - 127;
+    const float old = m;
+    m += (float)(e < 0 ? 0 : (e < kScaleMost ? e : kScaleMost));
+    return old == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(old - m);
+}
 
 // Values that are NaN, in keys that only some rows see (the causal mask): the product with a weight of 0 would be NaN for the others.
 // Eight codes: 1 (FP16) where one is NaN, and the codes without those.
