@@ -204,7 +204,8 @@ int tiled_sdpa_fwd_gqa(const void *q, const void *k, const void *v, void *o, flo
  * positions of the kv_lens[b]-long sequence (key j contributes to query row i only if
  * j <= i + kv_lens[b] - Sq).  A query row that no key reaches -- an empty entry, or under the causal
  * flag an entry shorter than Sq for its first Sq - kv_lens[b] rows -- gets O = 0 and LSE = -infinity
- * (a softmax over no keys has no value; zero is what leaves a residual stream untouched).  Shapes are
+ * (a softmax over no keys has no value; zero is what leaves a residual stream untouched).  A row with a score that is
+ * NaN has O = LSE = NaN, whatever the number of splits.  Shapes are
  * validated against the capacity; the split heuristic sees the capacity too, so workspace sizes do not
  * depend on the lengths.  Everything else as for tiled_sdpa_fwd_gqa.
  */
@@ -571,7 +572,7 @@ int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out,
  *
  * Scores and sums are FP32.  K is multiplied as 16-bit numbers of q's type, which its codes are; the weights are rounded to FP16 for the
  * product with V, each times its scale, against the greatest such product of the row, so that what contributes most keeps 11 bits.
- * A row that no key reaches gets O = 0 and LSE = -infinity.  Keys that a row does not see do not reach it, NaN among their values included.
+ * A row that no key reaches gets O = 0 and LSE = -infinity, one with a score that is NaN O = LSE = NaN, whatever the number of splits.  Keys that a row does not see do not reach it, NaN among their values included.
  * Page numbers that are none count as the nearest one that is.
  */
 int tiled_sdpa_fwd_cache8(const tsdpa_cache8 *c, const void *q, void *o, float *lse, const int *kv_lens, int B, int H, int Sq, float scale,

@@ -510,7 +510,7 @@ sdpa_decode_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__
             if (splits > 1) {
                 put_pair(ws + (size_t)heads * splits * S * D + ((size_t)(head * splits + sp) * S + row) * 2, M[nq], L[nq]);
             } else if (lse != nullptr) {
-                lse[(size_t)head * S + row] = L[nq] > 0.f ? (M[nq] + __builtin_amdgcn_logf(L[nq])) * 0.69314718055994530942f : -INFINITY;
+                lse[(size_t)head * S + row] = L[nq] != 0.f ? (M[nq] + __builtin_amdgcn_logf(L[nq])) * 0.69314718055994530942f : -INFINITY;
             }
         }
     for (int x = tid; x < S * (D / 4); x += NW * 64) {

@@ -1129,7 +1129,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
         }
         const float inv = m_ref == -INFINITY ? 0.f : 1.0f / l_tot;
         if (lse != nullptr && g == 0 && stream == 0 && qrow < S)
-            lse[(size_t)head * S + qrow] = l_tot > 0.f ? (m_ref + __builtin_amdgcn_logf(l_tot)) * 0.69314718055994530942f : -INFINITY;
+            lse[(size_t)head * S + qrow] = l_tot != 0.f ? (m_ref + __builtin_amdgcn_logf(l_tot)) * 0.69314718055994530942f : -INFINITY;
         // rows to the LDS and from there to memory, as below
         __syncthreads();
         constexpr int OCPR = G::OROW / 16, CMASK = OCPR - 1, ORPI = 64 / OCPR;
@@ -1236,7 +1236,7 @@ sdpa_fwd_kernel(const T *__restrict__ q, const T *__restrict__ k, const T *__res
     // (only the cache variants can have such a row: in the square problem every row sees key 0)
     const float inv = KV && m_ref == -INFINITY ? 0.f : 1.0f / l_tot;
     if (lse != nullptr && g == 0 && qrow < S)
-        lse[(size_t)head * S + qrow] = KV && !(l_tot > 0.f) ? -INFINITY : (m_ref + __builtin_amdgcn_logf(l_tot)) * 0.69314718055994530942f;
+        lse[(size_t)head * S + qrow] = KV && l_tot == 0.f ? -INFINITY : (m_ref + __builtin_amdgcn_logf(l_tot)) * 0.69314718055994530942f;
     // (the launcher sizes the dynamic LDS for the larger of the tile slots and this staging area)
     {
         constexpr int OCPR = G::OROW / 16, CMASK = OCPR - 1;   // chunks per staging row: a power of two

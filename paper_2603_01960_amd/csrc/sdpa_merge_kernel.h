@@ -101,7 +101,7 @@ sdpa_merge_kernel(const float *__restrict__ ws, T *__restrict__ o, float *__rest
     for (int e = 0; e < 4; ++e) out[e] = (T)(acc[e] * inv);
     *(vec4 *)(o + (size_t)r * D + d4 * 4) = out;
     if (lse != nullptr && d4 == 0)
-        lse[r] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+        lse[r] = L != 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
 #endif
 }
 
@@ -182,7 +182,7 @@ sdpa_merge_wide_kernel(const float *__restrict__ ws, T *__restrict__ o, float *_
     for (int e = 0; e < 4; ++e) out[e] = (T)(out_acc[e] * inv);
     *(vec4 *)(o + (size_t)r * D + d4 * 4) = out;
     if (lse != nullptr && d4 == 0)
-        lse[r] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+        lse[r] = L != 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
 #endif
 }
 

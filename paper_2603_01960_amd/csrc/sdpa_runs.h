@@ -79,7 +79,7 @@ __device__ __forceinline__ void finish_runs(T *o, float *lse, const float *ws, l
         if (lane == 0) {
             wgt[splits * S + row] = M == -INFINITY ? 0.f : 1.f / L;      // (a row that no key reaches: O = 0, LSE = -inf)
             if (lse != nullptr)
-                lse[(size_t)head * S + row] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+                lse[(size_t)head * S + row] = L != 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
         }
     }
     __syncthreads();
