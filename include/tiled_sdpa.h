@@ -570,8 +570,10 @@ int tiled_sdpa_cache8_read(const tsdpa_cache8 *c, const int *slots, void *k_out,
  *                  most 2^23 - 16.
  *   o, lse and the workspace must overlap neither each other nor what the call reads.
  *
- * Scores and sums are FP32.  K is multiplied as 16-bit numbers of q's type, which its codes are; the weights are rounded to FP16 for the
- * product with V, each times its scale, against the greatest such product of the row, so that what contributes most keeps 11 bits.
+ * Scores and sums are FP32.  K is multiplied as 16-bit numbers of q's type, which its codes are; the weights, each times its scale of V, are rounded to
+ * FP16 for the product with V: to 11 bits down to 2^-21 of the greatest such product of the row, to multiples of 2^-31 of it (at most) below.  That is by scale, not by
+ * value: where a row weighs blocks alike, those with a scale of 2^22 or more below the greatest lose bits, from 2^32 on all, even in columns in which the greatest's block
+ * has zeros.  (The normaliser, and so LSE, has all weights in FP32.)
  * A row that no key reaches gets O = 0 and LSE = -infinity, one with a score that is NaN O = LSE = NaN, whatever the number of splits.  Keys that a row does not see do not reach it, NaN among their values included.
  * Page numbers that are none count as the nearest one that is.
  */

@@ -170,7 +170,6 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     float m_ref = klim >= t0 * TN ? kNoWeight : -INFINITY, l_run = 0.f;
-    constexpr float kLazyLimit = 256.f;
     int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
 
     // ---- per-lane LDS read pointers (sdpa_fwd_kernel.h's; in compact rows the swizzle of K touches the low two bits of a chunk's index only and V has
@@ -216,7 +215,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     };
     auto softmax = [&](int row0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
         Sums ps = exponentials(row0, x8, mask_tag);
-        const bool over = !(ps.p <= kLazyLimit);                 // also inf (first score) and NaN
+        const bool over = !(ps.p <= kLazyLimit8);                 // also inf (first score) and NaN
         if (__builtin_amdgcn_ballot_w64(over || x8.far_lane) != 0) {
             // Eq. 2 for the rows that are over the limit (the two lanes of a row together): the tile's maximum, new reference, the rescale of Eqs. 3-4
             const int key0 = row0 + g * 4;
@@ -229,7 +228,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
                     if (!decltype(mask_tag)::value || !hidden(key0, nb, i)) mx = fmaxf(mx, sacc[nb][i]);
                 m_tile = fmaxf(m_tile, mx * x8.ck[nb] + x8.ev[nb]);
             }
-            m_tile = pair_max(m_tile);
+            m_tile = pair_max(m_tile) - kRoom;
             const bool grow = pair_max(over ? 1.f : 0.f) > 0.f && m_tile > m_ref;
             const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;

@@ -2,8 +2,8 @@
 //
 // The values of a cache are code * 2^E, E4M3 codes, one E for each head and 32 rows of K, one of V.  With c = scale * log2(e)
 //     s_j = <q, codes of key j>,   p_j = 2^(s_j * (c * 2^EK) + EV - m),   o = sum_j p_j * codes of value j,   l = sum_j p_j * 2^-EV,
-// and O = o / l: the scales cost nothing per value.  EK folds into the factor of the score, EV into the exponent, so that m is the greatest
-// score PLUS exponent seen: the weights that enter the products are sized by what they contribute, and the products, whose weights and
+// and O = o / l: the scales cost nothing per value.  EK folds into the factor of the score, EV into the exponent, so that m goes by the greatest
+// score PLUS exponent seen (kRoom in sdpa_cache8_values.h): the weights that enter the products are sized by what they contribute, and the products, whose weights and
 // values are both FP16 here whatever the type of q (every code is an FP16 number), keep 11 bits of the largest contributions.  l takes
 // the exponent out again, in FP32, and where exponents lie so far apart that p_j may be none of its normal numbers, before the exponential is taken (kFar).
 //
@@ -304,7 +304,6 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     float m_ref = klim >= t0 * kTile8 ? kNoWeight : -INFINITY, l_run = 0.f;      // the lazy reference of sdpa_fwd_kernel.h, this lane's share of the normaliser
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr float kLazyLimit = 256.f;
     int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
 
     // ---- pointers of the reads
@@ -342,13 +341,13 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     auto softmax = [&](f32x4 (&s)[4], int key0, const TileScales &x8, bool first_tile, auto mask_tag) __attribute__((always_inline)) {
         Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
         if (!first_tile) ps = exponentials(s, key0, x8, mask_tag);
-        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit) || x8.far_lane) != 0) {             // also inf and NaN
+        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit8) || x8.far_lane) != 0) {             // also inf and NaN
             // Eq. 2 for all rows of the wavefront: the tile's maximum, new reference and the rescale of Eqs. 3-4
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int x = 0; x < 16; ++x)
                 if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
-            const float m_tile = quad_max(fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1]));
+            const float m_tile = quad_max(fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1])) - kRoom;
             const bool grow = m_tile > m_ref;     // (a row without finite scores so far: -inf or NaN, left alone)
             const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;

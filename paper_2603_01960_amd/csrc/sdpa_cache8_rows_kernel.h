@@ -276,7 +276,6 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     float m_ref = kNoWeight, l_run = 0.f;
-    constexpr float kLazyLimit = 256.f;
     int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
     uint32_t kptr[G::NKP], vptr[DB];
 #pragma unroll
@@ -311,7 +310,7 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
     auto softmax = [&](const TileScales &x8, const float (&ev)[NB], bool first_tile) __attribute__((always_inline)) {
         Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
         if (!first_tile) ps = exponentials(x8);
-        const bool over = !(ps.p <= kLazyLimit);  // also inf and NaN
+        const bool over = !(ps.p <= kLazyLimit8);  // also inf and NaN
         if (__builtin_amdgcn_ballot_w64(over || x8.far_lane) != 0) {
             float m_tile = -INFINITY;
 #pragma unroll
@@ -321,7 +320,7 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[nb][i]);
                 m_tile = fmaxf(m_tile, mx * x8.ck[nb] + x8.ev[nb]);
             }
-            m_tile = pair_max(m_tile);
+            m_tile = pair_max(m_tile) - kRoom;
             const bool grow = pair_max(over ? 1.f : 0.f) > 0.f && m_tile > m_ref;
             const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;

@@ -67,11 +67,17 @@ template <bool PAGED> __device__ __forceinline__ int tile_scale_bytes(const Cach
     return (int)scales[((size_t)page * cache.heads + h) * (size_t)cache.blocks + block];
 }
 
-// A key counts in l by 2^(score - m), and its weight is 2^(score + EV - m), m being the greatest score plus EV: of two keys that count alike one may have EV = 62, the other
+// The weights that enter the product with V are FP16, which ends at 2^16 and has a least step of 2^-24.  So the reference m is kRoom below the greatest score plus EV
+// when it is set, and stays while a lane's sum of a tile is at most 2^15: the greatest weight of a row is 2^7 or more, and what a small one loses is 2^-25, or 2^-32 of the
+// greatest.  (Without that room many weights of 2^-26 would be lost from o together, though not from l: 4096 beside one key, 6e-5 of O, and all that a column has in which that
+// key's value is 0.)
+constexpr float kRoom = 7.f, kLazyLimit8 = 0x1p15f;
+
+// A key counts in l by 2^(score - m), and its weight is 2^(score + EV - m), m + kRoom being the greatest score plus EV: of two keys that count alike one may have EV = 62, the other
 // -62, and keys of 2^-24 of another, or many of less, still count.  So l is the sum of the weights times 2^-EV only as long as these are in FP32's normal range, below which
 // the exponential gives 0: weights that count are 2^-(kFar + 24) of the greatest or more where EV is at most kFar below the greatest that the wavefront
 // has met.  In tiles with a block that is further below, l is the sum of exponentials of its own, from which EV is taken before: 2^(-62 - 24) of the
-// greatest weight at least, and 2^70 at most.  (2^-126 leaves 32 and 40 powers of two to keys that count only because they are many.)
+// greatest weight at least, and 2^77 at most.  (2^-126 leaves 32 and 40 powers of two to keys that count only because they are many.)
 constexpr int kFar = 70;
 
 // Of a tile's two blocks: c * 2^EK, EV, 2^-EV; and in the lanes that have V's exponents whether one is far below the greatest so far (`top`, of bytes).
