@@ -510,8 +510,9 @@ unsigned long long tiled_sdpa_qk_norm_rope_bwd_workspace_bytes(int B, int S, int
  * infinity); 32 consecutive rows (0 ... 31, 32 ... 63, ... of an entry) of a head of K share one E, and of V another, kept as the byte
  * E + 127, -62 <= E <= 62 (other bytes count as the nearest of these).  A power of two, because the codes are floating point themselves: a
  * finer scale would gain the top of their range at most, and products with this one are exact.  What is stored is within 2^-4 of a value,
- * or within 2^-10 * 2^E if it is smaller than that, and E is the least with which the largest magnitude of the 32 rows (so far) is at
- * most 448 * 2^E: the values of a head's 32 rows keep their four significant bits down to 2^-14 of the largest one's magnitude or less.
+ * or, where that is less, within 2^-10 * 2^E (2^-9 * 2^E in rows that were there when the scale grew), and E is the least with which the largest
+ * magnitude of the 32 rows (so far) is at most 448 * 2^E: the values of a head's 32 rows keep their four significant bits down to 2^-13 of the largest
+ * one's magnitude.
  */
 typedef struct {
     void *k, *v;                 /* device, codes [pages, Hkv, block_rows, D], 16-byte aligned */
