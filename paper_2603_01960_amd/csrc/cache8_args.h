@@ -9,7 +9,7 @@ namespace tsdpa {
 
 constexpr int kScaleRows = 32;                    // rows of a head that share a scale
 // Exponents of scales.  A key that matters, 2^0 ... 2^-24 of the row's greatest, times 2^E or 2^-E stays far from the ends of FP32; times 2^(difference of two exponents,
-// 124 at most) it may lie below its normal numbers, which the attention kernels look out for (kFar and raise_reference in sdpa_cache8_values.h).
+// 124 at most) it may lie below its normal numbers, which the attention kernels look out for (kSmall and raise_reference in sdpa_cache8_values.h).
 constexpr int kScaleMost = 62, kScaleBias = 127;
 
 inline int scale_blocks(int rows) { return rows / kScaleRows + (rows % kScaleRows != 0); }

@@ -170,7 +170,6 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     float m_ref = klim >= t0 * TN ? kNoWeight : -INFINITY, l_run = 0.f;
-    int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
 
     // ---- per-lane LDS read pointers (sdpa_fwd_kernel.h's; in compact rows the swizzle of K touches the low two bits of a chunk's index only and V has
     // none, so that two pointers and one serve all columns)
@@ -193,7 +192,6 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
     f32x16 sacc[NB];
     f16x8 pb[NB][2];
     auto hidden = [&](int key0, int nb, int i) __attribute__((always_inline)) { return key0 + nb * 32 + (i >> 2) * 8 + (i & 3) > klim; };
-    struct Sums { float p, l; };
     auto exponentials = [&](int row0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
         const int key0 = row0 + g * 4;
         float sum[NB];
@@ -211,26 +209,27 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
             }
             sum[nb] = part[0] + part[1];
         }
-        return Sums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1]};
+        return TileSums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1], {sum[0], sum[1]}};
     };
     auto softmax = [&](int row0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
-        Sums ps = exponentials(row0, x8, mask_tag);
-        const bool over = !(ps.p <= kLazyLimit8);                 // also inf (first score) and NaN
-        if (__builtin_amdgcn_ballot_w64(over || x8.far_lane) != 0) {
+        TileSums ps = exponentials(row0, x8, mask_tag);
+        auto least = [&](int nb) __attribute__((always_inline)) { return !decltype(mask_tag)::value || !hidden(row0 + g * 4, nb, 0) ? kSmall : 0u; };
+        if (__builtin_amdgcn_ballot_w64(ps.unusual({least(0), least(1)})) != 0) {
             // Eq. 2 for the rows that are over the limit (the two lanes of a row together): the tile's maximum, new reference, the rescale of Eqs. 3-4
             const int key0 = row0 + g * 4;
-            float m_tile = -INFINITY;
+            float m_tile = -INFINITY, most[NB];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (!decltype(mask_tag)::value || !hidden(key0, nb, i)) mx = fmaxf(mx, sacc[nb][i]);
-                m_tile = fmaxf(m_tile, mx * x8.ck[nb] + x8.ev[nb]);
+                most[nb] = mx * x8.ck[nb] + x8.ev[nb];
+                m_tile = fmaxf(m_tile, most[nb]);
             }
             m_tile = pair_max(m_tile) - kRoom;
-            const bool grow = pair_max(over ? 1.f : 0.f) > 0.f && m_tile > m_ref;
-            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
+            const bool grow = pair_max(ps.p <= kLazyLimit8 ? 0.f : 1.f) > 0.f && m_tile > m_ref;
+            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;
             l_run = l_run * half * half;
 #pragma unroll
@@ -238,8 +237,8 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
 #pragma unroll
                 for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
             float l = 0.f;
-            const bool far = x8.far();
-            if (__builtin_expect(far, 0)) {
+            const bool apart = __builtin_amdgcn_ballot_w64(small_weights(most[0] - m_ref, most[1] - m_ref)) != 0;
+            if (__builtin_expect(apart, 0)) {
                 float m_l = m_ref;
                 asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 32 registers)
 #pragma unroll
@@ -251,7 +250,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
                     }
             }
             ps = exponentials(row0, x8, mask_tag);
-            if (far) ps.l = l;
+            if (apart) ps.l = l;
         }
         l_run += ps.l;
     };
@@ -342,7 +341,7 @@ sdpa_cache8_chunk_kernel(const T *__restrict__ q, T *__restrict__ o, float *__re
             }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
-            const TileScales x8(scale_now, c, top);
+            const TileScales x8(scale_now, c);
             softmax(j * TN, x8, mask_tag);
             if constexpr (MASK) {
                 if (causal && has_nan(VS)) take_nan(j * TN + g * 4, VS);

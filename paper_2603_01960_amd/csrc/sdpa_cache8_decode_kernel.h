@@ -5,7 +5,7 @@
 // and O = o / l: the scales cost nothing per value.  EK folds into the factor of the score, EV into the exponent, so that m goes by the greatest
 // score PLUS exponent seen (kRoom in sdpa_cache8_values.h): the weights that enter the products are sized by what they contribute, and the products, whose weights and
 // values are both FP16 here whatever the type of q (every code is an FP16 number), keep 11 bits of the largest contributions.  l takes
-// the exponent out again, in FP32, and where exponents lie so far apart that p_j may be none of its normal numbers, before the exponential is taken (kFar).
+// the exponent out again, in FP32, and where p_j may be none of its normal numbers before the exponential is taken (kSmall).
 //
 // Such a call is bound by reading the cache once.  As in sdpa_decode_kernel.h each wavefront streams tiles of its own through LDS slots
 // of its own, with no barrier in the loop: one slot for K and one for V, each refilled as soon as it has been read into registers.  A
@@ -304,7 +304,6 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
     float m_ref = klim >= t0 * kTile8 ? kNoWeight : -INFINITY, l_run = 0.f;      // the lazy reference of sdpa_fwd_kernel.h, this lane's share of the normaliser
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
 
     // ---- pointers of the reads
     uint32_t kptr[G::NKP], vptr[G::NVP];
@@ -321,7 +320,6 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
 
     f16x8 pb[2];
     // weights of one tile: their sum (what the lazy limit looks at) and their part of l
-    struct Sums { float p, l; };
     auto exponentials = [&](const f32x4 (&s)[4], int key0, const TileScales &x8, auto mask_tag) __attribute__((always_inline)) {
         float sum[2];
 #pragma unroll
@@ -336,20 +334,21 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
                 pb[kb][x] = (_Float16)p;
             }
         }
-        return Sums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1]};
+        return TileSums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1], {sum[0], sum[1]}};
     };
     auto softmax = [&](f32x4 (&s)[4], int key0, const TileScales &x8, bool first_tile, auto mask_tag) __attribute__((always_inline)) {
-        Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
+        TileSums ps{INFINITY, 0.f, {0.f, 0.f}};   // (against kNoWeight any weight overflows: the first tile is not asked)
         if (!first_tile) ps = exponentials(s, key0, x8, mask_tag);
-        if (__builtin_amdgcn_ballot_w64(!(ps.p <= kLazyLimit8) || x8.far_lane) != 0) {             // also inf and NaN
+        auto least = [&](int kb) __attribute__((always_inline)) { return !decltype(mask_tag)::value || key0 + kb * 32 <= klim ? kSmall : 0u; };
+        if (__builtin_amdgcn_ballot_w64(ps.unusual({least(0), least(1)})) != 0) {
             // Eq. 2 for all rows of the wavefront: the tile's maximum, new reference and the rescale of Eqs. 3-4
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int x = 0; x < 16; ++x)
                 if (!decltype(mask_tag)::value || key0 + (x >> 2) * 16 + (x & 3) <= klim) mx[x >> 3] = fmaxf(mx[x >> 3], s[x >> 2][x & 3]);
-            const float m_tile = quad_max(fmaxf(mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1])) - kRoom;
+            const float most[2] = {mx[0] * x8.ck[0] + x8.ev[0], mx[1] * x8.ck[1] + x8.ev[1]}, m_tile = quad_max(fmaxf(most[0], most[1])) - kRoom;
             const bool grow = m_tile > m_ref;     // (a row without finite scores so far: -inf or NaN, left alone)
-            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
+            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;
             l_run = l_run * half * half;
 #pragma unroll
@@ -357,10 +356,10 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
 #pragma unroll
                 for (int e = 0; e < 4; ++e) oacc[db][e] *= alpha;
             float l = 0.f;
-            const bool far = x8.far();
-            if (__builtin_expect(far, 0)) {
+            const bool apart = __builtin_amdgcn_ballot_w64(small_weights(most[0] - m_ref, most[1] - m_ref)) != 0;
+            if (__builtin_expect(apart, 0)) {
                 float m_l = m_ref;
-                asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 32 registers)
+                asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 16 registers)
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
                     const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 2][x & 3], x8.ck[x >> 3], x8.ev[x >> 3] - m_l) - x8.ev[x >> 3]);
@@ -368,7 +367,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
                 }
             }
             ps = exponentials(s, key0, x8, mask_tag);
-            if (far) ps.l = l;
+            if (apart) ps.l = l;
         }
         l_run += ps.l;
     };
@@ -388,7 +387,7 @@ sdpa_cache8_decode_kernel(const T *__restrict__ q, T *o, float *__restrict__ lse
         load_k(s);
         int scale_now = scale_next;
         asm volatile("" : "+v"(scale_now));       // (not looked at before: a wait for it there would be one for V)
-        const TileScales scale(scale_now, c, top);
+        const TileScales scale(scale_now, c);
         f32x4 sacc[4];
 #pragma unroll
         for (int blk = 0; blk < 4; ++blk) sacc[blk] = f32x4{0.f, 0.f, 0.f, 0.f};

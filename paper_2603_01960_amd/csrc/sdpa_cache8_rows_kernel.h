@@ -276,7 +276,6 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     float m_ref = kNoWeight, l_run = 0.f;
-    int top = 0;                                  // greatest exponent byte in the tiles so far: see TileScales
     uint32_t kptr[G::NKP], vptr[DB];
 #pragma unroll
     for (int i = 0; i < G::NKP; ++i) kptr[i] = __builtin_bit_cast(uint32_t, kslot) + l32 * G::ROW + (G::k_at(2 * i + g, l32) << 4);
@@ -288,7 +287,6 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
     f32x16 sacc[NB];
     f16x8 pb[NB][2];
     auto key_of = [](int nb, int i) __attribute__((always_inline)) { return nb * 32 + (i >> 2) * 8 + (i & 3); };
-    struct Sums { float p, l; };
     auto exponentials = [&](const TileScales &x8) __attribute__((always_inline)) {
         float sum[NB];
 #pragma unroll
@@ -304,25 +302,25 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
             }
             sum[nb] = part[0] + part[1];
         }
-        return Sums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1]};
+        return TileSums{sum[0] + sum[1], sum[0] * x8.ew[0] + sum[1] * x8.ew[1], {sum[0], sum[1]}};
     };
     // (of a masked tile the scores have EV already, and x8 has none: `ev` is what it was)
-    auto softmax = [&](const TileScales &x8, const float (&ev)[NB], bool first_tile) __attribute__((always_inline)) {
-        Sums ps{INFINITY, 0.f};                   // (against kNoWeight any weight overflows: the first tile is not asked)
+    auto softmax = [&](const TileScales &x8, const float (&ev)[NB], const uint32_t (&least)[NB], bool first_tile) __attribute__((always_inline)) {
+        TileSums ps{INFINITY, 0.f, {0.f, 0.f}};   // (against kNoWeight any weight overflows: the first tile is not asked)
         if (!first_tile) ps = exponentials(x8);
-        const bool over = !(ps.p <= kLazyLimit8);  // also inf and NaN
-        if (__builtin_amdgcn_ballot_w64(over || x8.far_lane) != 0) {
-            float m_tile = -INFINITY;
+        if (__builtin_amdgcn_ballot_w64(ps.unusual(least)) != 0) {
+            float m_tile = -INFINITY, most[NB];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[nb][i]);
-                m_tile = fmaxf(m_tile, mx * x8.ck[nb] + x8.ev[nb]);
+                most[nb] = mx * x8.ck[nb] + x8.ev[nb];
+                m_tile = fmaxf(m_tile, most[nb]);
             }
             m_tile = pair_max(m_tile) - kRoom;
-            const bool grow = pair_max(over ? 1.f : 0.f) > 0.f && m_tile > m_ref;
-            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (kFar: l may count where alpha is 0)
+            const bool grow = pair_max(ps.p <= kLazyLimit8 ? 0.f : 1.f) > 0.f && m_tile > m_ref;
+            const float half = grow ? __builtin_amdgcn_exp2f((m_ref - m_tile) * 0.5f) : 1.f, alpha = half * half;     // (l may count where alpha is 0)
             m_ref = grow ? m_tile : m_ref;
             l_run = l_run * half * half;
 #pragma unroll
@@ -330,8 +328,8 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
 #pragma unroll
                 for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
             float l = 0.f;
-            const bool far = x8.far();
-            if (__builtin_expect(far, 0)) {
+            const bool apart = __builtin_amdgcn_ballot_w64(small_weights(most[0] - m_ref, most[1] - m_ref)) != 0;
+            if (__builtin_expect(apart, 0)) {
                 float m_l = m_ref;
                 asm("" : "+v"(m_l));              // (else the arguments below are kept for the exponentials that follow: 32 registers)
 #pragma unroll
@@ -340,7 +338,7 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
                     for (int i = 0; i < 16; ++i) l += __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[nb][i], x8.ck[nb], x8.ev[nb] - m_l) - ev[nb]);
             }
             ps = exponentials(x8);
-            if (far) ps.l = l;
+            if (apart) ps.l = l;
         }
         l_run += ps.l;
     };
@@ -369,21 +367,23 @@ sdpa_cache8_rows_kernel(const T *__restrict__ q, T *__restrict__ o, float *__res
                     sacc[nb] = Elem<T>::mfma(Codes<T>::wide(kf[nb][kk >> 1][(kk & 1) * 2], kf[nb][kk >> 1][(kk & 1) * 2 + 1]), qf[kk], sacc[nb]);
         }
         __builtin_amdgcn_s_setprio(0);
-        TileScales x8(scale_next, c, top);
+        TileScales x8(scale_next, c);
         const bool masked = tile * TN + TN - 1 > klim_least;
         const int last = klim - (tile * TN + g * 4);          // the last of the tile's keys that this lane's row sees, from the lane's first
         const float ev[NB] = {x8.ev[0], x8.ev[1]};
+        uint32_t least[NB] = {kSmall, kSmall};
         if (masked) {
             // scores as they enter the softmax, -inf for hidden keys (a factor of 0 would make them NaN)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sacc[nb][e] = key_of(nb, e) > last ? -INFINITY : __builtin_fmaf(sacc[nb][e], x8.ck[nb], x8.ev[nb]);
+                if (nb * 32 > last) least[nb] = 0u;
                 x8.ck[nb] = 1.f;
                 x8.ev[nb] = 0.f;
             }
         }
-        softmax(x8, ev, i == 0);
+        softmax(x8, ev, least, i == 0);
         u32x2 vf[DB][4];
         TSDPA_WAIT_VMCNT(NU);
         ReadRows<D>::values(vf, vptr);

@@ -73,25 +73,40 @@ template <bool PAGED> __device__ __forceinline__ int tile_scale_bytes(const Cach
 // key's value is 0.)
 constexpr float kRoom = 7.f, kLazyLimit8 = 0x1p15f;
 
-// A key counts in l by 2^(score - m), and its weight is 2^(score + EV - m), m + kRoom being the greatest score plus EV: of two keys that count alike one may have EV = 62, the other
-// -62, and keys of 2^-24 of another, or many of less, still count.  So l is the sum of the weights times 2^-EV only as long as these are in FP32's normal range, below which
-// the exponential gives 0: weights that count are 2^-(kFar + 24) of the greatest or more where EV is at most kFar below the greatest that the wavefront
-// has met.  In tiles with a block that is further below, l is the sum of exponentials of its own, from which EV is taken before: 2^(-62 - 24) of the
-// greatest weight at least, and 2^77 at most.  (2^-126 leaves 32 and 40 powers of two to keys that count only because they are many.)
-constexpr int kFar = 70;
+// A key counts in l by 2^(score - m), and its weight is 2^(score + EV - m), m + kRoom being the greatest score plus EV: of two keys that count alike one may have EV = 62, the
+// other -62, and keys of 2^-24 of another, or many of less, still count.  So l is the sum of the weights times 2^-EV only where these are in FP32's normal range, below which
+// the exponential gives 0.  Which is known by the sum of a lane's weights of a block, 8 or 16 keys: from kSmall on, what is lost is 2^-32 of that sum or less.  Below that,
+// 2^-97 of the row's greatest weight, the tile's part of l is a sum of exponentials of its own, from which EV is taken before: 2^(-62 - 24) at least, with 40 powers of two
+// to spare for keys that count because they are many, and 2^77 at most.  (To compare EV itself with the greatest so far in each tile took 6 % more time of large tiles at D = 64.)
+constexpr float kSmallLog2 = -90.f;
+constexpr uint32_t kSmall = (uint32_t)(127 + (int)kSmallLog2) << 23;
 
-// Of a tile's two blocks: c * 2^EK, EV, 2^-EV; and in the lanes that have V's exponents whether one is far below the greatest so far (`top`, of bytes).
+// Weights of a tile, in a lane: their sum, their part of l, and the blocks' sums.
+struct TileSums {
+    float p, l, block[2];
+    // p above the lazy limit, inf or NaN, or a block's sum less than `least`, the bits of kSmall (or 0: of which the row sees no key).  One comparison, of the bits of numbers that
+    // are not negative: what is less is 2^31 and more above, and what is not less below the limit's.
+    __device__ __forceinline__ bool unusual(const uint32_t (&least)[2]) const
+    {
+        const uint32_t x = __builtin_bit_cast(uint32_t, block[0]) - least[0], y = __builtin_bit_cast(uint32_t, block[1]) - least[1];
+        const uint32_t most = x > y ? x : y, all = __builtin_bit_cast(uint32_t, p);
+        return (all > most ? all : most) > __builtin_bit_cast(uint32_t, kLazyLimit8);
+    }
+};
+
+// Whether one of a lane's greatest weights of the two blocks, in powers of two, is small, and not 0 (-infinity: no key that the row sees).
+__device__ __forceinline__ bool small_weights(float a, float b)
+{
+    const uint32_t first = __builtin_bit_cast(uint32_t, kSmallLog2) + 1, x = __builtin_bit_cast(uint32_t, a) - first, y = __builtin_bit_cast(uint32_t, b) - first;
+    return (x < y ? x : y) < __builtin_bit_cast(uint32_t, -INFINITY) - first;
+}
+
+// Of a tile's two blocks: c * 2^EK, EV, 2^-EV.
 struct TileScales {
     float ck[2], ev[2], ew[2];
-    bool far_lane;
-    __device__ __forceinline__ bool far() const { return __builtin_amdgcn_ballot_w64(far_lane) != 0; }
-    __device__ __forceinline__ TileScales(int x, float c, int &top)
+    __device__ __forceinline__ TileScales(int x, float c)
     {
         x = x < kScaleBias - kScaleMost ? kScaleBias - kScaleMost : (x < kScaleBias + kScaleMost ? x : kScaleBias + kScaleMost);
-        const int other = __builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, false);       // quad_perm: the other block's
-        top = x > top ? x : top;
-        top = other > top ? other : top;
-        far_lane = x + ((threadIdx.x & 2) ? kFar : 1 << 16) < top;
         const float power = __builtin_bit_cast(float, x << 23) * c, e = (float)(x - kScaleBias), inverse = __builtin_bit_cast(float, (2 * kScaleBias - x) << 23);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {

@@ -71,7 +71,7 @@ def patterns(blocks):
         "one high key": ([TOP] + [LOW] * (blocks - 1), [alone] + [-3.0] * (blocks - 1)),
         "one low block": ([TOP] * (blocks - 1) + [LOW], [-6.0] * (blocks - 1) + [0.0]),
         **{f"apart by {n}": ([TOP if i % 2 == 0 else TOP - n for i in range(blocks)], [-1.0 if i % 2 == 0 else -3.0 * (i % 4 == 3) for i in range(blocks)])
-           for n in (69, 70, 71, 100)},
+           for n in (70, 90, 94, 97, 100, 110, 123)},
         "low first, less": ([LOW] * half + [TOP] * (blocks - half), [-6.0] * half + [0.0] * (blocks - half)),
         "low first, equal": ([LOW] * half + [TOP] * (blocks - half), [0.0] * blocks),
         "all between": ([LOW + 124 * i // (blocks - 1) for i in range(blocks)], [-2.0 * (i % 4) for i in range(blocks)]),
