@@ -305,11 +305,14 @@ bool incomplete(const tsdpa_cache8 &c) { return !c.k || !c.v || !c.k_scales || !
 // (sdpa_cache8_chunk_kernel.h).  Tiles of 128 do a seventh less work per row, but have to be filled, and a wavefront of theirs passes over four times
 // as many keys: tiles of 32 where those of 128 would be half empty (3.5 of them cost as much as one), and up to 2^27 scores.  Where entries have
 // lengths of their own, these may be much shorter than the capacity, and unequal, both of which cost large tiles more: up to 2^28 scores, or 1024 tiles.
-// (us, tiles of 32 / of 128, BF16, D = 128: 8 heads of 64 rows, 8192 keys 13.0 / 22.3; 8 of 256 rows, 2048 keys 12.4 / 22.6, 8192 keys 20.5 / 32.5, 65536 keys
-// 88 / 90; 32 of 512, 2048 keys 25.5 / 38.7; 8 of 1024, 8192 keys 45 / 51, 65536 keys 307 / 271; 64 of 512, 4096 keys 83 / 84; 8 of 4096, 8192 keys 149 / 141;
-// 8 of 16384, 16384 keys 1042 / 899; 1024 of 64, 2048 keys 124 / 164; 4 entries of 8 heads of 2000 rows, 2560 keys each 102 / 93, 1408 ... 3712 keys 103 / 112.  In
-// pages, a capacity of 131072 keys: 8 heads of 256 rows, 2000 keys 17 / 30, 120000 keys 150 / 165; of 2048 rows 26 / 43, 1112 / 1023; of 4096 rows 43 / 59, 2186 / 2017; 8
-// entries of 8 heads, capacity 32768: 512 rows, 800 ... 1500 keys 37 / 49, 15300 ... 16000 keys 296 / 296; 2048 rows 109 / 103, 1132 / 1068.)
+// (us, tiles of 32 / of 128, BF16, D = 128: 8 heads of 64 rows, 8192 keys 13.5 / 21.6; 8 of 256 rows, 2048 keys 12.0 / 22.3, 8192 keys 19.0 / 28.8, 65536 keys
+// 81 / 80; 32 of 512, 2048 keys 24.6 / 38.2; 8 of 1024, 8192 keys 44 / 49, 65536 keys 284 / 259; 64 of 512, 4096 keys 80 / 81; 8 of 4096, 8192 keys 140 / 133; 8
+// of 16384, 16384 keys 969 / 859; 1024 of 64, 2048 keys 122 / 160; 4 entries of 8 heads of 2000 rows, 2560 keys each 100 / 91, 1408 ... 3712 keys 100 / 103.  In
+// pages, a capacity of 131072 keys: 8 heads of 256 rows, 2000 keys 16 / 28, 120000 keys 150 / 152; of 2048 rows 25 / 41, 1047 / 1002; of 4096 rows 41 / 55, 2073 / 1985; 8
+// entries of 8 heads, capacity 32768: 512 rows, 800 ... 1500 keys 35 / 44, 15300 ... 16000 keys 293 / 293; 2048 rows 108 / 93, 1109 / 1054.)
+// Of 17 ... 32 rows two tiles of 16 each read and convert the keys, which few heads have room for and many have not (us, 32 rows, tiles of 16 / of 32: D = 128, 8 heads of 512
+// keys 7.0 / 8.0, of 8192 10.6 / 11.7, of 32768 19.0 / 18.3, 64 heads of 2048 12.9 / 15.0, of 8192 33.6 / 30.1, 256 of 2048 33.8 / 25.6; D = 64, 64 heads of 8192 28.1 / 16.9: tiles of 32
+// would be right for many heads and long caches, and are not taken there yet).
 enum class Form { decode, rows, chunk };
 constexpr int kDecodeRows = 32;
 Form form_of(int heads, int rows, int Skv, bool lengths)
@@ -348,6 +351,8 @@ int row_splits(int64_t tiles, int Skv, int D, bool lengths)
 // 11.5 / 10.5 / 8.9 / 8.1 / 9.6; of 8192 33.5 / 21.8 / 14.7 / 11.1 / 10.0, 32 splits 9.6; 64 heads of 1024 keys 7.9 / 8.9 / 8.6, of 4096 18.8 / 15.7
 // / 15.8 / 16.2; 90 heads of 4001, D = 96, 17.4 / 15.6 / 16.6; 32 rows per head: 8 heads of 1024 keys 10.1 / 13.0 / 12.6, of 2048 13.9 / 13.9 / 11.7, D = 64 7.3 / 9.7 / 9.4, 10.0 / 10.1
 // / 9.5.)
+// The bounds, at 1 / 2 / 3 / 4 splits: 40 heads of 1484 keys, D = 128 9.9 / 9.9 / 9.3 / 9.2, of 1679 10.9 / 10.8 / 10.1 / 9.2; of 1187, D = 160 10.3 / 10.9 / 10.0 / 9.9; 90 heads of 1835 keys, D = 128
+// 11.9 / 12.1 / 15.5, of 2109 12.8 / 13.4; of 1468, D = 160 11.5 / 12.5, of 1687 12.6 / 14.0.  (At D = 64 they are too high: 40 heads of 2968 keys 11.6 / 10.1 / 9.0 / 8.5, 90 of 3671 14.6 / 12.3.)
 // From half as many key/value heads as CUs on none either, with two exceptions where runs are long.  CUs get equal shares of the memory's rate, and one
 // reaches 2.4 times that at most (58 GB/s): so 128 heads do not reach it all, and of 257 ... 448 heads those that share a CU take twice as
 // long (1 / 2 / 3 splits, FP16: 128 heads of 2048 keys 13.3 / 16.4, of 4096 28.0 / 28.7, of 8192 54 / 51, in pages 60 / 54, of 16384 100 / 96, 113 / 99; 192 of 16384 133 / 145;

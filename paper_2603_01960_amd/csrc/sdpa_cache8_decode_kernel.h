@@ -12,9 +12,9 @@
 // tile is 64 keys, as many bytes as 32 keys of 16 bits, so that as many are in flight.
 //
 // Measured (D = 128, from call to call): 4 entries of 65536 keys, 8 heads of 4 rows, BF16, 537 MB in 96 us, 5.6 TB/s, where a stream that only reads reaches 6.1; 32
-// entries of 2048 ... 8192 keys in pages, FP16, 336 MB in 70 us, for the longest of which (one workgroup per CU, 64 KB on their way) the rest waits; one
-// entry of 8192 keys in 32 runs 9.0 us, of which the kernel is 7.0 (prologue and the first keys 3.5, four tiles, the states' way to memory) and their
-// combination 2.1 ... 3.0.  Eight or two wavefronts per workgroup and 32 rows per wavefront (spilled) were no faster.
+// entries of 2048 ... 8192 keys in pages, FP16, 336 MB in 69 us, for the longest of which (one workgroup per CU, 64 KB on their way) the rest waits; one
+// entry of 8192 keys in 32 runs 9.3 us, of which the kernel is 7.2 (prologue and the first keys 3.5, four tiles, the states' way to memory) and their
+// combination 2.1 ... 2.9.  Eight or two wavefronts per workgroup and 32 rows per wavefront (spilled) were no faster.
 #pragma once
 #include "sdpa_cache8_values.h"
 #include "sdpa_runs.h"

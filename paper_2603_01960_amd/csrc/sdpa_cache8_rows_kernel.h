@@ -6,9 +6,9 @@
 // four states meet in the LDS at the end.  The products are 32 x 32 and the softmax is that of the chunks.
 //
 // A tile is converted by the wavefront that uses it, for 32 rows: with the softmax that is about a fifth more time on the vector units than the products take
-// on the matrix units, and bounds the kernel where the GPU is full (16384 rows of 8 heads, 16384 keys, D = 128: 1042 us, where tiles of 128 rows, which convert
-// a quarter as often, take 899).  Where it is not full, a wavefront's number of tiles does: a quarter of what a tile of 128 rows passes over in its four (8
-// heads of 64 rows, 8192 keys, D = 128, in 16 runs: 13.0 us, 22.3 in tiles of 128; a 16-bit cache 13.7).  Registers hold two workgroups per CU at D = 128
+// on the matrix units, and bounds the kernel where the GPU is full (16384 rows of 8 heads, 16384 keys, D = 128: 969 us, where tiles of 128 rows, which convert
+// a quarter as often, take 859).  Where it is not full, a wavefront's number of tiles does: a quarter of what a tile of 128 rows passes over in its four (8
+// heads of 64 rows, 8192 keys, D = 128, in 16 runs: 13.5 us, 21.6 in tiles of 128; a 16-bit cache 12.5).  Registers hold two workgroups per CU at D = 128
 // and above; hidden keys are taken out of the scores before the softmax, which therefore is there once: with masked and unmasked forms of it
 // the compiler spilled in all loops from D = 128 on.
 #pragma once
